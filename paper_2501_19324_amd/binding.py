@@ -410,3 +410,10 @@ def rsd_probe_attention(ctx: Context, model: int, ctx_len: np.ndarray, reps: int
     ms = C.c_double()
     ctx.check(load_library().rsd_probe_attention(ctx.handle, C.c_int32(model), _np_ptr(cl), C.c_int32(reps), C.byref(ms)))
     return ms.value
+
+
+# the operators of include/rsd_ops.h (they use this module's library and errors)
+from .ops import *  # noqa: E402,F401,F403
+from .ops import __all__ as _ops_all  # noqa: E402
+
+__all__ += _ops_all

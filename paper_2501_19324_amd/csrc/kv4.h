@@ -1,0 +1,580 @@
+// A paged KV cache held in 4 bits: writing and reading entries, attention, eviction.
+//
+// Page [kv head][HD * 17 bytes], 16 tokens.  Keys: quarter q of the head dimension, token t, HD/8 bytes: lane l = 16 q + t of a wave loads its
+// part of the page as one vector, the A operand of the products q.K (rows: tokens) after the conversion to bf16.  Values: lane l = 16 c + m
+// loads for tokens 4 c .. + 3 the dims m and m + 16 of every group of 32: byte [group][token % 4] holds that pair, so the conversion (one scale for both values of a
+// byte) sees one token and one group at a time.  Four tokens' pairs are transposed by byte permutes into the A operands of the products
+// V^T P^T (rows: dims), whose contraction order (tokens 4 c + i of one page, then of the next) is the layout in which the matrix instruction
+// leaves the scores: the probabilities go from one product into the other without leaving their lanes.
+// A byte belongs to one token: entries are written without reading their neighbours.
+#pragma once
+#include "q4.h"
+
+#define KV4_PAGE 16
+#define KV4_CHUNK 64        // tokens a wave takes at once
+
+struct Kv4Cache {
+    uint8_t* pool;
+    const int* table;       // [batch][max_pages]
+    int* kv_len;            // [batch]
+    int n_pages, hkv, batch, max_pages;
+};
+__device__ __forceinline__ int64_t kv4_block(int hd) { return (int64_t)hd * 17; }
+// address of a (page, head) block; a table entry outside the pool gives null
+__device__ __forceinline__ uint8_t* kv4_page(const Kv4Cache& c, int hd, int seq, int page, int head) {
+    const int p = c.table[(int64_t)seq * c.max_pages + page];
+    return (unsigned)p < (unsigned)c.n_pages ? c.pool + ((int64_t)p * c.hkv + head) * kv4_block(hd) : nullptr;
+}
+// places of one entry's bytes inside its block
+__device__ __forceinline__ int kv4_key_at(int hd, int t, int dim) { return dim / (hd / 4) * 2 * hd + t * (hd / 8) + dim % (hd / 4) / 2; }
+__device__ __forceinline__ int kv4_val_at(int hd, int t, int g, int m) { return 8 * hd + (t >> 2) * 2 * hd + m * (hd / 8) + g * 4 + (t & 3); }
+__device__ __forceinline__ int kv4_key_scale_at(int hd, int t, int g) { return 16 * hd + g * 16 + t; }
+__device__ __forceinline__ int kv4_val_scale_at(int hd, int t, int g) { return 16 * hd + hd / 2 + ((t >> 2) * (hd / 32) + g) * 4 + (t & 3); }
+
+struct Kv4Book {            // per entry: accumulated attention weight, position; either may be null
+    float* scores;
+    int* pos;
+    int64_t score_b, score_h, pos_b, pos_h;
+};
+
+// ---- entries in: 16 lanes take one group of 32 dims of one (row, head), keys and values
+template <typename T>
+__global__ void kv4_append_kernel(Kv4Cache c, int hd, const T* __restrict__ k, int64_t k_row, int64_t k_head, const T* __restrict__ v,
+                                  int64_t v_row, int64_t v_head, const int* __restrict__ seq, const int* __restrict__ slot,
+                                  const int* __restrict__ position, int rows, Kv4Book book) {
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int l = threadIdx.x & 15, groups = hd / 32;
+    const int g = (int)(item % groups), h = (int)(item / groups % c.hkv);
+    const int64_t row = item / groups / c.hkv;
+    if (row >= rows) return;
+    const int b = seq[row], s = slot[row];
+    if ((unsigned)b >= (unsigned)c.batch || (unsigned)s >= (unsigned)c.max_pages * KV4_PAGE) return;
+    uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
+    if (!block) return;
+    const int t = s % KV4_PAGE;
+    const T* kr = k + row * k_row + h * k_head + g * 32;
+    const T* vr = v + row * v_row + h * v_head + g * 32;
+    const float k0 = ld1(kr + 2 * l), k1 = ld1(kr + 2 * l + 1), v0 = ld1(vr + l), v1 = ld1(vr + 16 + l);
+    const bool kbad = row16_or(!q4_finite(k0) || !q4_finite(k1)) != 0, vbad = row16_or(!q4_finite(v0) || !q4_finite(v1)) != 0;
+    const int ke = q4_scale_byte(row16_max(fmaxf(fabsf(k0), fabsf(k1)))), ve = q4_scale_byte(row16_max(fmaxf(fabsf(v0), fabsf(v1))));
+    block[kv4_key_at(hd, t, g * 32 + 2 * l)] = kbad ? 0 : (uint8_t)q4_encode2(k0, k1, __uint_as_float((uint32_t)ke << 23));
+    block[kv4_val_at(hd, t, g, l)] = vbad ? 0 : (uint8_t)q4_encode2(v0, v1, __uint_as_float((uint32_t)ve << 23));
+    if (l == 0) {
+        block[kv4_key_scale_at(hd, t, g)] = kbad ? Q4_NAN : (uint8_t)ke;
+        block[kv4_val_scale_at(hd, t, g)] = vbad ? Q4_NAN : (uint8_t)ve;
+        if (g == 0 && book.scores) book.scores[b * book.score_b + h * book.score_h + s] = 0.f;
+        if (g == 0 && book.pos) book.pos[b * book.pos_b + h * book.pos_h + s] = position[row];
+    }
+}
+
+// ---- entries out: [rows][heads][hd], contiguous; a row that names no entry of the cache gives zeros
+template <typename T>
+__global__ void kv4_read_kernel(Kv4Cache c, int hd, const int* __restrict__ seq, const int* __restrict__ slot, int rows, T* __restrict__ k,
+                                T* __restrict__ v) {
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int l = threadIdx.x & 15, groups = hd / 32;
+    const int g = (int)(item % groups), h = (int)(item / groups % c.hkv);
+    const int64_t row = item / groups / c.hkv;
+    if (row >= rows) return;
+    const int b = seq[row], s = slot[row], t = s % KV4_PAGE;
+    uint32_t kk = 0, vv = 0;
+    if ((unsigned)b < (unsigned)c.batch && (unsigned)s < (unsigned)c.max_pages * KV4_PAGE) {
+        const uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
+        if (block) {
+            kk = q4_decode2<0>(block[kv4_key_at(hd, t, g * 32 + 2 * l)], (uint32_t)block[kv4_key_scale_at(hd, t, g)] << 23);
+            vv = q4_decode2<0>(block[kv4_val_at(hd, t, g, l)], (uint32_t)block[kv4_val_scale_at(hd, t, g)] << 23);
+        }
+    }
+    const int64_t o = (row * c.hkv + h) * hd + g * 32;
+    st1(k + o + 2 * l, __uint_as_float(kk << 16));
+    st1(k + o + 2 * l + 1, __uint_as_float(kk & 0xFFFF0000u));
+    st1(v + o + l, __uint_as_float(vv << 16));
+    st1(v + o + 16 + l, __uint_as_float(vv & 0xFFFF0000u));
+}
+
+// ---- attention
+struct Kv4Attn {
+    Kv4Cache c;
+    const void* q;
+    int64_t q_row, q_head;
+    const int* row_start;   // [batch + 1]; null: row b is sequence b's
+    int total_rows, max_rows, heads, group;
+    float factor2;          // scale * log2(e): exponents are taken to the base 2
+    void* out;
+    int64_t o_row, o_head;
+    float* lse;             // [rows][heads] or null
+    int max_kv, split, splits, tiles;
+    float* part_o;          // [rows][heads][splits][hd], unnormalised
+    float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
+    Kv4Book book;
+};
+// rows of sequence b: the first one and how many; entries it has
+__device__ __forceinline__ void kv4_rows(const Kv4Attn& a, int b, int& r0, int& count, int& n) {
+    r0 = b;
+    count = b < a.total_rows ? 1 : 0;
+    if (a.row_start) {
+        r0 = min(max(a.row_start[b], 0), a.total_rows);
+        count = min(min(max(a.row_start[b + 1], r0), a.total_rows) - r0, a.max_rows);
+    }
+    n = min(min(max(a.c.kv_len[b], 0), a.max_kv), a.c.max_pages * KV4_PAGE);
+}
+
+template <int HD> struct Kv4Keys { typename u32vec<HD / 32>::type w[4]; uint32_t scale[4]; };
+template <int HD> struct Kv4Vals { typename u32vec<HD / 32>::type w[4], scale[4]; };
+
+// the blocks of the four pages of a chunk; bit p of `there` is clear where the table names no page of the pool
+template <int HD> __device__ __forceinline__ void kv4_pages(const Kv4Cache& c, int seq, int head, int slot0, const uint8_t* page[4], int& there) {
+    there = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int id = __builtin_amdgcn_readfirstlane(c.table[(int64_t)seq * c.max_pages + min(slot0 / KV4_PAGE + p, c.max_pages - 1)]);
+        const bool ok = (unsigned)id < (unsigned)c.n_pages;
+        there |= ok << p;
+        page[p] = c.pool + ((int64_t)(ok ? id : 0) * c.hkv + head) * kv4_block(HD);
+    }
+}
+template <int HD> __device__ __forceinline__ void kv4_load_keys(const uint8_t* const page[4], int lane, Kv4Keys<HD>& k) {
+    typedef typename u32vec<HD / 32>::type V;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        k.w[p] = reinterpret_cast<const V*>(page[p])[lane];
+        k.scale[p] = page[p][16 * HD + (lane >> 4) * (HD / 4) / 32 * 16 + (lane & 15)];
+    }
+}
+template <int HD> __device__ __forceinline__ void kv4_load_vals(const uint8_t* const page[4], int lane, Kv4Vals<HD>& v) {
+    typedef typename u32vec<HD / 32>::type V;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        v.w[p] = reinterpret_cast<const V*>(page[p] + 8 * HD)[lane];
+        v.scale[p] = reinterpret_cast<const V*>(page[p] + 16 * HD + HD / 2)[lane >> 4];
+    }
+}
+// q of one tile of 16 columns as B operands [HD/32][plane]; column c of a (sequence, kv head) is row c / group, head c % group
+template <typename T, int HD, int PLANES>
+__device__ __forceinline__ void kv4_load_q(const Kv4Attn& a, int r0, int count, int head, int col, int lane, u32x4_t q[HD / 32][PLANES]) {
+    const int r = col / a.group, g = col % a.group;
+    const T* p = static_cast<const T*>(a.q) + (int64_t)(r0 + r) * a.q_row + (int64_t)(head * a.group + g) * a.q_head + (lane >> 4) * (HD / 4);
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = r < count ? ld1(p + j * 8 + i) : 0.f;
+        q4_operand<PLANES>(x, q[j]);
+    }
+}
+// scores of one page: rows (tokens) 4 (lane / 16) + i, column lane % 16
+template <int HD, int PLANES>
+__device__ __forceinline__ f32x4_t kv4_scores(const Kv4Keys<HD>& k, int p, const u32x4_t q[HD / 32][PLANES]) {
+    f32x4_t s = {};
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) {
+        const u32x4_t m = q4_decode8(k.w[p][j], k.scale[p] << 23);
+#pragma unroll
+        for (int x = 0; x < PLANES; ++x) s = q4_mfma(m, q[j][x], s);
+    }
+    return s;
+}
+// values of two pages, group g, as the A operands of dims 32 g .. + 15 (lo) and 32 g + 16 .. + 31 (hi)
+template <int HD> __device__ __forceinline__ void kv4_val_operands(const Kv4Vals<HD>& v, int p, int g, u32x4_t& lo, u32x4_t& hi) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t w = v.w[p + e][g], s = v.scale[p + e][g];
+        const uint32_t c0 = q4_decode2<0>(w, q4_scale_at<0>(s)), c1 = q4_decode2<1>(w, q4_scale_at<1>(s));
+        const uint32_t c2 = q4_decode2<2>(w, q4_scale_at<2>(s)), c3 = q4_decode2<3>(w, q4_scale_at<3>(s));
+        lo[2 * e] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
+        lo[2 * e + 1] = __builtin_amdgcn_perm(c3, c2, 0x05040100u);
+        hi[2 * e] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
+        hi[2 * e + 1] = __builtin_amdgcn_perm(c3, c2, 0x07060302u);
+    }
+}
+
+// An entry that reads as NaN must not reach the columns that do not see it (as 0 * NaN).  Such groups among the entries from slot `safe` on
+// are taken out of the product (scale byte 0), and the sums of the columns that do see the entry become NaN instead.
+template <int HD, int MT>
+__device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int safe, const int (&limit)[MT], f32x4_t (&o)[MT][HD / 16]) {
+    const int quad = (threadIdx.x & 63) >> 4;
+    uint32_t any = 0;
+    uint32_t marks[4][HD / 32];                             // bit 8 i + 7: token i of the quad is NaN in this group
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int from = safe - (slot0 + p * KV4_PAGE + quad * 4);
+        const uint32_t look = from <= 0 ? 0xFFFFFFFFu : from >= 4 ? 0u : 0xFFFFFFFFu << (8 * from);
+#pragma unroll
+        for (int g = 0; g < HD / 32; ++g) {
+            const uint32_t s = v.scale[p][g];
+            marks[p][g] = ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u & look;
+            any |= marks[p][g];
+        }
+    }
+    if (!__any(any != 0)) return;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int g = 0; g < HD / 32; ++g) {
+            v.scale[p][g] &= ~((marks[p][g] >> 7) * 255u);
+            for (int t = 0; t < KV4_PAGE; ++t) {            // every lane looks at every token of the page
+                const uint32_t m = (uint32_t)__builtin_amdgcn_readlane((int)marks[p][g], t / 4 * 16);
+                if (!((m >> (8 * (t % 4) + 7)) & 1)) continue;
+#pragma unroll
+                for (int c = 0; c < MT; ++c)
+                    if (slot0 + p * KV4_PAGE + t < limit[c]) {
+                        const float nan = __uint_as_float(0x7FC00000u);
+                        o[c][2 * g] = f32x4_t{nan, nan, nan, nan};
+                        o[c][2 * g + 1] = f32x4_t{nan, nan, nan, nan};
+                    }
+            }
+        }
+}
+
+// A block owns MT tiles of 16 columns of one (sequence, kv head) and one part of its entries, of which its four waves take chunks of 64
+// in turn, each with its own running maximum and sum; they are joined in LDS.
+template <typename T, int HD, int PLANES, int MT>
+__global__ __launch_bounds__(256) void kv4_attn_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32;
+    constexpr int PP = PLANES == 1 ? 2 : 3;                 // parts of a probability: see below
+    __shared__ __align__(16) float lds_o[4][MT][G * 2][64][4];
+    __shared__ float lds_ml[4][MT][2][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
+    const int bh = blockIdx.x / a.tiles, tile0 = blockIdx.x % a.tiles * MT;
+    const int b = bh / a.c.hkv, head = bh % a.c.hkv;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group;
+    if (tile0 * 16 >= cols) return;
+    // entries seen by the column's row: slots < limit
+    int limit[MT];
+    u32x4_t q[MT][G][PLANES];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int col = (tile0 + m) * 16 + (lane & 15);
+        limit[m] = col < cols ? n - (count - 1 - col / a.group) : 0;
+        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q[m]);
+    }
+    const int last_row = min(cols - 1, (tile0 + MT) * 16 - 1) / a.group;
+    const int begin = blockIdx.y * a.split, end = min(begin + a.split, n - (count - 1 - last_row));
+    const int safe = min(end, n - (count - 1 - tile0 * 16 / a.group));      // below: every column sees every entry
+
+    f32x4_t o[MT][2 * G] = {};
+    float top[MT], sum[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) top[m] = -INFINITY, sum[m] = 0.f;
+    for (int slot0 = begin + wave * KV4_CHUNK; slot0 < end; slot0 += 4 * KV4_CHUNK) {
+        const uint8_t* page[4];
+        int there;
+        kv4_pages<HD>(a.c, b, head, slot0, page, there);
+        Kv4Keys<HD> k;
+        Kv4Vals<HD> v;
+        kv4_load_keys<HD>(page, lane, k);
+        kv4_load_vals<HD>(page, lane, v);
+        const bool whole = slot0 + KV4_CHUNK <= safe && there == 15;
+        if (!whole) {
+            // Values that are not there, or not seen by all columns: what lies behind the last entry may read as NaN, and 0 * NaN is NaN.
+            // Their scales are cleared.
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int left = (there >> p) & 1 ? end - (slot0 + p * KV4_PAGE + quad * 4) : 0;
+                const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+                for (int g = 0; g < G; ++g) v.scale[p][g] &= keep;
+            }
+            if (slot0 + KV4_CHUNK > safe) kv4_nan_values<HD, MT>(v, slot0, safe, limit, o);
+        }
+        f32x4_t s[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                s[m][p] = kv4_scores<HD, PLANES>(k, p, q[m]) * a.factor2;
+                if (!whole) {
+                    const int end_p = (there >> p) & 1 ? min(limit[m], end) : 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[m][p][i] = slot0 + p * KV4_PAGE + quad * 4 + i < end_p ? s[m][p][i] : -INFINITY;
+                }
+            }
+            float best = -INFINITY;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) best = fmaxf(best, s[m][p][i]);
+            best = fmaxf(top[m], rows4_max(best));
+            const float base = best == -INFINITY ? 0.f : best;
+            const float scale = __builtin_amdgcn_exp2f(top[m] - base);
+            top[m] = best;
+            sum[m] *= scale;
+#pragma unroll
+            for (int d = 0; d < 2 * G; ++d) o[m][d] *= scale;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[m][p][i] = __builtin_amdgcn_exp2f(s[m][p][i] - base);
+                    sum[m] += s[m][p][i];
+                }
+        }
+        // Probabilities as operands: the sum of two bf16 numbers (16 bits) where the result is rounded to bf16, of three (all 24 bits) where it is fp32.
+#pragma unroll
+        for (int p = 0; p < 4; p += 2) {
+            u32x4_t w[MT][PP];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = s[m][p + i / 2][2 * (i % 2)], y = s[m][p + i / 2][2 * (i % 2) + 1];
+                    if constexpr (PP == 2) {
+                        uint32_t hi, lo;
+                        split2(x, y, hi, lo);
+                        w[m][0][i] = hi;
+                        w[m][1][i] = lo;
+                    } else {
+                        uint32_t a0, b0, c0, a1, b1, c1;
+                        q4_cut3(x, a0, b0, c0);
+                        q4_cut3(y, a1, b1, c1);
+                        w[m][0][i] = a0 | (a1 << 16);
+                        w[m][1][i] = b0 | (b1 << 16);
+                        w[m][2][i] = c0 | (c1 << 16);
+                    }
+                }
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                u32x4_t lo, hi;
+                kv4_val_operands<HD>(v, p, g, lo, hi);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int x = 0; x < PP; ++x) {
+                        o[m][2 * g] = q4_mfma(lo, w[m][x], o[m][2 * g]);
+                        o[m][2 * g + 1] = q4_mfma(hi, w[m][x], o[m][2 * g + 1]);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        sum[m] = rows4_sum(sum[m]);
+        if (quad == 0) lds_ml[wave][m][0][lane] = top[m], lds_ml[wave][m][1][lane] = sum[m];
+#pragma unroll
+        for (int d = 0; d < 2 * G; ++d) *reinterpret_cast<f32x4_t*>(lds_o[wave][m][d][lane]) = o[m][d];
+    }
+    __syncthreads();
+    for (int e = wave; e < MT * 2 * G; e += 4) {
+        const int m = e / (2 * G), d = e % (2 * G), c = lane & 15, col = (tile0 + m) * 16 + c;
+        float best = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) best = fmaxf(best, lds_ml[w][m][0][c]);
+        const float base = best == -INFINITY ? 0.f : best;
+        f32x4_t acc = {};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float scale = __builtin_amdgcn_exp2f(lds_ml[w][m][0][c] - base);
+            total += scale * lds_ml[w][m][1][c];
+            acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][m][d][lane]);
+        }
+        if (col >= cols) continue;
+        const int64_t row = r0 + col / a.group;
+        const int qh = head * a.group + col % a.group, dim = d * 16 + quad * 4;
+        if (a.splits > 1) {
+            const int64_t at = (row * a.heads + qh) * a.splits + blockIdx.y;
+            *reinterpret_cast<f32x4_t*>(a.part_o + at * HD + dim) = acc;
+            if (d == 0 && quad == 0) a.part_ml[at] = make_float2(best, total);
+        } else {
+            const float inv = total == 0.f ? 0.f : 1.f / total;
+            T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st1(dst + i, acc[i] * inv);
+            if (d == 0 && quad == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+        }
+    }
+}
+
+// joins the parts of the entries: one wave per (row, head)
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a, int hd) {
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= (int64_t)a.c.batch * a.max_rows * a.heads) return;
+    const int qh = (int)(id % a.heads), r = (int)(id / a.heads % a.max_rows), b = (int)(id / a.heads / a.max_rows);
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    if (r >= count) return;
+    // the blocks of this column's tile wrote a part for every split (an empty one where there was nothing to see)
+    const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;
+    float best = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) best = fmaxf(best, a.part_ml[at + s].x);
+    const float base = best == -INFINITY ? 0.f : best;
+    float total = 0.f, acc[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[at + s];
+        const float scale = __builtin_amdgcn_exp2f(ml.x - base);
+        total += scale * ml.y;
+        for (int d = lane, i = 0; d < hd; d += 64, ++i) acc[i] += scale * a.part_o[(at + s) * hd + d];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head;
+    for (int d = lane, i = 0; d < hd; d += 64, ++i) st1(dst + d, acc[i] * inv);
+    if (lane == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+}
+
+// Attention weight per entry, added to the accumulated one: the scores are computed a second time (keys are half of the cache; storing a
+// group's probabilities would move as many bytes), now with the final sum of every row.  A wave owns 64 entries of one (sequence, kv head): no atomics, one order.
+template <typename T, int HD, int PLANES>
+__global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group, slot0 = (blockIdx.y * 4 + wave) * KV4_CHUNK;
+    if (slot0 >= n || cols == 0) return;
+    const uint8_t* page[4];
+    int there;
+    kv4_pages<HD>(a.c, b, head, slot0, page, there);
+    Kv4Keys<HD> k;
+    kv4_load_keys<HD>(page, lane, k);
+    f32x4_t weight[4] = {};
+    for (int c0 = 0; c0 < cols; c0 += 16) {
+        const int col = c0 + (lane & 15), r = col / a.group;
+        const int limit = col < cols ? n - (count - 1 - r) : 0;
+        const float lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : 0.f;
+        u32x4_t q[G][PLANES];
+        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q) * a.factor2;
+            const int end = (there >> p) & 1 ? limit : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) weight[p][i] += slot0 + p * KV4_PAGE + quad * 4 + i < end ? __builtin_amdgcn_exp2f(s[i] - lse2) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w = row16_sum(weight[p][i]);
+            const int slot = slot0 + p * KV4_PAGE + quad * 4 + i;
+            if ((lane & 15) == 0 && slot < n && ((there >> p) & 1)) a.book.scores[b * a.book.score_b + head * a.book.score_h + slot] += w;
+        }
+}
+
+// ---- eviction
+struct Kv4Evict {
+    Kv4Cache c;
+    Kv4Book book;
+    int budget, recent;
+    int* plan;              // [batch][hkv][2 + 2 * moves]: entries moved, entries before, targets, sources
+    int moves;
+};
+// Scores as whole numbers of the same order; protected entries above all, NaN as -inf, both zeros alike
+__device__ __forceinline__ uint32_t kv4_rank_key(float score, bool safe) {
+    if (safe) return 0xFFFFFFFFu;
+    const uint32_t u = __float_as_uint(score != score ? -INFINITY : score + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// One block per (sequence, kv head): the key of the budget-th entry by four passes over eight bits each, then one pass in slot order that lists
+// the freed slots below the budget and the kept entries above it.
+__global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
+    __shared__ int hist[256], wsum[3][16], found[2];
+    __shared__ int newest_w[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
+    int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
+    const int n = min(max(a.c.kv_len[b], 0), a.c.max_pages * KV4_PAGE);
+    if (tid == 0) plan[0] = 0, plan[1] = n;
+    if (n <= a.budget) return;
+    const float* score = a.book.scores + b * a.book.score_b + h * a.book.score_h;
+    const int* pos = a.book.pos + b * a.book.pos_b + h * a.book.pos_h;
+    int newest = INT32_MIN;
+    for (int s = tid; s < n; s += 1024) newest = max(newest, pos[s]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) newest = max(newest, __shfl_xor(newest, d));
+    if (lane == 0) newest_w[wave] = newest;
+    __syncthreads();
+    for (int w = 0; w < 16; ++w) newest = max(newest, newest_w[w]);
+    // protected: position > newest - recent, in 64 bits (positions may be any int32)
+    const int64_t bound = (int64_t)newest - a.recent;
+    uint32_t key = 0;
+    int need = a.budget;                                    // entries still to be kept among those that agree with `key` so far
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
+        for (int s = tid; s < n; s += 1024) {
+            const uint32_t u = kv4_rank_key(score[s], pos[s] > bound);
+            if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255], 1);
+        }
+        __syncthreads();
+        if (wave == 0) {                                    // lane l: bins 255 - 4 l .. 252 - 4 l, from the top
+            int c[4], mine = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = hist[255 - 4 * lane - i], mine += c[i];
+            int before = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) { const int x = __shfl_up(before, d); if (lane >= d) before += x; }
+            before -= mine;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (before < need && before + c[i] >= need) found[0] = 255 - 4 * lane - i, found[1] = need - before;
+                before += c[i];
+            }
+        }
+        __syncthreads();
+        key |= (uint32_t)found[0] << shift;
+        need = found[1];
+        __syncthreads();
+    }
+    // keep: keys above, and the first `need` of those equal to it
+    int ties = 0, holes = 0, extras = 0;
+    for (int s0 = 0; s0 < n; s0 += 1024) {
+        const int s = s0 + tid;
+        const uint32_t u = s < n ? kv4_rank_key(score[s], pos[s] > bound) : 0u;
+        const bool tie = s < n && u == key;
+        const uint64_t tm = __ballot(tie);
+        if (lane == 0) wsum[0][wave] = __popcll(tm);
+        __syncthreads();
+        int rank = ties + __popcll(tm & ((1ull << lane) - 1));
+        int all = 0;
+        for (int w = 0; w < 16; ++w) { if (w < wave) rank += wsum[0][w]; all += wsum[0][w]; }
+        ties += all;
+        const bool keep = s < n && (u > key || (tie && rank < need));
+        const bool hole = s < a.budget && !keep, extra = s >= a.budget && keep;
+        const uint64_t hm = __ballot(hole), em = __ballot(extra);
+        if (lane == 0) wsum[1][wave] = __popcll(hm), wsum[2][wave] = __popcll(em);
+        __syncthreads();
+        int hr = holes + __popcll(hm & ((1ull << lane) - 1)), er = extras + __popcll(em & ((1ull << lane) - 1)), ha = 0, ea = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) hr += wsum[1][w], er += wsum[2][w];
+            ha += wsum[1][w], ea += wsum[2][w];
+        }
+        if (hole) plan[2 + hr] = s;
+        if (extra) plan[2 + a.moves + er] = s;
+        holes += ha;
+        extras += ea;
+        __syncthreads();
+    }
+    if (tid == 0) plan[0] = holes;
+}
+// one wave per moved entry
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int hd, int hkv) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
+    const int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
+    const int count = plan[0];
+    if (blockIdx.y == 0 && h == 0 && threadIdx.x == 0) a.c.kv_len[b] = min(plan[1], a.budget);
+    float* score = a.book.scores + b * a.book.score_b + h * a.book.score_h;
+    int* pos = a.book.pos + b * a.book.pos_b + h * a.book.pos_h;
+    for (int i = blockIdx.y * 4 + wave; i < count; i += gridDim.y * 4) {
+        const int to = plan[2 + i], from = plan[2 + a.moves + i], t1 = to % KV4_PAGE, t0 = from % KV4_PAGE;
+        uint8_t* dst = kv4_page(a.c, hd, b, to / KV4_PAGE, h);
+        const uint8_t* src = kv4_page(a.c, hd, b, from / KV4_PAGE, h);
+        if (dst && src) {
+            if (lane < hd / 2) {
+                dst[kv4_key_at(hd, t1, 2 * lane)] = src[kv4_key_at(hd, t0, 2 * lane)];
+                dst[kv4_val_at(hd, t1, lane >> 4, lane & 15)] = src[kv4_val_at(hd, t0, lane >> 4, lane & 15)];
+            }
+            if (lane < hd / 32) {
+                dst[kv4_key_scale_at(hd, t1, lane)] = src[kv4_key_scale_at(hd, t0, lane)];
+                dst[kv4_val_scale_at(hd, t1, lane)] = src[kv4_val_scale_at(hd, t0, lane)];
+            }
+        }
+        if (lane == 0) score[to] = score[from], pos[to] = pos[from];
+    }
+}

@@ -1,0 +1,283 @@
+// Entry points of include/rsd_ops.h: argument checks, launch shapes.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+
+#include "rsd_ops.h"
+#include "q4.h"
+#include "w4.h"
+#include "kv4.h"
+
+namespace {
+
+thread_local char op_error[256] = "";
+
+int fail(int code, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(op_error, sizeof(op_error), fmt, ap);
+    va_end(ap);
+    return code;
+}
+// the launches before this call: an error that an earlier, unrelated call left behind is not this call's
+struct Launches {
+    Launches() { (void)hipGetLastError(); }
+    int done(const char* what) {
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? RSD_OK : fail(RSD_EHIP, "%s: %s", what, hipGetErrorString(e));
+    }
+};
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool is_type(int32_t t) { return t == RSD_F32 || t == RSD_BF16; }
+size_t size_of(int32_t t) { return t == RSD_F32 ? 4 : 2; }
+uint64_t up256(uint64_t n) { return (n + 255) & ~255ull; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t kMostBlocks = 1ll << 22;      // blocks of at most 512 threads: a launch counts threads in 32 bits per dimension
+
+// ---- products with 4-bit weights
+
+struct W4Plan { int nt, kt, ks, rt, planes, tiles, row_tiles, splits, units, waves; uint64_t xs_bytes, part_bytes; };
+
+W4Plan w4_plan(int rows, int n, int k, int dtype) {
+    W4Plan p;
+    p.nt = (int)ceil_div(n, 16);
+    p.kt = (int)ceil_div(k, 128);
+    p.ks = (int)ceil_div(k, 512);
+    p.rt = (int)ceil_div(rows, 16);
+    p.planes = dtype == RSD_F32 ? 3 : 1;
+    p.tiles = 2;
+    p.row_tiles = p.rt == 1 ? 1 : p.rt == 2 ? 2 : 4;
+    p.splits = 1;
+    p.units = p.ks;
+    p.waves = std::min(8, std::max(1, p.ks));
+    p.xs_bytes = up256((uint64_t)p.rt * p.kt * p.planes * 4096);
+    p.part_bytes = p.splits > 1 ? up256((uint64_t)p.splits * rows * n * 4) : 0;
+    return p;
+}
+
+template <typename T, int NT, int R, int PLANES> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
+    const dim3 grid((unsigned)ceil_div(p.nt, NT), (unsigned)p.splits, (unsigned)ceil_div(p.rt, R));
+    w4_kernel<T, NT, R, PLANES><<<grid, 64 * p.waves, (size_t)p.waves * NT * R * 1024, st>>>(a);
+}
+template <typename T, int PLANES> void w4_run(const W4Plan& p, const W4Args& a, const void* x, int64_t ldx, hipStream_t st) {
+    const int64_t items = (int64_t)p.rt * p.kt * 256;
+    w4_stage_kernel<T, PLANES><<<(unsigned)(items / 256), 256, 0, st>>>(static_cast<const T*>(x), ldx, a.rows, a.k, a.kt,
+                                                                       reinterpret_cast<uint4*>(const_cast<u32x4_t*>(a.xs)));
+    if (p.row_tiles == 1) w4_launch<T, 2, 1, PLANES>(p, a, st);
+    else if (p.row_tiles == 2) w4_launch<T, 2, 2, PLANES>(p, a, st);
+    else w4_launch<T, 2, 4, PLANES>(p, a, st);
+    if (p.splits > 1)
+        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * a.n, 256), 256, 0, st>>>(a.part, p.splits, a.rows, a.n, static_cast<T*>(a.y), a.ldy);
+}
+
+// ---- the cache
+
+int check_cache(const rsd_kv4_cache* c, const char* what) {
+    if (!c || !c->pool || !c->table || !c->kv_len) return fail(RSD_EINVAL, "%s: null cache array", what);
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return fail(RSD_EINVAL, "%s: head_dim %d (32, 64 or 128)", what, c->head_dim);
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1 || c->max_pages > INT32_MAX / KV4_PAGE)
+        return fail(RSD_EINVAL, "%s: pages %d, kv heads %d, batch %d, pages per sequence %d", what, c->n_pages, c->n_kv_heads, c->batch, c->max_pages);
+    if ((int64_t)c->batch * c->n_kv_heads > kMostBlocks / 4) return fail(RSD_EINVAL, "%s: batch %d x %d kv heads", what, c->batch, c->n_kv_heads);
+    if (!aligned(c->pool, 16)) return fail(RSD_EINVAL, "%s: the pool is not 16-byte aligned", what);
+    return RSD_OK;
+}
+Kv4Cache dev_cache(const rsd_kv4_cache* c) {
+    return Kv4Cache{static_cast<uint8_t*>(c->pool), c->table, c->kv_len, c->n_pages, c->n_kv_heads, c->batch, c->max_pages};
+}
+Kv4Book dev_book(const rsd_kv4_book* b) {
+    return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
+}
+
+struct AttnPlan { int mt, tiles, split, splits; uint64_t o_bytes, ml_bytes, lse_bytes; };
+
+AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
+    AttnPlan p;
+    const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
+    const int64_t max_kv = std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KV4_PAGE);
+    p.mt = cols <= 16 ? 1 : 2;
+    p.tiles = (int)ceil_div(cols, 16 * p.mt);
+    const int64_t base = (int64_t)c->batch * c->n_kv_heads * p.tiles;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(1024, base), ceil_div(max_kv, 256)));
+    p.split = (int)(ceil_div(ceil_div(std::max<int64_t>(max_kv, 1), want), 256) * 256);
+    p.splits = (int)std::max<int64_t>(1, ceil_div(max_kv, p.split));
+    const uint64_t lines = (uint64_t)a->rows * a->n_heads;
+    p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
+    p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
+    p.lse_bytes = scored && !a->lse ? up256(lines * 4) : 0;
+    return p;
+}
+int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
+    if (int rc = check_cache(c, "attention")) return rc;
+    if (!a) return fail(RSD_EINVAL, "attention: null arguments");
+    if (!is_type(a->dtype)) return fail(RSD_EINVAL, "attention: type %d", a->dtype);
+    if (a->rows < 1 || a->max_rows < 1 || a->max_kv < 0) return fail(RSD_EINVAL, "attention: rows %d, at most %d a sequence, entries %d", a->rows, a->max_rows, a->max_kv);
+    if (a->n_heads < 1 || a->n_heads % c->n_kv_heads) return fail(RSD_EINVAL, "attention: %d heads over %d kv heads", a->n_heads, c->n_kv_heads);
+    if (!a->row_start && a->max_rows != 1) return fail(RSD_EINVAL, "attention: max_rows %d without row_start", a->max_rows);
+    if ((int64_t)a->max_rows * a->n_heads > INT32_MAX / 16 || (int64_t)c->batch * a->max_rows * a->n_heads > kMostBlocks * 4)
+        return fail(RSD_EINVAL, "attention: %d rows x %d heads x %d sequences", a->max_rows, a->n_heads, c->batch);
+    return RSD_OK;
+}
+
+template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
+    const dim3 grid((unsigned)(k.c.batch * k.c.hkv * p.tiles), (unsigned)p.splits);
+    if (p.mt == 1) kv4_attn_kernel<T, HD, PLANES, 1><<<grid, 256, 0, st>>>(k);
+    else kv4_attn_kernel<T, HD, PLANES, 2><<<grid, 256, 0, st>>>(k);
+    if (p.splits > 1)
+        kv4_join_kernel<T><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 4), 256, 0, st>>>(k, HD);
+    if (k.book.scores) {
+        const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
+        if (n > 0) kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)(k.c.batch * k.c.hkv), (unsigned)ceil_div(n, 4 * KV4_CHUNK)), 256, 0, st>>>(k);
+    }
+}
+template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, hipStream_t st) {
+    if (hd == 32) attn_run<T, 32, PLANES>(k, p, st);
+    else if (hd == 64) attn_run<T, 64, PLANES>(k, p, st);
+    else attn_run<T, 128, PLANES>(k, p, st);
+}
+int evict_moves(const rsd_kv4_cache* c, int budget) {
+    return (int)std::max<int64_t>(0, std::min<int64_t>(budget, (int64_t)c->max_pages * KV4_PAGE - budget));
+}
+
+}  // namespace
+
+extern "C" const char* rsd_op_last_error(void) { return op_error; }
+
+extern "C" int rsd_w4_pack(const void* w, int32_t dtype, int64_t ld, int32_t n, int32_t k, void* codes, void* scales, void* hip_stream) {
+    if (!w || !codes || !scales) return fail(RSD_EINVAL, "w4_pack: null array");
+    if (!is_type(dtype)) return fail(RSD_EINVAL, "w4_pack: type %d", dtype);
+    if (n < 1 || k < 1 || ld < k) return fail(RSD_EINVAL, "w4_pack: [%d][%d], rows %lld apart", n, k, (long long)ld);
+    const int nt = (int)ceil_div(n, 16), kt = (int)ceil_div(k, 128), ks = (int)ceil_div(k, 512);
+    const int64_t blocks = (int64_t)nt * ks * 16;        // 16 rows x 16 groups x 16 lanes of every 512 columns
+    if (blocks > kMostBlocks) return fail(RSD_EINVAL, "w4_pack: [%d][%d] is too large", n, k);
+    Launches l;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (dtype == RSD_F32)
+        w4_pack_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(static_cast<const float*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+    else
+        w4_pack_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(static_cast<const bf16_t*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+    return l.done("w4_pack");
+}
+
+extern "C" uint64_t rsd_w4_linear_workspace(int32_t rows, int32_t n, int32_t k, int32_t dtype) {
+    if (rows < 1 || n < 1 || k < 1 || !is_type(dtype)) return 0;
+    const W4Plan p = w4_plan(rows, n, k, dtype);
+    return p.xs_bytes + p.part_bytes;
+}
+
+extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* y, int64_t ldy, int32_t rows, int32_t dtype,
+                             void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    if (!w || !w->codes || !w->scales || !x || !y) return fail(RSD_EINVAL, "w4_linear: null array");
+    if (!is_type(dtype)) return fail(RSD_EINVAL, "w4_linear: type %d", dtype);
+    if (rows < 1 || w->n < 1 || w->k < 1 || ldx < w->k || ldy < w->n)
+        return fail(RSD_EINVAL, "w4_linear: %d rows, [%d][%d], rows of x %lld apart, of y %lld", rows, w->n, w->k, (long long)ldx, (long long)ldy);
+    if (!aligned(w->codes, 16) || !aligned(w->scales, 16)) return fail(RSD_EINVAL, "w4_linear: the weights are not 16-byte aligned");
+    if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(dtype))) return fail(RSD_EINVAL, "w4_linear: x or y is not aligned to its type");
+    if (ceil_div(rows, 16) * ceil_div(w->k, 128) > kMostBlocks || (int64_t)rows * w->n > kMostBlocks * 256 || rows > 1 << 20 || w->n > 1 << 26)
+        return fail(RSD_EINVAL, "w4_linear: %d rows with [%d][%d] are too many", rows, w->n, w->k);
+    const W4Plan p = w4_plan(rows, w->n, w->k, dtype);
+    if (workspace_bytes < p.xs_bytes + p.part_bytes || (p.xs_bytes + p.part_bytes && (!workspace || !aligned(workspace, 256))))
+        return fail(RSD_EINVAL, "w4_linear: the workspace holds %llu of %llu bytes, or is not 256-byte aligned",
+                    (unsigned long long)workspace_bytes, (unsigned long long)(p.xs_bytes + p.part_bytes));
+    char* ws = static_cast<char*>(workspace);
+    const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks,
+                   reinterpret_cast<const u32x4_t*>(ws), rows, y, ldy, p.splits > 1 ? reinterpret_cast<float*>(ws + p.xs_bytes) : nullptr, p.units};
+    Launches l;
+    if (dtype == RSD_F32) w4_run<float, 3>(p, a, x, ldx, static_cast<hipStream_t>(hip_stream));
+    else w4_run<bf16_t, 1>(p, a, x, ldx, static_cast<hipStream_t>(hip_stream));
+    return l.done("w4_linear");
+}
+
+extern "C" int rsd_kv4_append(const rsd_kv4_cache* c, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                              int32_t dtype, const int32_t* seq, const int32_t* slot, const int32_t* position, int32_t rows,
+                              const rsd_kv4_book* book, void* hip_stream) {
+    if (int rc = check_cache(c, "append")) return rc;
+    if (!k || !v || !seq || !slot) return fail(RSD_EINVAL, "append: null array");
+    if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "append: type %d, %d rows", dtype, rows);
+    if (book && book->positions && !position) return fail(RSD_EINVAL, "append: positions are kept but none are given");
+    if (!aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: k or v is not aligned to its type");
+    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 16);
+    if (blocks > kMostBlocks) return fail(RSD_EINVAL, "append: %d rows are too many", rows);
+    Launches l;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (dtype == RSD_F32)
+        kv4_append_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const float*>(k), k_row, k_head,
+                                                                   static_cast<const float*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
+    else
+        kv4_append_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const bf16_t*>(k), k_row, k_head,
+                                                                    static_cast<const bf16_t*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
+    return l.done("append");
+}
+
+extern "C" int rsd_kv4_read(const rsd_kv4_cache* c, const int32_t* seq, const int32_t* slot, int32_t rows, void* k, void* v, int32_t dtype,
+                            void* hip_stream) {
+    if (int rc = check_cache(c, "read")) return rc;
+    if (!k || !v || !seq || !slot) return fail(RSD_EINVAL, "read: null array");
+    if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "read: type %d, %d rows", dtype, rows);
+    if (!aligned(k, 16) || !aligned(v, 16)) return fail(RSD_EINVAL, "read: k or v is not 16-byte aligned");
+    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 16);
+    if (blocks > kMostBlocks) return fail(RSD_EINVAL, "read: %d rows are too many", rows);
+    Launches l;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (dtype == RSD_F32) kv4_read_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, seq, slot, rows, static_cast<float*>(k), static_cast<float*>(v));
+    else kv4_read_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, seq, slot, rows, static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
+    return l.done("read");
+}
+
+extern "C" uint64_t rsd_kv4_attention_workspace(const rsd_kv4_cache* c, const rsd_kv4_attn* a, int32_t scored) {
+    if (check_attn(c, a)) return 0;
+    const AttnPlan p = attn_plan(c, a, scored != 0);
+    return p.o_bytes + p.ml_bytes + p.lse_bytes;
+}
+
+extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, const rsd_kv4_book* book, void* workspace,
+                                 uint64_t workspace_bytes, void* hip_stream) {
+    if (int rc = check_attn(c, a)) return rc;
+    if (!a->q || !a->out) return fail(RSD_EINVAL, "attention: null array");
+    if (!aligned(a->q, size_of(a->dtype)) || !aligned(a->out, size_of(a->dtype))) return fail(RSD_EINVAL, "attention: q or out is not aligned to its type");
+    const bool scored = book && book->scores;
+    const AttnPlan p = attn_plan(c, a, scored);
+    const uint64_t need = p.o_bytes + p.ml_bytes + p.lse_bytes;
+    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
+        return fail(RSD_EINVAL, "attention: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
+    char* ws = static_cast<char*>(workspace);
+    Kv4Attn k{};
+    k.c = dev_cache(c);
+    k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
+    k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads, k.group = a->n_heads / c->n_kv_heads;
+    k.factor2 = (float)((double)a->scale * 1.4426950408889634);
+    k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
+    k.lse = a->lse ? a->lse : scored ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
+    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.tiles = p.tiles;
+    k.part_o = reinterpret_cast<float*>(ws);
+    k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
+    if (scored) k.book = dev_book(book);
+    Launches l;
+    if (a->dtype == RSD_F32) attn_run<float, 3>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
+    else attn_run<bf16_t, 1>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
+    return l.done("attention");
+}
+
+extern "C" uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache* c, int32_t budget) {
+    if (check_cache(c, "evict") || budget < 1) return 0;
+    return up256((uint64_t)c->batch * c->n_kv_heads * (2 + 2 * (uint64_t)evict_moves(c, budget)) * 4);
+}
+
+extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, int32_t budget, int32_t recent, void* workspace,
+                             uint64_t workspace_bytes, void* hip_stream) {
+    if (int rc = check_cache(c, "evict")) return rc;
+    if (!book || !book->scores || !book->positions) return fail(RSD_EINVAL, "evict: scores and positions are needed");
+    if (budget < 1 || recent < 0 || recent > budget) return fail(RSD_EINVAL, "evict: budget %d, recent %d", budget, recent);
+    const uint64_t need = rsd_kv4_evict_workspace(c, budget);
+    if (workspace_bytes < need || !workspace || !aligned(workspace, 256))
+        return fail(RSD_EINVAL, "evict: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
+    const Kv4Evict e{dev_cache(c), dev_book(book), budget, recent, static_cast<int*>(workspace), evict_moves(c, budget)};
+    if (e.moves == 0) return RSD_OK;                     // no sequence can hold more than the budget
+    Launches l;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const unsigned lists = (unsigned)(c->batch * c->n_kv_heads);
+    kv4_select_kernel<<<lists, 1024, 0, st>>>(e, c->n_kv_heads);
+    kv4_move_kernel<<<dim3(lists, (unsigned)std::min<int64_t>(16, ceil_div(e.moves, 4))), 256, 0, st>>>(e, c->head_dim, c->n_kv_heads);
+    return l.done("evict");
+}
