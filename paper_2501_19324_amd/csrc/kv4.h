@@ -37,59 +37,113 @@ struct Kv4Book {            // per entry: accumulated attention weight, position
     int64_t score_b, score_h, pos_b, pos_h;
 };
 
-// ---- entries in: 16 lanes take one group of 32 dims of one (row, head), keys and values
-template <typename T>
-__global__ void kv4_append_kernel(Kv4Cache c, int hd, const T* __restrict__ k, int64_t k_row, int64_t k_head, const T* __restrict__ v,
-                                  int64_t v_row, int64_t v_head, const int* __restrict__ seq, const int* __restrict__ slot,
-                                  const int* __restrict__ position, int rows, Kv4Book book) {
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int l = threadIdx.x & 15, groups = hd / 32;
-    const int g = (int)(item % groups), h = (int)(item / groups % c.hkv);
-    const int64_t row = item / groups / c.hkv;
-    if (row >= rows) return;
+// four consecutive values as they lie in memory; ALIGNED: the address is a multiple of their size together
+template <bool ALIGNED> __device__ __forceinline__ void kv4_load4(const float* p, float o[4]) {
+    if constexpr (ALIGNED) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = p[i];
+    }
+}
+template <bool ALIGNED> __device__ __forceinline__ void kv4_load4(const bf16_t* p, float o[4]) {
+    if constexpr (ALIGNED) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = ld1(p + i);
+    }
+}
+// scale byte and codes of a group of 32 held by four neighbouring lanes, eight values each: x[i], x[i + 4] share byte i where PAIRED,
+// x[2 i], x[2 i + 1] otherwise
+template <bool PAIRED> __device__ __forceinline__ uint32_t kv4_encode8(const float x[8], int& scale_byte) {
+    float amax = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i])), bad |= !q4_finite(x[i]);
+    amax = fmaxf(amax, __uint_as_float(dpp_move<0xB1>(__float_as_uint(amax))));
+    amax = fmaxf(amax, __uint_as_float(dpp_move<0x4E>(__float_as_uint(amax))));
+    uint32_t any = bad;
+    any |= dpp_move<0xB1>(any);
+    any |= dpp_move<0x4E>(any);
+    scale_byte = any ? Q4_NAN : q4_scale_byte(amax);
+    const float scale = __uint_as_float((uint32_t)scale_byte << 23);
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes |= (PAIRED ? q4_encode2(x[i], x[i + 4], scale) : q4_encode2(x[2 * i], x[2 * i + 1], scale)) << (8 * i);
+    return any ? 0u : codes;
+}
+
+// ---- entries in: four lanes take one group of 32 dims of one (row, head), keys and values.  What a lane has to wait for in turn (row numbers,
+// then the table, then the stores) is a chain of latencies: keys and values are requested before it, eight of each to a lane.
+// 7936 rows of 8 heads in fp32 (75 MB): 37 us with two values to a lane, requested behind the chain.
+template <typename T, bool ALIGNED>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int hd, const T* __restrict__ k, int64_t k_row, int64_t k_head, const T* __restrict__ v,
+                                                         int64_t v_row, int64_t v_head, const int* __restrict__ seq, const int* __restrict__ slot,
+                                                         const int* __restrict__ position, int rows, Kv4Book book) {
+    const int l = threadIdx.x & 3, groups = hd / 32;
+    const uint32_t item = (blockIdx.x * 256 + threadIdx.x) >> 2, line = item / groups;
+    const int g = (int)(item % groups), h = (int)(line % c.hkv), row = (int)(line / c.hkv);
+    if (row >= rows) return;                              // four lanes leave together
     const int b = seq[row], s = slot[row];
+    const T* kr = k + row * k_row + h * k_head + g * 32 + 8 * l;
+    const T* vr = v + row * v_row + h * v_head + g * 32 + 4 * l;
+    float kx[8], vx[8];
+    kv4_load4<ALIGNED>(kr, kx);
+    kv4_load4<ALIGNED>(kr + 4, kx + 4);
+    kv4_load4<ALIGNED>(vr, vx);
+    kv4_load4<ALIGNED>(vr + 16, vx + 4);
     if ((unsigned)b >= (unsigned)c.batch || (unsigned)s >= (unsigned)c.max_pages * KV4_PAGE) return;
     uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
     if (!block) return;
     const int t = s % KV4_PAGE;
-    const T* kr = k + row * k_row + h * k_head + g * 32;
-    const T* vr = v + row * v_row + h * v_head + g * 32;
-    const float k0 = ld1(kr + 2 * l), k1 = ld1(kr + 2 * l + 1), v0 = ld1(vr + l), v1 = ld1(vr + 16 + l);
-    const bool kbad = row16_or(!q4_finite(k0) || !q4_finite(k1)) != 0, vbad = row16_or(!q4_finite(v0) || !q4_finite(v1)) != 0;
-    const int ke = q4_scale_byte(row16_max(fmaxf(fabsf(k0), fabsf(k1)))), ve = q4_scale_byte(row16_max(fmaxf(fabsf(v0), fabsf(v1))));
-    block[kv4_key_at(hd, t, g * 32 + 2 * l)] = kbad ? 0 : (uint8_t)q4_encode2(k0, k1, __uint_as_float((uint32_t)ke << 23));
-    block[kv4_val_at(hd, t, g, l)] = vbad ? 0 : (uint8_t)q4_encode2(v0, v1, __uint_as_float((uint32_t)ve << 23));
+    int ke, ve;
+    const uint32_t kc = kv4_encode8<false>(kx, ke), vc = kv4_encode8<true>(vx, ve);
+    *reinterpret_cast<uint32_t*>(block + kv4_key_at(hd, t, g * 32 + 8 * l)) = kc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) block[kv4_val_at(hd, t, g, 4 * l + i)] = (uint8_t)(vc >> (8 * i));
     if (l == 0) {
-        block[kv4_key_scale_at(hd, t, g)] = kbad ? Q4_NAN : (uint8_t)ke;
-        block[kv4_val_scale_at(hd, t, g)] = vbad ? Q4_NAN : (uint8_t)ve;
+        block[kv4_key_scale_at(hd, t, g)] = (uint8_t)ke;
+        block[kv4_val_scale_at(hd, t, g)] = (uint8_t)ve;
         if (g == 0 && book.scores) book.scores[b * book.score_b + h * book.score_h + s] = 0.f;
         if (g == 0 && book.pos) book.pos[b * book.pos_b + h * book.pos_h + s] = position[row];
     }
 }
 
-// ---- entries out: [rows][heads][hd], contiguous; a row that names no entry of the cache gives zeros
+// ---- entries out: [rows][heads][hd], contiguous; a row that names no entry of the cache gives zeros.  The lanes as above.
+template <typename T> __device__ __forceinline__ void kv4_store4(T* p, const uint32_t a, const uint32_t b) {      // two pairs of bf16
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
+    else *reinterpret_cast<float4*>(p) = make_float4(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+}
 template <typename T>
-__global__ void kv4_read_kernel(Kv4Cache c, int hd, const int* __restrict__ seq, const int* __restrict__ slot, int rows, T* __restrict__ k,
-                                T* __restrict__ v) {
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int l = threadIdx.x & 15, groups = hd / 32;
-    const int g = (int)(item % groups), h = (int)(item / groups % c.hkv);
-    const int64_t row = item / groups / c.hkv;
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache c, int hd, const int* __restrict__ seq, const int* __restrict__ slot, int rows,
+                                                       T* __restrict__ k, T* __restrict__ v) {
+    const int l = threadIdx.x & 3, groups = hd / 32;
+    const uint32_t item = (blockIdx.x * 256 + threadIdx.x) >> 2, line = item / groups;
+    const int g = (int)(item % groups), h = (int)(line % c.hkv), row = (int)(line / c.hkv);
     if (row >= rows) return;
     const int b = seq[row], s = slot[row], t = s % KV4_PAGE;
-    uint32_t kk = 0, vv = 0;
+    u32x4_t kk = {}, vv = {};
     if ((unsigned)b < (unsigned)c.batch && (unsigned)s < (unsigned)c.max_pages * KV4_PAGE) {
         const uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
         if (block) {
-            kk = q4_decode2<0>(block[kv4_key_at(hd, t, g * 32 + 2 * l)], (uint32_t)block[kv4_key_scale_at(hd, t, g)] << 23);
-            vv = q4_decode2<0>(block[kv4_val_at(hd, t, g, l)], (uint32_t)block[kv4_val_scale_at(hd, t, g)] << 23);
+            const uint32_t kc = *reinterpret_cast<const uint32_t*>(block + kv4_key_at(hd, t, g * 32 + 8 * l));
+            uint32_t vc = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vc |= (uint32_t)block[kv4_val_at(hd, t, g, 4 * l + i)] << (8 * i);
+            kk = q4_decode8(kc, (uint32_t)block[kv4_key_scale_at(hd, t, g)] << 23);
+            vv = q4_decode8(vc, (uint32_t)block[kv4_val_scale_at(hd, t, g)] << 23);
         }
     }
-    const int64_t o = (row * c.hkv + h) * hd + g * 32;
-    st1(k + o + 2 * l, __uint_as_float(kk << 16));
-    st1(k + o + 2 * l + 1, __uint_as_float(kk & 0xFFFF0000u));
-    st1(v + o + l, __uint_as_float(vv << 16));
-    st1(v + o + 16 + l, __uint_as_float(vv & 0xFFFF0000u));
+    const int64_t o = (int64_t)line * hd + g * 32;
+    kv4_store4(k + o + 8 * l, kk[0], kk[1]);
+    kv4_store4(k + o + 8 * l + 4, kk[2], kk[3]);
+    // pairs (m, m + 16): the low halves are dims 4 l .. + 3, the high ones those 16 further on
+    kv4_store4(v + o + 4 * l, __builtin_amdgcn_perm(vv[1], vv[0], 0x05040100u), __builtin_amdgcn_perm(vv[3], vv[2], 0x05040100u));
+    kv4_store4(v + o + 16 + 4 * l, __builtin_amdgcn_perm(vv[1], vv[0], 0x07060302u), __builtin_amdgcn_perm(vv[3], vv[2], 0x07060302u));
 }
 
 // ---- attention
@@ -469,11 +523,34 @@ __device__ __forceinline__ uint32_t kv4_rank_key(float score, bool safe) {
     const uint32_t u = __float_as_uint(score != score ? -INFINITY : score + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-// One block per (sequence, kv head): the key of the budget-th entry by four passes over eight bits each, then one pass in slot order that lists
-// the freed slots below the budget and the kept entries above it.
+// Exclusive sums over the 1024 threads of a block of two counts, and the totals; `part` is 2 x 16 words of LDS, free again after the next barrier.
+__device__ __forceinline__ void kv4_block_scan(int& a, int& b, int& all_a, int& all_b, int (*part)[16]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = a, y = b;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int p = __shfl_up(x, d), q = __shfl_up(y, d);
+        if (lane >= d) x += p, y += q;
+    }
+    if (lane == 63) part[0][wave] = x, part[1][wave] = y;
+    __syncthreads();
+    a = x - a, b = y - b, all_a = all_b = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        const int p = part[0][w], q = part[1][w];
+        if (w < wave) a += p, b += q;
+        all_a += p, all_b += q;
+    }
+}
+
+// One block per (sequence, kv head).  The key of the budget-th entry comes from a radix selection, eight bits a pass from the top, that ends
+// as soon as a bin is kept whole (two or three passes for scores that differ).  Then every thread takes a run of consecutive slots: one sum over the block
+// ranks the ties, a second one the freed slots below the budget and the kept entries above it, which are the moves.
+// CACHED: the keys stay in LDS (up to 16384 slots); longer lists are read again by every pass.
+template <bool CACHED>
 __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
-    __shared__ int hist[256], wsum[3][16], found[2];
-    __shared__ int newest_w[16];
+    extern __shared__ uint32_t kv4_keys[];
+    __shared__ int hist[256], part[2][2][16], found[3], newest_w[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
     int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
@@ -482,15 +559,27 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     if (n <= a.budget) return;
     const float* score = a.book.scores + b * a.book.score_b + h * a.book.score_h;
     const int* pos = a.book.pos + b * a.book.pos_b + h * a.book.pos_h;
-    int newest = INT32_MIN;
-    for (int s = tid; s < n; s += 1024) newest = max(newest, pos[s]);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) newest = max(newest, __shfl_xor(newest, d));
-    if (lane == 0) newest_w[wave] = newest;
-    __syncthreads();
-    for (int w = 0; w < 16; ++w) newest = max(newest, newest_w[w]);
     // protected: position > newest - recent, in 64 bits (positions may be any int32)
-    const int64_t bound = (int64_t)newest - a.recent;
+    int64_t bound = INT64_MAX;
+    if (a.recent > 0) {
+        int newest = INT32_MIN;
+        for (int s = tid; s < n; s += 1024) {
+            const int x = pos[s];
+            if constexpr (CACHED) kv4_keys[s] = (uint32_t)x;
+            newest = max(newest, x);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) newest = max(newest, __shfl_xor(newest, d));
+        if (lane == 0) newest_w[wave] = newest;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 16; ++w) newest = max(newest, newest_w[w]);
+        bound = (int64_t)newest - a.recent;
+    }
+    if constexpr (CACHED) {
+        for (int s = tid; s < n; s += 1024) kv4_keys[s] = kv4_rank_key(score[s], a.recent > 0 && (int)kv4_keys[s] > bound);
+    }
+    auto key_of = [&](int s) { return CACHED ? kv4_keys[s] : kv4_rank_key(score[s], a.recent > 0 && pos[s] > bound); };
     uint32_t key = 0;
     int need = a.budget;                                    // entries still to be kept among those that agree with `key` so far
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -498,7 +587,7 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
         __syncthreads();
         const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
         for (int s = tid; s < n; s += 1024) {
-            const uint32_t u = kv4_rank_key(score[s], pos[s] > bound);
+            const uint32_t u = key_of(s);
             if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255], 1);
         }
         __syncthreads();
@@ -512,69 +601,83 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
             before -= mine;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (before < need && before + c[i] >= need) found[0] = 255 - 4 * lane - i, found[1] = need - before;
+                if (before < need && before + c[i] >= need) found[0] = 255 - 4 * lane - i, found[1] = need - before, found[2] = c[i];
                 before += c[i];
             }
         }
         __syncthreads();
         key |= (uint32_t)found[0] << shift;
         need = found[1];
-        __syncthreads();
+        if (need == found[2]) {                             // the bin is kept whole: every key from `key` on
+            key -= 1, need = 0;                             // (key > 0: not every entry is kept)
+            break;
+        }
     }
     // keep: keys above, and the first `need` of those equal to it
-    int ties = 0, holes = 0, extras = 0;
-    for (int s0 = 0; s0 < n; s0 += 1024) {
-        const int s = s0 + tid;
-        const uint32_t u = s < n ? kv4_rank_key(score[s], pos[s] > bound) : 0u;
-        const bool tie = s < n && u == key;
-        const uint64_t tm = __ballot(tie);
-        if (lane == 0) wsum[0][wave] = __popcll(tm);
-        __syncthreads();
-        int rank = ties + __popcll(tm & ((1ull << lane) - 1));
-        int all = 0;
-        for (int w = 0; w < 16; ++w) { if (w < wave) rank += wsum[0][w]; all += wsum[0][w]; }
-        ties += all;
-        const bool keep = s < n && (u > key || (tie && rank < need));
-        const bool hole = s < a.budget && !keep, extra = s >= a.budget && keep;
-        const uint64_t hm = __ballot(hole), em = __ballot(extra);
-        if (lane == 0) wsum[1][wave] = __popcll(hm), wsum[2][wave] = __popcll(em);
-        __syncthreads();
-        int hr = holes + __popcll(hm & ((1ull << lane) - 1)), er = extras + __popcll(em & ((1ull << lane) - 1)), ha = 0, ea = 0;
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) hr += wsum[1][w], er += wsum[2][w];
-            ha += wsum[1][w], ea += wsum[2][w];
-        }
-        if (hole) plan[2 + hr] = s;
-        if (extra) plan[2 + a.moves + er] = s;
-        holes += ha;
-        extras += ea;
-        __syncthreads();
+    const int run = (n + 1023) / 1024, s0 = min(tid * run, n), s1 = min(s0 + run, n);
+    int ties = 0, none = 0, all_a, all_b;
+    if (need > 0) {
+        for (int s = s0; s < s1; ++s) ties += key_of(s) == key;
+        kv4_block_scan(ties, none, all_a, all_b, part[0]);
     }
-    if (tid == 0) plan[0] = holes;
+    int holes = 0, extras = 0, rank = ties;
+    for (int s = s0; s < s1; ++s) {
+        const uint32_t u = key_of(s);
+        const bool keep = u > key || (u == key && rank++ < need);
+        holes += s < a.budget && !keep;
+        extras += s >= a.budget && keep;
+    }
+    kv4_block_scan(holes, extras, all_a, all_b, part[1]);
+    rank = ties;
+    for (int s = s0; s < s1; ++s) {
+        const uint32_t u = key_of(s);
+        const bool keep = u > key || (u == key && rank++ < need);
+        if (s < a.budget && !keep) plan[2 + holes++] = s;
+        if (s >= a.budget && keep) plan[2 + a.moves + extras++] = s;
+    }
+    if (tid == 0) plan[0] = all_a;
 }
-// one wave per moved entry
-__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int hd, int hkv) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+
+// The moves: 16 lanes take one entry, eight words of hd at a time, so that a wave has four entries' chains of latencies (plan, table, bytes) under way.
+// 64 sequences x 4 heads, 225000 moves: 96 us with a wave per entry and a byte per lane.
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int hkv) {
+    constexpr int G = HD / 32;
+    typedef typename u32vec<G>::type V;
+    const int l = threadIdx.x & 15;
     const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
     const int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
     const int count = plan[0];
     if (blockIdx.y == 0 && h == 0 && threadIdx.x == 0) a.c.kv_len[b] = min(plan[1], a.budget);
     float* score = a.book.scores + b * a.book.score_b + h * a.book.score_h;
     int* pos = a.book.pos + b * a.book.pos_b + h * a.book.pos_h;
-    for (int i = blockIdx.y * 4 + wave; i < count; i += gridDim.y * 4) {
+    for (int i = blockIdx.y * 16 + (threadIdx.x >> 4); i < count; i += gridDim.y * 16) {
         const int to = plan[2 + i], from = plan[2 + a.moves + i], t1 = to % KV4_PAGE, t0 = from % KV4_PAGE;
-        uint8_t* dst = kv4_page(a.c, hd, b, to / KV4_PAGE, h);
-        const uint8_t* src = kv4_page(a.c, hd, b, from / KV4_PAGE, h);
+        uint8_t* dst = kv4_page(a.c, HD, b, to / KV4_PAGE, h);
+        const uint8_t* src = kv4_page(a.c, HD, b, from / KV4_PAGE, h);
         if (dst && src) {
-            if (lane < hd / 2) {
-                dst[kv4_key_at(hd, t1, 2 * lane)] = src[kv4_key_at(hd, t0, 2 * lane)];
-                dst[kv4_val_at(hd, t1, lane >> 4, lane & 15)] = src[kv4_val_at(hd, t0, lane >> 4, lane & 15)];
-            }
-            if (lane < hd / 32) {
-                dst[kv4_key_scale_at(hd, t1, lane)] = src[kv4_key_scale_at(hd, t0, lane)];
-                dst[kv4_val_scale_at(hd, t1, lane)] = src[kv4_val_scale_at(hd, t0, lane)];
-            }
+            // keys: HD/32 bytes at a time, of quarter l / 4
+            const int key = l / 4 * 2 * HD + l % 4 * G;
+            uint32_t k = 0;
+            if constexpr (G == 4) k = *reinterpret_cast<const uint32_t*>(src + key + t0 * (HD / 8));
+            else if constexpr (G == 2) k = *reinterpret_cast<const uint16_t*>(src + key + t0 * (HD / 8));
+            else k = src[key + t0 * (HD / 8)];
+            // values: lane l has the bytes of dim l of every group, among those of the four tokens of a quad
+            const V v = *reinterpret_cast<const V*>(src + 8 * HD + (t0 >> 2) * 2 * HD + l * (HD / 8));
+            uint32_t ks = 0, vs = 0, sc = 0;
+            int po = 0;
+            if (l < G) ks = src[kv4_key_scale_at(HD, t0, l)], vs = src[kv4_val_scale_at(HD, t0, l)];
+            if (l == 15) sc = __float_as_uint(score[from]), po = pos[from];
+            if constexpr (G == 4) *reinterpret_cast<uint32_t*>(dst + key + t1 * (HD / 8)) = k;
+            else if constexpr (G == 2) *reinterpret_cast<uint16_t*>(dst + key + t1 * (HD / 8)) = (uint16_t)k;
+            else dst[key + t1 * (HD / 8)] = (uint8_t)k;
+            uint8_t* d = dst + 8 * HD + (t1 >> 2) * 2 * HD + l * (HD / 8) + (t1 & 3);
+#pragma unroll
+            for (int g = 0; g < G; ++g) d[4 * g] = (uint8_t)(v[g] >> (8 * (t0 & 3)));
+            if (l < G) dst[kv4_key_scale_at(HD, t1, l)] = (uint8_t)ks, dst[kv4_val_scale_at(HD, t1, l)] = (uint8_t)vs;
+            if (l == 15) score[to] = __uint_as_float(sc), pos[to] = po;
+        } else if (l == 15) {
+            score[to] = score[from], pos[to] = pos[from];
         }
-        if (lane == 0) score[to] = score[from], pos[to] = pos[from];
     }
 }

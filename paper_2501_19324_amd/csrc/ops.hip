@@ -90,6 +90,16 @@ Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
 }
 
+// Four values at once where every row and head starts on a multiple of four values' size
+template <typename T>
+void append_run(const rsd_kv4_cache* c, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const int32_t* seq,
+                const int32_t* slot, const int32_t* position, int32_t rows, const rsd_kv4_book* book, unsigned blocks, hipStream_t st) {
+    const bool wide = aligned(k, 4 * sizeof(T)) && aligned(v, 4 * sizeof(T)) && !((k_row | k_head | v_row | v_head) & 3);
+    const T *kt = static_cast<const T*>(k), *vt = static_cast<const T*>(v);
+    if (wide) kv4_append_kernel<T, true><<<blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, kt, k_row, k_head, vt, v_row, v_head, seq, slot, position, rows, dev_book(book));
+    else kv4_append_kernel<T, false><<<blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, kt, k_row, k_head, vt, v_row, v_head, seq, slot, position, rows, dev_book(book));
+}
+
 struct AttnPlan { int mt, tiles, split, splits; uint64_t o_bytes, ml_bytes, lse_bytes; };
 
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
@@ -197,16 +207,12 @@ extern "C" int rsd_kv4_append(const rsd_kv4_cache* c, const void* k, int64_t k_r
     if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "append: type %d, %d rows", dtype, rows);
     if (book && book->positions && !position) return fail(RSD_EINVAL, "append: positions are kept but none are given");
     if (!aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: k or v is not aligned to its type");
-    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 16);
+    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "append: %d rows are too many", rows);
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (dtype == RSD_F32)
-        kv4_append_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const float*>(k), k_row, k_head,
-                                                                   static_cast<const float*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
-    else
-        kv4_append_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const bf16_t*>(k), k_row, k_head,
-                                                                    static_cast<const bf16_t*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
+    if (dtype == RSD_F32) append_run<float>(c, k, k_row, k_head, v, v_row, v_head, seq, slot, position, rows, book, (unsigned)blocks, st);
+    else append_run<bf16_t>(c, k, k_row, k_head, v, v_row, v_head, seq, slot, position, rows, book, (unsigned)blocks, st);
     return l.done("append");
 }
 
@@ -216,7 +222,7 @@ extern "C" int rsd_kv4_read(const rsd_kv4_cache* c, const int32_t* seq, const in
     if (!k || !v || !seq || !slot) return fail(RSD_EINVAL, "read: null array");
     if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "read: type %d, %d rows", dtype, rows);
     if (!aligned(k, 16) || !aligned(v, 16)) return fail(RSD_EINVAL, "read: k or v is not 16-byte aligned");
-    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 16);
+    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "read: %d rows are too many", rows);
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -277,7 +283,13 @@ extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, i
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const unsigned lists = (unsigned)(c->batch * c->n_kv_heads);
-    kv4_select_kernel<<<lists, 1024, 0, st>>>(e, c->n_kv_heads);
-    kv4_move_kernel<<<dim3(lists, (unsigned)std::min<int64_t>(16, ceil_div(e.moves, 4))), 256, 0, st>>>(e, c->head_dim, c->n_kv_heads);
+    const int64_t slots = (int64_t)c->max_pages * KV4_PAGE;
+    if (slots <= 16384) kv4_select_kernel<true><<<lists, 1024, (size_t)slots * 4, st>>>(e, c->n_kv_heads);
+    else kv4_select_kernel<false><<<lists, 1024, 0, st>>>(e, c->n_kv_heads);
+    // 16 moves to a block at a time; at most 64 blocks to a list, which then go on with the next 1024
+    const dim3 grid(lists, (unsigned)std::min<int64_t>(64, ceil_div(e.moves, 16)));
+    if (c->head_dim == 32) kv4_move_kernel<32><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
+    else if (c->head_dim == 64) kv4_move_kernel<64><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
+    else kv4_move_kernel<128><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
     return l.done("evict");
 }
