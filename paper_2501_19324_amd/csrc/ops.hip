@@ -38,38 +38,56 @@ constexpr int64_t kMostBlocks = 1ll << 22;      // blocks of at most 512 threads
 
 // ---- products with 4-bit weights
 
-struct W4Plan { int nt, kt, ks, rt, planes, tiles, row_tiles, splits, units, waves; uint64_t xs_bytes, part_bytes; };
+struct W4Plan { int nt, kt, ks; bool few; int waves, xt, splits, tiles; uint64_t part_bytes; };
 
+// Which kernel, and how the columns are split (by sizes and type alone; measured on both sides of each bound, times with launch):
+//  - few rows (<= 16): while its blocks together read at most 64 MB of x (16 rows bf16, 3584 x 3584: 8.2 us against 12.4; 8 rows, 8192 x 29568: 35.8 against 29.4),
+//    and for more than four rows of fp32, which its waves cut into three parts each for itself, up to 16 tiles of columns (1536 x 1536: 8.4 against 12.2, 3584 x 3584: 15.5 against 12.3).
+//  - many rows: blocks for every CU, two where a tile of x is small (64 rows, 3584 x 18944: 73 us in 2 splits, 40 in 4, 24 in 8, 19 in 16; 256 rows: 73, 44, 44, 55),
+//    no split of fewer than four tiles.  From six on splits come in eights: one part of x per XCD.
 W4Plan w4_plan(int rows, int n, int k, int dtype) {
-    W4Plan p;
+    W4Plan p{};
     p.nt = (int)ceil_div(n, 16);
     p.kt = (int)ceil_div(k, 128);
     p.ks = (int)ceil_div(k, 512);
-    p.rt = (int)ceil_div(rows, 16);
-    p.planes = dtype == RSD_F32 ? 3 : 1;
-    p.tiles = 2;
-    p.row_tiles = p.rt == 1 ? 1 : p.rt == 2 ? 2 : 4;
-    p.splits = 1;
-    p.units = p.ks;
-    p.waves = std::min(8, std::max(1, p.ks));
-    p.xs_bytes = up256((uint64_t)p.rt * p.kt * p.planes * 4096);
-    p.part_bytes = p.splits > 1 ? up256((uint64_t)p.splits * rows * n * 4) : 0;
+    const bool f32 = dtype == RSD_F32;
+    p.few = rows <= 16 && ceil_div(p.nt, 2) * rows * k * (int64_t)size_of(dtype) <= 64 << 20 && !(f32 && rows > 4 && p.kt > 16);
+    int64_t splits = 1;
+    if (!p.few) {
+        p.xt = rows <= 16 ? 1 : rows <= 32 || f32 ? 2 : 4;
+        const int64_t blocks = ceil_div(p.nt, 16) * ceil_div(rows, p.xt * 16);
+        splits = std::max<int64_t>(1, std::min<int64_t>((p.xt == 4 ? 256 : 512) / blocks, p.kt / 4));
+        if (splits > 5) splits = std::min<int64_t>((splits + 3) / 8 * 8, 16);
+    }
+    p.tiles = (int)ceil_div(p.kt, splits);
+    if (!p.few) p.tiles = (p.tiles + 3) & ~3;
+    p.splits = (int)ceil_div(p.kt, p.tiles);
+    // waves of a few-row block: some 4096 in all, at least four, as many as take equally many tiles
+    p.waves = (int)std::min<int64_t>(std::min(f32 && rows > 4 ? 8 : 16, p.kt), std::max<int64_t>(4, ceil_div(4096, ceil_div(p.nt, 2))));
+    p.waves = (int)ceil_div(p.kt, ceil_div(p.kt, p.waves));
+    p.part_bytes = p.splits > 1 ? up256((uint64_t)p.splits * rows * w4_padded(n) * 4) : 0;
     return p;
 }
 
-template <typename T, int NT, int R, int PLANES> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
-    const dim3 grid((unsigned)ceil_div(p.nt, NT), (unsigned)p.splits, (unsigned)ceil_div(p.rt, R));
-    w4_kernel<T, NT, R, PLANES><<<grid, 64 * p.waves, (size_t)p.waves * NT * R * 1024, st>>>(a);
+template <typename T, bool VEC> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
+    if (p.few) {
+        const dim3 grid((unsigned)ceil_div(p.nt, 2));
+        const unsigned threads = 64 * p.waves;
+        if (a.rows <= 4) w4_few_kernel<T, 2, 1, VEC><<<grid, threads, 0, st>>>(a);
+        else w4_few_kernel<T, 2, 4, VEC><<<grid, threads, 0, st>>>(a);
+        return;
+    }
+    const dim3 grid((unsigned)p.splits, (unsigned)ceil_div(p.nt, 16), (unsigned)ceil_div(a.rows, p.xt * 16));
+    if (p.xt == 1) w4_many_kernel<T, 1, VEC><<<grid, 256, 0, st>>>(a);
+    else if (p.xt == 2) w4_many_kernel<T, 2, VEC><<<grid, 256, 0, st>>>(a);
+    else if constexpr (sizeof(T) == 2) w4_many_kernel<T, 4, VEC><<<grid, 256, 0, st>>>(a);
 }
-template <typename T, int PLANES> void w4_run(const W4Plan& p, const W4Args& a, const void* x, int64_t ldx, hipStream_t st) {
-    const int64_t items = (int64_t)p.rt * p.kt * 256;
-    w4_stage_kernel<T, PLANES><<<(unsigned)(items / 256), 256, 0, st>>>(static_cast<const T*>(x), ldx, a.rows, a.k, a.kt,
-                                                                       reinterpret_cast<uint4*>(const_cast<u32x4_t*>(a.xs)));
-    if (p.row_tiles == 1) w4_launch<T, 2, 1, PLANES>(p, a, st);
-    else if (p.row_tiles == 2) w4_launch<T, 2, 2, PLANES>(p, a, st);
-    else w4_launch<T, 2, 4, PLANES>(p, a, st);
+template <typename T> void w4_run(const W4Plan& p, const W4Args& a, hipStream_t st) {
+    const bool vec = aligned(a.x, 16) && a.ldx % (16 / sizeof(T)) == 0 && a.k % 128 == 0;
+    if (vec) w4_launch<T, true>(p, a, st);
+    else w4_launch<T, false>(p, a, st);
     if (p.splits > 1)
-        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * a.n, 256), 256, 0, st>>>(a.part, p.splits, a.rows, a.n, static_cast<T*>(a.y), a.ldy);
+        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, st>>>(a, p.splits);
 }
 
 // ---- the cache
@@ -173,7 +191,7 @@ extern "C" int rsd_w4_pack(const void* w, int32_t dtype, int64_t ld, int32_t n, 
 extern "C" uint64_t rsd_w4_linear_workspace(int32_t rows, int32_t n, int32_t k, int32_t dtype) {
     if (rows < 1 || n < 1 || k < 1 || !is_type(dtype)) return 0;
     const W4Plan p = w4_plan(rows, n, k, dtype);
-    return p.xs_bytes + p.part_bytes;
+    return p.part_bytes;
 }
 
 extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* y, int64_t ldy, int32_t rows, int32_t dtype,
@@ -184,18 +202,18 @@ extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* 
         return fail(RSD_EINVAL, "w4_linear: %d rows, [%d][%d], rows of x %lld apart, of y %lld", rows, w->n, w->k, (long long)ldx, (long long)ldy);
     if (!aligned(w->codes, 16) || !aligned(w->scales, 16)) return fail(RSD_EINVAL, "w4_linear: the weights are not 16-byte aligned");
     if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(dtype))) return fail(RSD_EINVAL, "w4_linear: x or y is not aligned to its type");
-    if (ceil_div(rows, 16) * ceil_div(w->k, 128) > kMostBlocks || (int64_t)rows * w->n > kMostBlocks * 256 || rows > 1 << 20 || w->n > 1 << 26)
+    if ((int64_t)rows * w->n > kMostBlocks * 256 || rows > 1 << 20 || w->n > 1 << 26)
         return fail(RSD_EINVAL, "w4_linear: %d rows with [%d][%d] are too many", rows, w->n, w->k);
     const W4Plan p = w4_plan(rows, w->n, w->k, dtype);
-    if (workspace_bytes < p.xs_bytes + p.part_bytes || (p.xs_bytes + p.part_bytes && (!workspace || !aligned(workspace, 256))))
+    if (workspace_bytes < p.part_bytes || (p.part_bytes && (!workspace || !aligned(workspace, 256))))
         return fail(RSD_EINVAL, "w4_linear: the workspace holds %llu of %llu bytes, or is not 256-byte aligned",
-                    (unsigned long long)workspace_bytes, (unsigned long long)(p.xs_bytes + p.part_bytes));
-    char* ws = static_cast<char*>(workspace);
-    const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks,
-                   reinterpret_cast<const u32x4_t*>(ws), rows, y, ldy, p.splits > 1 ? reinterpret_cast<float*>(ws + p.xs_bytes) : nullptr, p.units};
+                    (unsigned long long)workspace_bytes, (unsigned long long)p.part_bytes);
+    const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks, x, ldx, rows, y, ldy,
+                   p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles,
+                   aligned(y, 4 * size_of(dtype)) && ldy % 4 == 0};
     Launches l;
-    if (dtype == RSD_F32) w4_run<float, 3>(p, a, x, ldx, static_cast<hipStream_t>(hip_stream));
-    else w4_run<bf16_t, 1>(p, a, x, ldx, static_cast<hipStream_t>(hip_stream));
+    if (dtype == RSD_F32) w4_run<float>(p, a, static_cast<hipStream_t>(hip_stream));
+    else w4_run<bf16_t>(p, a, static_cast<hipStream_t>(hip_stream));
     return l.done("w4_linear");
 }
 

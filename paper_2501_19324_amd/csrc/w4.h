@@ -7,105 +7,271 @@
 #pragma once
 #include "q4.h"
 
-// x as B operands: [row tile of 16][tile of 128 columns][plane][j][lane][8], zero beyond rows and K.  PLANES = 1: bf16; 3: fp32 exactly.
-template <typename T, int PLANES>
-__global__ void w4_stage_kernel(const T* __restrict__ x, int64_t ld, int rows, int k, int kt, uint4* __restrict__ xs) {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t total = (int64_t)((rows + 15) / 16) * kt * 256;
-    if (id >= total) return;
-    const int lane = (int)(id & 63), j = (int)(id >> 6) & 3;
-    const int64_t tile = id >> 8;
-    const int t = (int)(tile % kt), row = (int)(tile / kt) * 16 + (lane & 15), k0 = t * 128 + (lane >> 4) * 32 + j * 8;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = row < rows && k0 + i < k ? ld1(x + row * ld + k0 + i) : 0.f;
-    u32x4_t o[PLANES];
-    q4_operand<PLANES>(v, o);
-#pragma unroll
-    for (int p = 0; p < PLANES; ++p) xs[((tile * PLANES + p) * 4 + j) * 64 + lane] = __builtin_bit_cast(uint4, o[p]);
-}
-
 struct W4Args {
     const u32x4_t* codes;
     const uint32_t* scales;
     int n, k, nt, kt, ks;
-    const u32x4_t* xs;
+    const void* x;
+    int64_t ldx;
     int rows;
     void* y;
     int64_t ldy;
     float* part;        // partial sums [split][rows][n], null: the block writes y
-    int units;          // groups of four tiles (512 columns) per split
+    int tiles;          // tiles of 128 columns per split
+    bool y_wide;        // rows of y start on multiples of four values
 };
+template <typename T> constexpr int w4_planes = sizeof(T) == 4 ? 3 : 1;
 
-// A block owns NT tiles of rows of W and R tiles of rows of x; its waves share K in units of 512 columns.
-template <typename T, int NT, int R, int PLANES>
-__global__ __launch_bounds__(512) void w4_kernel(W4Args a) {
-    extern __shared__ float w4_lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * NT, rt0 = blockIdx.z * R, rts = (a.rows + 15) >> 4;
-    const int u0 = blockIdx.y * a.units, u1 = min(a.ks, u0 + a.units);
-    f32x4_t acc[NT][R] = {};
-    for (int u = u0 + wave; u < u1; u += waves) {
-        uint32_t sc[NT];
+// Eight values of x.  VEC: the row's 16-byte pieces are aligned and k is a multiple of 128; otherwise value by value, zero from column k on.
+template <typename T> struct W4Piece;
+template <> struct W4Piece<bf16_t> { u32x4_t v; };
+template <> struct W4Piece<float> { f32x4_t a, b; };
+template <bool VEC> __device__ __forceinline__ void w4_load(const bf16_t* row, int k0, int k, W4Piece<bf16_t>& o) {
+    if constexpr (VEC) {
+        o.v = *reinterpret_cast<const u32x4_t*>(row + k0);
+    } else {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) sc[i] = a.scales[((int64_t)min(n0 + i, a.nt - 1) * a.ks + u) * 64 + lane];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int t = u * 4 + c;
-            if (t >= a.kt) break;
-            u32x4_t w[NT];
-#pragma unroll
-            for (int i = 0; i < NT; ++i) w[i] = a.codes[((int64_t)min(n0 + i, a.nt - 1) * a.kt + t) * 64 + lane];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32x4_t b[R][PLANES];
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int p = 0; p < PLANES; ++p)
-                        b[r][p] = a.xs[((((int64_t)min(rt0 + r, rts - 1) * a.kt + t) * PLANES + p) * 4 + j) * 64 + lane];
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    const u32x4_t m = q4_decode8(w[i][j], (sc[i] >> (8 * c)) << 23);
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int p = 0; p < PLANES; ++p) acc[i][r] = q4_mfma(m, b[r][p], acc[i][r]);
-                }
-            }
-        }
-    }
-    // the waves' parts, added in the order of the waves
-    f32x4_t* lds = reinterpret_cast<f32x4_t*>(w4_lds);
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int r = 0; r < R; ++r) lds[(wave * NT * R + i * R + r) * 64 + lane] = acc[i][r];
-    __syncthreads();
-    for (int e = wave; e < NT * R; e += waves) {
-        f32x4_t s = lds[e * 64 + lane];
-        for (int w = 1; w < waves; ++w) s += lds[(w * NT * R + e) * 64 + lane];
-        const int row = (rt0 + e % R) * 16 + (lane & 15), n = (n0 + e / R) * 16 + (lane >> 4) * 4;
-        if (row >= a.rows) continue;
-        if (a.part) {
-            float* o = a.part + ((int64_t)blockIdx.y * a.rows + row) * a.n + n;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (n + i < a.n) o[i] = s[i];
-        } else {
-            T* o = static_cast<T*>(a.y) + row * a.ldy + n;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (n + i < a.n) st1(o + i, s[i]);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = row[min(k0 + 2 * i, k - 1)].v, hi = row[min(k0 + 2 * i + 1, k - 1)].v;
+            o.v[i] = (k0 + 2 * i < k ? lo : 0u) | (k0 + 2 * i + 1 < k ? hi << 16 : 0u);
         }
     }
 }
+template <bool VEC> __device__ __forceinline__ void w4_load(const float* row, int k0, int k, W4Piece<float>& o) {
+    if constexpr (VEC) {
+        o.a = *reinterpret_cast<const f32x4_t*>(row + k0);
+        o.b = *reinterpret_cast<const f32x4_t*>(row + k0 + 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p = row[min(k0 + i, k - 1)], q = row[min(k0 + 4 + i, k - 1)];
+            o.a[i] = k0 + i < k ? p : 0.f;
+            o.b[i] = k0 + 4 + i < k ? q : 0.f;
+        }
+    }
+}
+// the piece as operands, one per plane, `stride` vectors apart
+__device__ __forceinline__ void w4_put(const W4Piece<bf16_t>& x, u32x4_t* at, int) { *at = x.v; }
+__device__ __forceinline__ void w4_put(const W4Piece<float>& x, u32x4_t* at, int stride) {
+    const float v[8] = {x.a[0], x.a[1], x.a[2], x.a[3], x.b[0], x.b[1], x.b[2], x.b[3]};
+    u32x4_t o[3];
+    q4_operand<3>(v, o);
+    at[0] = o[0];
+    at[stride] = o[1];
+    at[2 * stride] = o[2];
+}
+template <int NT> struct W4Tile { u32x4_t w[NT]; uint32_t s[NT]; };
+template <int NT> __device__ __forceinline__ void w4_load(const W4Args& a, int n0, int t, int lane, W4Tile<NT>& o) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int n = min(n0 + i, a.nt - 1);
+        o.w[i] = a.codes[((int64_t)n * a.kt + t) * 64 + lane];
+        o.s[i] = a.scales[((int64_t)n * a.ks + (t >> 2)) * 64 + lane];
+    }
+}
+// four results (rows of W n .. n + 3) of row `row` of x.  The splits' rows are padded to whole vectors; y takes vectors where it is aligned for them.
+__host__ __device__ inline int w4_padded(int n) { return (n + 3) & ~3; }
+template <typename T> __device__ __forceinline__ void w4_store(const W4Args& a, int split, int row, int n, f32x4_t s) {
+    if (row >= a.rows || n >= a.n) return;
+    if (a.part) {
+        *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)split * a.rows + row) * w4_padded(a.n) + n) = s;
+        return;
+    }
+    T* o = static_cast<T*>(a.y) + row * a.ldy + n;
+    if (n + 3 < a.n && a.y_wide) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(f2bf2(s[0], s[1]), f2bf2(s[2], s[3]));
+        else *reinterpret_cast<f32x4_t*>(o) = s;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (n + i < a.n) st1(o + i, s[i]);
+    }
+}
 
+// Up to 16 rows of x (XL * 4 of them).  A block owns NT tiles of rows of W, its waves share the columns.  A wave brings its part of x into operand order through
+// LDS of its own: no barrier until the waves' sums are added, in the order of the waves.  Columns of the matrix instruction beyond the rows of x
+// repeat some row; nobody reads their results.
+// Bound by the weights' bytes: 7B gate and up, one row: 72 MB in 14.5 us; what x costs is read once per block, from L2.
+// waves that a block may have: their parts of x, and their sums, share 64 KB (fp32 with up to 16 rows: 96 KB)
+template <typename T, int XL> constexpr int w4_few_waves = w4_planes<T> == 3 && XL == 4 ? 8 : 16;
+template <typename T, int NT, int XL, bool VEC>
+__global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Args a) {
+    constexpr int P = w4_planes<T>, WAVES = w4_few_waves<T, XL>, XR = XL * 4, PLANE = 16 * XR;
+    __shared__ u32x4_t lds[WAVES * (P * PLANE > NT * 64 ? P * PLANE : NT * 64)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int n0 = blockIdx.x * NT;
+    // the block's tiles of columns, dealt to the waves in runs
+    const int b0 = blockIdx.y * a.tiles, count = min(a.kt - b0, a.tiles);
+    const int t0 = b0 + count * wave / waves, t1 = b0 + count * (wave + 1) / waves;
+    u32x4_t* stage = lds + wave * P * PLANE;                // [plane][j][q][row]
+    const T* row[XL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) row[i] = static_cast<const T*>(a.x) + (int64_t)min(i * 4 + (lane >> 4), a.rows - 1) * a.ldx;
+    const int k8 = lane & 15;                               // the piece of a row's 128 columns; operand k8 % 4 of group k8 / 4
+    f32x4_t acc[NT] = {};
+    W4Tile<NT> w[2];
+    W4Piece<T> x[2][XL];
+    auto load = [&](int t, W4Tile<NT>& w_, W4Piece<T>(&x_)[XL]) {
+        t = min(t, t1 - 1);
+#pragma unroll
+        for (int i = 0; i < XL; ++i) w4_load<VEC>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
+        w4_load<NT>(a, n0, t, lane, w_);
+    };
+    auto work = [&](int t, const W4Tile<NT>& w_, const W4Piece<T>(&x_)[XL]) {
+#pragma unroll
+        for (int i = 0; i < XL; ++i) w4_put(x_[i], stage + ((k8 & 3) * 4 + (k8 >> 2)) * XR + i * 4 + (lane >> 4), PLANE);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4_t b[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) b[p] = stage[p * PLANE + (j * 4 + (lane >> 4)) * XR + (lane & (XR - 1))];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const u32x4_t m = q4_decode8(w_.w[i][j], (w_.s[i] >> (8 * (t & 3))) << 23);
+#pragma unroll
+                for (int p = 0; p < P; ++p) acc[i] = q4_mfma(m, b[p], acc[i]);
+            }
+        }
+    };
+    if (t0 < t1) {
+        load(t0, w[0], x[0]);
+        for (int t = t0;;) {
+            load(t + 1, w[1], x[1]);
+            work(t, w[0], x[0]);
+            if (++t >= t1) break;
+            load(t + 1, w[0], x[0]);
+            work(t, w[1], x[1]);
+            if (++t >= t1) break;
+        }
+    }
+    __syncthreads();                                        // the stages become the sums' place
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(lds);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sums[(wave * NT + i) * 64 + lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < NT; i += waves) {
+        f32x4_t s = sums[i * 64 + lane];
+        for (int v = 1; v < waves; ++v) s += sums[(v * NT + i) * 64 + lane];
+        w4_store<T>(a, blockIdx.y, lane & 15, (n0 + i) * 16 + (lane >> 4) * 4, s);
+    }
+}
+
+// More rows: a block of four waves owns 16 tiles of rows of W, four to a wave, and XT tiles of rows of x.  x goes through LDS in operand order, shared by the
+// waves; a wave decodes its own weights, which stay in registers for XT products each.  Splits start at multiples of four tiles of columns, so that
+// a word of scale bytes serves one turn of the loop.
+//  - Loads run three tiles ahead: a tile is 0.4 us of matrix work, less than a load takes.
+//  - 16 lanes load 256 consecutive bytes of one row of x (with 16 rows x 64 bytes the loads of x alone took 22 of 51 us at 64 rows of the 7B gate and up product).
+//    They write to 16 different operands: slot r of operand (j, q) is kept at r ^ (4 q + j), or all of them would hit the same banks.
+//  - Splits are the fastest index of the grid: with eight of them an XCD's L2 sees one part of x (256 rows, 7B down: 90 -> 70 us).
+// Bound by the issue of a single wave per SIMD: a product takes 25 clocks instead of 16 with the conversions, LDS operands and loads between.  256 rows,
+// 3584 x 18944: 44 us, 790 TFLOP/s, and 5 us for the sums.
+template <typename T, int XT, bool VEC>
+__global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
+    constexpr int P = w4_planes<T>, NT = 4, DW = 4, DX = 4;
+    __shared__ u32x4_t lds[2][P][XT * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = (blockIdx.y * 4 + wave) * NT, r0 = blockIdx.z * XT * 16;
+    const int t0 = blockIdx.x * a.tiles, t1 = min(a.kt, t0 + a.tiles);
+    f32x4_t acc[NT][XT] = {};
+    u32x4_t w[DW][NT];
+    uint32_t scale[2][NT];
+    W4Piece<T> x[DX][XT];
+    // piece i of a thread: row 16 i + tid / 16 of the block's, columns 8 (tid % 16) of the tile's 128
+    const int k8 = tid & 15, slot = (tid >> 4) ^ ((k8 >> 2) * 4 + (k8 & 3));
+    const T* row[XT];
+#pragma unroll
+    for (int i = 0; i < XT; ++i) row[i] = static_cast<const T*>(a.x) + (int64_t)min(r0 + i * 16 + (tid >> 4), a.rows - 1) * a.ldx;
+    const u32x4_t* codes[NT];
+    const uint32_t* scales[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int64_t n = min(n0 + i, a.nt - 1);
+        codes[i] = a.codes + n * a.kt * 64;
+        scales[i] = a.scales + n * a.ks * 64;
+    }
+    auto load_x = [&](int t, W4Piece<T>(&x_)[XT]) {
+        t = min(t, t1 - 1);
+#pragma unroll
+        for (int i = 0; i < XT; ++i) w4_load<VEC>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
+    };
+    auto put_x = [&](const W4Piece<T>(&x_)[XT], int buf) {
+#pragma unroll
+        for (int i = 0; i < XT; ++i) w4_put(x_[i], &lds[buf][0][(i * 4 + (k8 & 3)) * 64 + (k8 >> 2) * 16 + slot], XT * 256);
+    };
+    auto load_w = [&](int t, u32x4_t(&w_)[NT]) {
+        t = min(t, t1 - 1);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) w_[i] = codes[i][t * 64 + lane];
+    };
+    auto load_s = [&](int t, uint32_t(&s_)[NT]) {
+        t = min(t, t1 - 1) >> 2;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) s_[i] = scales[i][t * 64 + lane];
+    };
+    const int q = lane >> 4, r = lane & 15;
+    int place[4];                                           // where operand j keeps this lane's slot
+#pragma unroll
+    for (int j = 0; j < 4; ++j) place[j] = j * 64 + q * 16 + (r ^ (4 * q + j));
+    auto work = [&](int shift, int buf, const u32x4_t(&w_)[NT], const uint32_t(&s_)[NT]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4_t m[NT], b[XT][P];
+#pragma unroll
+            for (int e = 0; e < XT; ++e)
+#pragma unroll
+                for (int p = 0; p < P; ++p) b[e][p] = lds[buf][p][e * 256 + place[j]];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) m[i] = q4_decode8(w_[i][j], shift == 24 ? s_[i] >> 1 : s_[i] << (23 - shift));
+#pragma unroll
+            for (int e = 0; e < XT; ++e)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) acc[i][e] = q4_mfma(m[i], b[e][p], acc[i][e]);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < DX; ++s) load_x(t0 + s, x[s]);
+    load_s(t0, scale[0]);
+#pragma unroll
+    for (int s = 0; s < DW - 1; ++s) load_w(t0 + s, w[s]);
+    put_x(x[0], 0);
+    __syncthreads();
+    for (int t = t0; t < t1; t += 2 * DW) {                 // two turns: the scales have two buffers
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_s(t + (h + 1) * DW, scale[1 - h]);
+#pragma unroll
+            for (int s = 0; s < DW; ++s) {
+                const int u = t + h * DW + s;
+                load_x(u + DX, x[s % DX]);
+                load_w(u + DW - 1, w[(s + DW - 1) % DW]);
+                if (u < t1) {
+                    put_x(x[(s + 1) % DX], (s + 1) & 1);
+                    work(8 * s, s & 1, w[s], scale[h]);
+                }
+                __syncthreads();
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < XT; ++e) w4_store<T>(a, blockIdx.x, r0 + e * 16 + (lane & 15), (n0 + i) * 16 + (lane >> 4) * 4, acc[i][e]);
+}
+
+// the splits' sums, in order; four results to a thread
 template <typename T>
-__global__ void w4_sum_kernel(const float* __restrict__ part, int splits, int rows, int n, T* __restrict__ y, int64_t ldy) {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)rows * n;
+__global__ __launch_bounds__(256) void w4_sum_kernel(W4Args a, int splits) {
+    const int quads = w4_padded(a.n) / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)a.rows * quads;
     if (id >= total) return;
-    float s = part[id];
-    for (int i = 1; i < splits; ++i) s += part[i * total + id];
-    st1(y + id / n * ldy + id % n, s);
+    const f32x4_t* part = reinterpret_cast<const f32x4_t*>(a.part) + id;
+    f32x4_t s = part[0];
+#pragma unroll 4
+    for (int i = 1; i < splits; ++i) s += part[i * total];
+    W4Args y = a;
+    y.part = nullptr;
+    w4_store<T>(y, 0, (int)(id / quads), (int)(id % quads) * 4, s);
 }
 
 // Weights [n][k] (fp32 or bf16, rows `ld` apart) to tiles: 16 lanes take one group of 32 columns.

@@ -87,11 +87,11 @@ def test_small_or_unaligned_workspaces_are_refused(lib):
     need = lib.rsd_kv4_evict_workspace(C.byref(c), 100)
     for ws, n in ((1 << 20, need - 1), (None, need), ((1 << 20) + 16, need)):
         assert lib.rsd_kv4_evict(C.byref(c), C.byref(book), 100, 0, ws, n, None) == -1
-    w = ops._W4(4096, 4096, 1000, 5000)
-    need = lib.rsd_w4_linear_workspace(7, 1000, 5000, 0)
+    w = ops._W4(4096, 4096, 200, 5000)
+    need = lib.rsd_w4_linear_workspace(300, 200, 5000, 0)
     assert need > 0
     for ws, n in ((1 << 20, need - 1), (None, need), ((1 << 20) + 16, need)):
-        assert lib.rsd_w4_linear(C.byref(w), 4096, 5000, 4096, 1000, 7, 0, ws, n, None) == -1
+        assert lib.rsd_w4_linear(C.byref(w), 4096, 5000, 4096, 200, 300, 0, ws, n, None) == -1
 
 
 @pytest.mark.parametrize("budget,recent", [(0, 0), (-1, 0), (4, 5), (4, -1)])
