@@ -153,11 +153,13 @@ struct Kv4Attn {
     int64_t q_row, q_head;
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
     int total_rows, max_rows, heads, group;
-    float factor2;          // scale * log2(e): exponents are taken to the base 2
+    float factor2;          // |scale| * log2(e): exponents are taken to the base 2
+    bool negative;          // scale < 0: q changes its sign instead
     void* out;
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
-    int max_kv, split, splits, tiles;
+    int max_kv, split, splits, hd;
+    bool q_wide, o_wide;    // rows and heads of q start on multiples of 16 bytes, of out on multiples of four values
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
     Kv4Book book;
@@ -207,13 +209,24 @@ template <int HD> __device__ __forceinline__ void kv4_load_vals(const uint8_t* c
 template <typename T, int HD, int PLANES>
 __device__ __forceinline__ void kv4_load_q(const Kv4Attn& a, int r0, int count, int head, int col, int lane, u32x4_t q[HD / 32][PLANES]) {
     const int r = col / a.group, g = col % a.group;
-    const T* p = static_cast<const T*>(a.q) + (int64_t)(r0 + r) * a.q_row + (int64_t)(head * a.group + g) * a.q_head + (lane >> 4) * (HD / 4);
+    // a column beyond the rows repeats the last one; its results are not used
+    const T* p = static_cast<const T*>(a.q) + (int64_t)(r0 + min(r, count - 1)) * a.q_row + (int64_t)(head * a.group + g) * a.q_head + (lane >> 4) * (HD / 4);
+    float x[HD / 32][8];
+    if (a.q_wide) {
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) load8(p + j * 8, x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j][i] = ld1(p + j * 8 + i);
+    }
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) {
-        float x[8];
+        if (a.negative)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = r < count ? ld1(p + j * 8 + i) : 0.f;
-        q4_operand<PLANES>(x, q[j]);
+            for (int i = 0; i < 8; ++i) x[j][i] = -x[j][i];
+        q4_operand<PLANES>(x[j], q[j]);
     }
 }
 // scores of one page: rows (tokens) 4 (lane / 16) + i, column lane % 16
@@ -228,285 +241,471 @@ __device__ __forceinline__ f32x4_t kv4_scores(const Kv4Keys<HD>& k, int p, const
     }
     return s;
 }
-// values of two pages, group g, as the A operands of dims 32 g .. + 15 (lo) and 32 g + 16 .. + 31 (hi)
-template <int HD> __device__ __forceinline__ void kv4_val_operands(const Kv4Vals<HD>& v, int p, int g, u32x4_t& lo, u32x4_t& hi) {
+// one group's values of two pages (w: bytes, s: scale bytes of four tokens) as the A operands of its dims 0 .. 15 (lo) and 16 .. 31 (hi)
+__device__ __forceinline__ void kv4_pair_operands(uint32_t w0, uint32_t s0, uint32_t w1, uint32_t s1, u32x4_t& lo, u32x4_t& hi) {
+    const uint32_t w[2] = {w0, w1}, s[2] = {s0, s1};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const uint32_t w = v.w[p + e][g], s = v.scale[p + e][g];
-        const uint32_t c0 = q4_decode2<0>(w, q4_scale_at<0>(s)), c1 = q4_decode2<1>(w, q4_scale_at<1>(s));
-        const uint32_t c2 = q4_decode2<2>(w, q4_scale_at<2>(s)), c3 = q4_decode2<3>(w, q4_scale_at<3>(s));
+        const uint32_t c0 = q4_decode2<0>(w[e], q4_scale_at<0>(s[e])), c1 = q4_decode2<1>(w[e], q4_scale_at<1>(s[e]));
+        const uint32_t c2 = q4_decode2<2>(w[e], q4_scale_at<2>(s[e])), c3 = q4_decode2<3>(w[e], q4_scale_at<3>(s[e]));
         lo[2 * e] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
         lo[2 * e + 1] = __builtin_amdgcn_perm(c3, c2, 0x05040100u);
         hi[2 * e] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
         hi[2 * e + 1] = __builtin_amdgcn_perm(c3, c2, 0x07060302u);
     }
 }
-
+// the scale bytes of four tokens of which the first `left` are to be kept
+__device__ __forceinline__ uint32_t kv4_keep(int left) { return left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1; }
+// bit 8 i + 7: byte i is 255 and i >= from
+__device__ __forceinline__ uint32_t kv4_nan_marks(uint32_t s, int from) {
+    const uint32_t look = from <= 0 ? 0xFFFFFFFFu : from >= 4 ? 0u : 0xFFFFFFFFu << (8 * from);
+    return ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u & look;
+}
 // An entry that reads as NaN must not reach the columns that do not see it (as 0 * NaN).  Such groups among the entries from slot `safe` on
 // are taken out of the product (scale byte 0), and the sums of the columns that do see the entry become NaN instead.
-template <int HD, int MT>
-__device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int safe, const int (&limit)[MT], f32x4_t (&o)[MT][HD / 16]) {
+template <int HD>
+__device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int safe, int limit, f32x4_t (&o)[HD / 16]) {
     const int quad = (threadIdx.x & 63) >> 4;
     uint32_t any = 0;
     uint32_t marks[4][HD / 32];                             // bit 8 i + 7: token i of the quad is NaN in this group
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int from = safe - (slot0 + p * KV4_PAGE + quad * 4);
-        const uint32_t look = from <= 0 ? 0xFFFFFFFFu : from >= 4 ? 0u : 0xFFFFFFFFu << (8 * from);
 #pragma unroll
         for (int g = 0; g < HD / 32; ++g) {
-            const uint32_t s = v.scale[p][g];
-            marks[p][g] = ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u & look;
+            marks[p][g] = kv4_nan_marks(v.scale[p][g], from);
             any |= marks[p][g];
         }
     }
     if (!__any(any != 0)) return;
+    // how many such entries each column sees: a product of marks (rows: any dim) and of what is seen, like the one of values and probabilities
+    f32x4_t seen[HD / 32] = {};
+#pragma unroll
+    for (int p = 0; p < 4; p += 2) {
+        u32x4_t mark[HD / 32];
+#pragma unroll
+        for (int g = 0; g < HD / 32; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t m = marks[p + e / 2][g] >> (16 * (e & 1));
+                mark[g][e] = (m & 0x80u ? 0x3F80u : 0u) | (m & 0x8000u ? 0x3F800000u : 0u);
+            }
+        u32x4_t sees;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int slot = slot0 + (p + e / 2) * KV4_PAGE + quad * 4 + 2 * (e & 1);
+            sees[e] = (slot < limit ? 0x3F80u : 0u) | (slot + 1 < limit ? 0x3F800000u : 0u);
+        }
+#pragma unroll
+        for (int g = 0; g < HD / 32; ++g) seen[g] = q4_mfma(mark[g], sees, seen[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < HD / 32; ++g) {
+        const float add = seen[g][0] > 0.f ? __uint_as_float(0x7FC00000u) : 0.f;
+        o[2 * g] += add;
+        o[2 * g + 1] += add;
+    }
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
-        for (int g = 0; g < HD / 32; ++g) {
-            v.scale[p][g] &= ~((marks[p][g] >> 7) * 255u);
-            for (int t = 0; t < KV4_PAGE; ++t) {            // every lane looks at every token of the page
-                const uint32_t m = (uint32_t)__builtin_amdgcn_readlane((int)marks[p][g], t / 4 * 16);
-                if (!((m >> (8 * (t % 4) + 7)) & 1)) continue;
-#pragma unroll
-                for (int c = 0; c < MT; ++c)
-                    if (slot0 + p * KV4_PAGE + t < limit[c]) {
-                        const float nan = __uint_as_float(0x7FC00000u);
-                        o[c][2 * g] = f32x4_t{nan, nan, nan, nan};
-                        o[c][2 * g + 1] = f32x4_t{nan, nan, nan, nan};
-                    }
-            }
-        }
+        for (int g = 0; g < HD / 32; ++g) v.scale[p][g] &= ~((marks[p][g] >> 7) * 255u);
 }
 
-// A block owns MT tiles of 16 columns of one (sequence, kv head) and one part of its entries, of which its four waves take chunks of 64
-// in turn, each with its own running maximum and sum; they are joined in LDS.
-template <typename T, int HD, int PLANES, int MT>
-__global__ __launch_bounds__(256) void kv4_attn_kernel(Kv4Attn a) {
-    constexpr int G = HD / 32;
-    constexpr int PP = PLANES == 1 ? 2 : 3;                 // parts of a probability: see below
-    __shared__ __align__(16) float lds_o[4][MT][G * 2][64][4];
-    __shared__ float lds_ml[4][MT][2][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
-    const int bh = blockIdx.x / a.tiles, tile0 = blockIdx.x % a.tiles * MT;
-    const int b = bh / a.c.hkv, head = bh % a.c.hkv;
-    int r0, count, n;
-    kv4_rows(a, b, r0, count, n);
-    const int cols = count * a.group;
-    if (tile0 * 16 >= cols) return;
-    // entries seen by the column's row: slots < limit
-    int limit[MT];
-    u32x4_t q[MT][G][PLANES];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int col = (tile0 + m) * 16 + (lane & 15);
-        limit[m] = col < cols ? n - (count - 1 - col / a.group) : 0;
-        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q[m]);
-    }
-    const int last_row = min(cols - 1, (tile0 + MT) * 16 - 1) / a.group;
-    const int begin = blockIdx.y * a.split, end = min(begin + a.split, n - (count - 1 - last_row));
-    const int safe = min(end, n - (count - 1 - tile0 * 16 / a.group));      // below: every column sees every entry
-
-    f32x4_t o[MT][2 * G] = {};
-    float top[MT], sum[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) top[m] = -INFINITY, sum[m] = 0.f;
-    for (int slot0 = begin + wave * KV4_CHUNK; slot0 < end; slot0 += 4 * KV4_CHUNK) {
-        const uint8_t* page[4];
-        int there;
-        kv4_pages<HD>(a.c, b, head, slot0, page, there);
-        Kv4Keys<HD> k;
-        Kv4Vals<HD> v;
-        kv4_load_keys<HD>(page, lane, k);
-        kv4_load_vals<HD>(page, lane, v);
-        const bool whole = slot0 + KV4_CHUNK <= safe && there == 15;
-        if (!whole) {
-            // Values that are not there, or not seen by all columns: what lies behind the last entry may read as NaN, and 0 * NaN is NaN.
-            // Their scales are cleared.
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int left = (there >> p) & 1 ? end - (slot0 + p * KV4_PAGE + quad * 4) : 0;
-                const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-#pragma unroll
-                for (int g = 0; g < G; ++g) v.scale[p][g] &= keep;
-            }
-            if (slot0 + KV4_CHUNK > safe) kv4_nan_values<HD, MT>(v, slot0, safe, limit, o);
-        }
-        f32x4_t s[MT][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                s[m][p] = kv4_scores<HD, PLANES>(k, p, q[m]) * a.factor2;
-                if (!whole) {
-                    const int end_p = (there >> p) & 1 ? min(limit[m], end) : 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[m][p][i] = slot0 + p * KV4_PAGE + quad * 4 + i < end_p ? s[m][p][i] : -INFINITY;
-                }
-            }
-            float best = -INFINITY;
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) best = fmaxf(best, s[m][p][i]);
-            best = fmaxf(top[m], rows4_max(best));
-            const float base = best == -INFINITY ? 0.f : best;
-            const float scale = __builtin_amdgcn_exp2f(top[m] - base);
-            top[m] = best;
-            sum[m] *= scale;
-#pragma unroll
-            for (int d = 0; d < 2 * G; ++d) o[m][d] *= scale;
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[m][p][i] = __builtin_amdgcn_exp2f(s[m][p][i] - base);
-                    sum[m] += s[m][p][i];
-                }
-        }
-        // Probabilities as operands: the sum of two bf16 numbers (16 bits) where the result is rounded to bf16, of three (all 24 bits) where it is fp32.
-#pragma unroll
-        for (int p = 0; p < 4; p += 2) {
-            u32x4_t w[MT][PP];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = s[m][p + i / 2][2 * (i % 2)], y = s[m][p + i / 2][2 * (i % 2) + 1];
-                    if constexpr (PP == 2) {
-                        uint32_t hi, lo;
-                        split2(x, y, hi, lo);
-                        w[m][0][i] = hi;
-                        w[m][1][i] = lo;
-                    } else {
-                        uint32_t a0, b0, c0, a1, b1, c1;
-                        q4_cut3(x, a0, b0, c0);
-                        q4_cut3(y, a1, b1, c1);
-                        w[m][0][i] = a0 | (a1 << 16);
-                        w[m][1][i] = b0 | (b1 << 16);
-                        w[m][2][i] = c0 | (c1 << 16);
-                    }
-                }
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                u32x4_t lo, hi;
-                kv4_val_operands<HD>(v, p, g, lo, hi);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int x = 0; x < PP; ++x) {
-                        o[m][2 * g] = q4_mfma(lo, w[m][x], o[m][2 * g]);
-                        o[m][2 * g + 1] = q4_mfma(hi, w[m][x], o[m][2 * g + 1]);
-                    }
-            }
-        }
-    }
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        sum[m] = rows4_sum(sum[m]);
-        if (quad == 0) lds_ml[wave][m][0][lane] = top[m], lds_ml[wave][m][1][lane] = sum[m];
-#pragma unroll
-        for (int d = 0; d < 2 * G; ++d) *reinterpret_cast<f32x4_t*>(lds_o[wave][m][d][lane]) = o[m][d];
-    }
-    __syncthreads();
-    for (int e = wave; e < MT * 2 * G; e += 4) {
-        const int m = e / (2 * G), d = e % (2 * G), c = lane & 15, col = (tile0 + m) * 16 + c;
-        float best = -INFINITY, total = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) best = fmaxf(best, lds_ml[w][m][0][c]);
-        const float base = best == -INFINITY ? 0.f : best;
-        f32x4_t acc = {};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float scale = __builtin_amdgcn_exp2f(lds_ml[w][m][0][c] - base);
-            total += scale * lds_ml[w][m][1][c];
-            acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][m][d][lane]);
-        }
-        if (col >= cols) continue;
-        const int64_t row = r0 + col / a.group;
-        const int qh = head * a.group + col % a.group, dim = d * 16 + quad * 4;
-        if (a.splits > 1) {
-            const int64_t at = (row * a.heads + qh) * a.splits + blockIdx.y;
-            *reinterpret_cast<f32x4_t*>(a.part_o + at * HD + dim) = acc;
-            if (d == 0 && quad == 0) a.part_ml[at] = make_float2(best, total);
-        } else {
-            const float inv = total == 0.f ? 0.f : 1.f / total;
-            T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st1(dst + i, acc[i] * inv);
-            if (d == 0 && quad == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
-        }
-    }
-}
-
-// joins the parts of the entries: one wave per (row, head)
+// what a column has gathered, for the join: rows (dims) 4 quad + i of every block d of 16 dims, column lane % 16
 template <typename T>
-__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a, int hd) {
-    const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= (int64_t)a.c.batch * a.max_rows * a.heads) return;
-    const int qh = (int)(id % a.heads), r = (int)(id / a.heads % a.max_rows), b = (int)(id / a.heads / a.max_rows);
-    int r0, count, n;
-    kv4_rows(a, b, r0, count, n);
-    if (r >= count) return;
-    // the blocks of this column's tile wrote a part for every split (an empty one where there was nothing to see)
-    const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;
-    float best = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) best = fmaxf(best, a.part_ml[at + s].x);
-    const float base = best == -INFINITY ? 0.f : best;
-    float total = 0.f, acc[2] = {0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = a.part_ml[at + s];
-        const float scale = __builtin_amdgcn_exp2f(ml.x - base);
-        total += scale * ml.y;
-        for (int d = lane, i = 0; d < hd; d += 64, ++i) acc[i] += scale * a.part_o[(at + s) * hd + d];
+__device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total) {
+    if (a.splits > 1) {
+        const int64_t at = (row * a.heads + qh) * a.splits + blockIdx.z;
+        *reinterpret_cast<f32x4_t*>(a.part_o + at * a.hd + dim) = acc;
+        if (first) a.part_ml[at] = make_float2(top, total);
+        return;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head;
-    for (int d = lane, i = 0; d < hd; d += 64, ++i) st1(dst + d, acc[i] * inv);
-    if (lane == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+    T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
+    if (a.o_wide) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv));
+        else *reinterpret_cast<f32x4_t*>(dst) = acc * inv;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st1(dst + i, acc[i] * inv);
+    }
+    if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
 }
 
-// Attention weight per entry, added to the accumulated one: the scores are computed a second time (keys are half of the cache; storing a
-// group's probabilities would move as many bytes), now with the final sum of every row.  A wave owns 64 entries of one (sequence, kv head): no atomics, one order.
-template <typename T, int HD, int PLANES>
-__global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
-    constexpr int G = HD / 32;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
-    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
-    int r0, count, n;
-    kv4_rows(a, b, r0, count, n);
-    const int cols = count * a.group, slot0 = (blockIdx.y * 4 + wave) * KV4_CHUNK;
-    if (slot0 >= n || cols == 0) return;
-    const uint8_t* page[4];
-    int there;
-    kv4_pages<HD>(a.c, b, head, slot0, page, there);
-    Kv4Keys<HD> k;
-    kv4_load_keys<HD>(page, lane, k);
-    f32x4_t weight[4] = {};
-    for (int c0 = 0; c0 < cols; c0 += 16) {
-        const int col = c0 + (lane & 15), r = col / a.group;
-        const int limit = col < cols ? n - (count - 1 - r) : 0;
-        const float lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : 0.f;
-        u32x4_t q[G][PLANES];
-        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
+// One chunk against one tile of columns: scores q.k (masked where `whole` is false), new maximum, probabilities in place of the scores; what was gathered is scaled.
+// factor2 >= 0; top is in units of the exponent.
+template <int NB>
+__device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there, int slot0, int limit, int quad, float factor2, float& top, float& sum, f32x4_t o[NB]) {
+    if (!whole) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q) * a.factor2;
-            const int end = (there >> p) & 1 ? limit : 0;
+            const int end_p = (there >> p) & 1 ? limit : 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) weight[p][i] += slot0 + p * KV4_PAGE + quad * 4 + i < end ? __builtin_amdgcn_exp2f(s[i] - lse2) : 0.f;
+            for (int i = 0; i < 4; ++i) s[p][i] = slot0 + p * KV4_PAGE + quad * 4 + i < end_p ? s[p][i] : -INFINITY;
         }
+    }
+    float best = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) best = fmaxf(best, s[p][i]);
+    best = rows4_max(best);
+    best = fmaxf(top, best == -INFINITY ? best : best * factor2);      // (0 * inf is no maximum)
+    const float base = best == -INFINITY ? 0.f : best;
+    if (__any(best != top)) {                               // a new maximum somewhere in the tile
+        const float scale = __builtin_amdgcn_exp2f(top - base);
+        sum *= scale;
+#pragma unroll
+        for (int d = 0; d < NB; ++d) o[d] *= scale;
+        top = best;
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float w = row16_sum(weight[p][i]);
-            const int slot = slot0 + p * KV4_PAGE + quad * 4 + i;
-            if ((lane & 15) == 0 && slot < n && ((there >> p) & 1)) a.book.scores[b * a.book.score_b + head * a.book.score_h + slot] += w;
+            float e = __builtin_fmaf(s[p][i], factor2, -base);
+            if (!whole) e = s[p][i] == -INFINITY ? -INFINITY : e;       // factor2 = 0
+            s[p][i] = __builtin_amdgcn_exp2f(e);
+            sum += s[p][i];
         }
+}
+// Probabilities of two pages as operands: the sum of two bf16 numbers (16 bits) where the result is rounded to bf16, of three (all 24 bits) where it is fp32.
+template <int PP> __device__ __forceinline__ void kv4_weights(const f32x4_t s0, const f32x4_t s1, u32x4_t w[PP]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = i < 2 ? s0[2 * i] : s1[2 * i - 4], y = i < 2 ? s0[2 * i + 1] : s1[2 * i - 3];
+        if constexpr (PP == 2) {
+            uint32_t hi, lo;
+            split2(x, y, hi, lo);
+            w[0][i] = hi;
+            w[1][i] = lo;
+        } else {
+            // cut as in q4_cut3; a probability is at most 1 or NaN, whose first part is NaN
+            const float x1 = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u), y1 = y - __uint_as_float(__float_as_uint(y) & 0xFFFF0000u);
+            const float x2 = x1 - __uint_as_float(__float_as_uint(x1) & 0xFFFF0000u), y2 = y1 - __uint_as_float(__float_as_uint(y1) & 0xFFFF0000u);
+            w[0][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+            w[1][i] = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(x1), 0x07060302u);
+            w[2][i] = __builtin_amdgcn_perm(__float_as_uint(y2), __float_as_uint(x2), 0x07060302u);
+        }
+    }
+}
+
+// Few columns (single tokens, verification of a few): a block owns a tile of 16 columns of one (sequence, kv head) and one part of its entries, of which
+// its waves take chunks of 64 in turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's bytes are requested before
+// this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (28 columns, 64 sequences: 62 us against 78 with
+// both tiles in one wave's registers).
+// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 186 us, 4.6 TB/s, of the 4.9 that a copy reaches; 519 vector and 48 matrix instructions per chunk
+// keep a SIMD busy for two thirds of that.  Without the requests ahead 190 us, with them dropped for a third wave per SIMD 198.
+template <typename T, int HD, int PLANES>
+__global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, WAVES = 8;
+    __shared__ __align__(16) float lds_o[WAVES][G * 2][64][4];
+    __shared__ float lds_ml[WAVES][2][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, quad = lane >> 4;
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * 16, col = col0 + (lane & 15);
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group;
+    if (col0 >= cols) return;
+    const int begin = blockIdx.z * a.split, end = min(begin + a.split, n - (count - 1 - (min(cols, col0 + 16) - 1) / a.group));
+    const int safe = min(end, n - (count - 1 - col0 / a.group));      // below: every column sees every entry
+    const int limit = min(end, col < cols ? n - (count - 1 - col / a.group) : 0);      // entries seen by the column's row: slots below
+    const int step = waves * KV4_CHUNK;
+
+    Kv4Keys<HD> k[2];
+    Kv4Vals<HD> v[2];
+    const uint8_t* page[2][4];
+    int there[2];
+    int slot0 = begin + wave * KV4_CHUNK;
+    u32x4_t q[G][PLANES];
+    f32x4_t o[2 * G] = {};
+    float top = -INFINITY, sum = 0.f;
+    auto work = [&](Kv4Keys<HD>& k_, Kv4Vals<HD>& v_, int there_) {
+        const bool whole = slot0 + KV4_CHUNK <= safe && there_ == 15;
+        if (!whole) {
+            // Values that are not there, or not seen by all columns: what lies behind the last entry may read as NaN, and 0 * NaN is NaN.
+            // Their scales are cleared.
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const uint32_t keep = kv4_keep((there_ >> p) & 1 ? end - (slot0 + p * KV4_PAGE + quad * 4) : 0);
+#pragma unroll
+                for (int g = 0; g < G; ++g) v_.scale[p][g] &= keep;
+            }
+            if (slot0 + KV4_CHUNK > safe) kv4_nan_values<HD>(v_, slot0, safe, limit, o);
+        }
+        f32x4_t s[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) s[p] = kv4_scores<HD, PLANES>(k_, p, q);
+        kv4_softmax<2 * G>(s, whole, there_, slot0, limit, quad, a.factor2, top, sum, o);
+#pragma unroll
+        for (int p = 0; p < 4; p += 2) {
+            u32x4_t w[PP];
+            kv4_weights<PP>(s[p], s[p + 1], w);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                u32x4_t lo, hi;
+                kv4_pair_operands(v_.w[p][g], v_.scale[p][g], v_.w[p + 1][g], v_.scale[p + 1][g], lo, hi);
+#pragma unroll
+                for (int x = 0; x < PP; ++x) {
+                    o[2 * g] = q4_mfma(lo, w[x], o[2 * g]);
+                    o[2 * g + 1] = q4_mfma(hi, w[x], o[2 * g + 1]);
+                }
+            }
+        }
+    };
+    kv4_pages<HD>(a.c, b, head, slot0, page[0], there[0]);
+    kv4_load_keys<HD>(page[0], lane, k[0]);
+    kv4_load_vals<HD>(page[0], lane, v[0]);
+    kv4_pages<HD>(a.c, b, head, slot0 + step, page[1], there[1]);
+    kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
+    while (slot0 < end) {
+        kv4_load_keys<HD>(page[1], lane, k[1]);
+        kv4_load_vals<HD>(page[1], lane, v[1]);
+        const int there1 = there[1];
+        kv4_pages<HD>(a.c, b, head, slot0 + 2 * step, page[0], there[1]);
+        work(k[0], v[0], there[0]);
+        slot0 += step;
+        if (slot0 >= end) break;
+        kv4_load_keys<HD>(page[0], lane, k[0]);
+        kv4_load_vals<HD>(page[0], lane, v[0]);
+        there[0] = there[1];
+        kv4_pages<HD>(a.c, b, head, slot0 + 2 * step, page[1], there[1]);
+        work(k[1], v[1], there1);
+        slot0 += step;
+    }
+    sum = rows4_sum(sum);
+    if (quad == 0) lds_ml[wave][0][lane] = top, lds_ml[wave][1][lane] = sum;
+#pragma unroll
+    for (int d = 0; d < 2 * G; ++d) *reinterpret_cast<f32x4_t*>(lds_o[wave][d][lane]) = o[d];
+    __syncthreads();
+    for (int d = wave; d < 2 * G; d += waves) {
+        const int c = lane & 15;
+        float best = -INFINITY, total = 0.f;
+        for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][c]);
+        const float base = best == -INFINITY ? 0.f : best;
+        f32x4_t acc = {};
+        for (int w = 0; w < waves; ++w) {
+            const float scale = __builtin_amdgcn_exp2f(lds_ml[w][0][c] - base);
+            total += scale * lds_ml[w][1][c];
+            acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
+        }
+        if (col < cols) kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total);
+    }
+}
+
+// Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
+// need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows, 72B heads, fp32: 253 us with one buffer in LDS and three waves a SIMD,
+// 267 with two buffers and two waves, 365 with two tiles to a wave (half the reads of LDS, one wave a SIMD), 510 with four waves (registers spill).
+template <typename T, int HD, int PLANES>
+__global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
+    typedef typename u32vec<G>::type V;
+    __shared__ u32x4_t lds_k[4 * G][64], lds_v[4 * G][64];              // keys [page][j], values [pair of pages][block of 16 dims]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * COLS;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group;
+    if (col0 >= cols) return;
+    const int begin = blockIdx.z * a.split, end = min(begin + a.split, n - (count - 1 - (min(cols, col0 + COLS) - 1) / a.group));
+    const int safe = min(end, n - (count - 1 - col0 / a.group));
+    const bool mine = col0 + wave * 16 < cols;              // some of this wave's columns exist
+    const int col = col0 + wave * 16 + (lane & 15);
+    const int limit = min(end, col < cols ? n - (count - 1 - col / a.group) : 0);
+    u32x4_t q[G][PLANES];
+    f32x4_t o[2 * G] = {};
+    float top = -INFINITY, sum = 0.f;
+    kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
+    // this wave's share of a chunk: its page's keys; the values of VS of the 2 G (pair of pages, group)
+    constexpr int VS = 2 * G > NW ? 2 * G / NW : 1;
+    const bool has_v = wave * VS < 2 * G;
+    const int pair = min(wave * VS, 2 * G - 1) / G * 2, g0 = wave * VS % G;
+    V raw_k;
+    uint32_t raw_ks, raw_v[2][VS], raw_vs[2][VS];
+    int there;
+    auto request = [&](int slot0) {
+        const uint8_t* page[4];
+        kv4_pages<HD>(a.c, b, head, slot0, page, there);
+        const uint8_t *pk = page[0], *pv[2] = {page[0], page[1]};
+#pragma unroll
+        for (int p = 1; p < 4; ++p) pk = wave == p ? page[p] : pk;
+        if (pair) pv[0] = page[2], pv[1] = page[3];
+        raw_k = reinterpret_cast<const V*>(pk)[lane];
+        raw_ks = pk[16 * HD + quad * (HD / 4) / 32 * 16 + (lane & 15)];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t* v = reinterpret_cast<const uint32_t*>(pv[e] + 8 * HD) + lane * G + g0;
+            const uint32_t* s = reinterpret_cast<const uint32_t*>(pv[e] + 16 * HD + HD / 2) + quad * G + g0;
+#pragma unroll
+            for (int g = 0; g < VS; ++g) raw_v[e][g] = v[g], raw_vs[e][g] = s[g];
+        }
+    };
+    auto decode = [&](int slot0) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) lds_k[wave * G + j][lane] = q4_decode8(raw_k[j], raw_ks << 23);
+        if (!has_v) return;
+        if (slot0 + KV4_CHUNK > safe || there != 15) {
+            // as in the kernel above: what is not there, and NaN that not every column sees, is taken out of the product
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int first = slot0 + (pair + e) * KV4_PAGE + quad * 4;
+                const uint32_t keep = kv4_keep((there >> (pair + e)) & 1 ? end - first : 0);
+#pragma unroll
+                for (int g = 0; g < VS; ++g) raw_vs[e][g] &= keep, raw_vs[e][g] &= ~((kv4_nan_marks(raw_vs[e][g], safe - first) >> 7) * 255u);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < VS; ++g) {
+            u32x4_t lo, hi;
+            kv4_pair_operands(raw_v[0][g], raw_vs[0][g], raw_v[1][g], raw_vs[1][g], lo, hi);
+            lds_v[pair * G + 2 * (g0 + g)][lane] = lo;
+            lds_v[pair * G + 2 * (g0 + g) + 1][lane] = hi;
+        }
+    };
+    if (begin < end) request(begin);
+    for (int slot0 = begin; slot0 < end; slot0 += KV4_CHUNK) {
+        decode(slot0);
+        const int there0 = there;
+        __syncthreads();
+        request(min(slot0 + KV4_CHUNK, end - 1));
+        if (mine) {
+            if (slot0 + KV4_CHUNK > safe) {                 // a NaN that some of the columns see
+                const uint8_t* page[4];
+                int there_;
+                Kv4Vals<HD> v;
+                kv4_pages<HD>(a.c, b, head, slot0, page, there_);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    v.scale[p] = reinterpret_cast<const V*>(page[p] + 16 * HD + HD / 2)[quad];
+                    const uint32_t keep = kv4_keep((there_ >> p) & 1 ? end - (slot0 + p * KV4_PAGE + quad * 4) : 0);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) v.scale[p][g] &= keep;
+                }
+                kv4_nan_values<HD>(v, slot0, safe, limit, o);
+            }
+            f32x4_t s[4] = {};
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    const u32x4_t k = lds_k[p * G + j][lane];
+#pragma unroll
+                    for (int x = 0; x < PLANES; ++x) s[p] = q4_mfma(k, q[j][x], s[p]);
+                }
+            kv4_softmax<2 * G>(s, slot0 + KV4_CHUNK <= safe && there0 == 15, there0, slot0, limit, quad, a.factor2, top, sum, o);
+#pragma unroll
+            for (int p = 0; p < 4; p += 2) {
+                u32x4_t w[PP];
+                kv4_weights<PP>(s[p], s[p + 1], w);
+#pragma unroll
+                for (int d = 0; d < 2 * G; ++d) {
+                    const u32x4_t v = lds_v[p * G + d][lane];
+#pragma unroll
+                    for (int x = 0; x < PP; ++x) o[d] = q4_mfma(v, w[x], o[d]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    sum = rows4_sum(sum);
+    if (col >= cols) return;
+#pragma unroll
+    for (int d = 0; d < 2 * G; ++d)
+        kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum);
+}
+
+// Joins the parts of the entries: 16 lanes per (row, head), HD/16 dims each.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
+    constexpr int N = HD / 16;
+    const int l = threadIdx.x & 15;
+    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    if (id >= (int64_t)a.c.batch * a.max_rows * a.heads) return;
+    const int qh = (int)(id % a.heads), r = (int)(id / a.heads % a.max_rows), b = (int)(id / a.heads / a.max_rows);
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    if (r >= count) return;
+    // the blocks of this column wrote a part for every split (an empty one where there was nothing to see)
+    const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;
+    float best = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) best = fmaxf(best, a.part_ml[at + s].x);
+    const float base = best == -INFINITY ? 0.f : best;
+    float total = 0.f, acc[N] = {};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[at + s];
+        const float scale = __builtin_amdgcn_exp2f(ml.x - base);
+        total += scale * ml.y;
+        const float* p = a.part_o + (at + s) * HD + l * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] += scale * p[i];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + l * N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) st1(dst + i, acc[i] * inv);
+    if (l == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+}
+
+// Attention weight per entry, added to the accumulated one: the scores are computed a second time (keys are half of the cache; storing a
+// group's probabilities would move as many bytes), now with the final sum of every row.  A wave owns chunks of 64 entries of one (sequence, kv head): no atomics, one order.
+template <typename T, int HD, int PLANES>
+__global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group, step = gridDim.y * 4 * KV4_CHUNK;
+    int slot0 = (blockIdx.y * 4 + wave) * KV4_CHUNK;
+    if (slot0 >= n || cols == 0) return;
+    const uint8_t* page[4];
+    int there, next;
+    Kv4Keys<HD> k, k1;
+    u32x4_t q[G][PLANES];
+    int limit;
+    float lse2;
+    auto column = [&](int c0) {
+        const int col = c0 + (lane & 15), r = col / a.group;
+        limit = col < cols ? n - (count - 1 - r) : 0;
+        lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : 0.f;
+        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
+    };
+    kv4_pages<HD>(a.c, b, head, slot0, page, there);
+    kv4_load_keys<HD>(page, lane, k);
+    column(0);
+    float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
+    for (; slot0 < n; slot0 += step) {
+        kv4_pages<HD>(a.c, b, head, slot0 + step, page, next);
+        kv4_load_keys<HD>(page, lane, k1);
+        // each of the 16 lanes of a quad keeps one of its 16 entries' sums: entry 4 p + i
+        const int slot = slot0 + (lane & 12) * 4 + quad * 4 + (lane & 3);
+        const bool there_l = slot < n && ((there >> ((lane & 15) >> 2)) & 1);
+        const float before = there_l ? scores[slot] : 0.f;
+        f32x4_t weight[4] = {};
+        for (int c0 = 0; c0 < cols; c0 += 16) {
+            if (cols > 16) column(c0);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q);
+                const int end = (there >> p) & 1 ? limit : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) weight[p][i] += slot0 + p * KV4_PAGE + quad * 4 + i < end ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.factor2, -lse2)) : 0.f;
+            }
+        }
+        float mine = 0.f;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = row16_sum(weight[p][i]);
+                mine = (lane & 15) == p * 4 + i ? w : mine;
+            }
+        if (there_l) scores[slot] = before + mine;
+        k = k1;
+        there = next;
+    }
 }
 
 // ---- eviction

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
@@ -118,18 +119,27 @@ void append_run(const rsd_kv4_cache* c, const void* k, int64_t k_row, int64_t k_
     else kv4_append_kernel<T, false><<<blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, kt, k_row, k_head, vt, v_row, v_head, seq, slot, position, rows, dev_book(book));
 }
 
-struct AttnPlan { int mt, tiles, split, splits; uint64_t o_bytes, ml_bytes, lse_bytes; };
+struct AttnPlan { int tiles, waves, split, splits; bool many; uint64_t o_bytes, ml_bytes, lse_bytes; };
 
+// Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
+//  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
+//  - one tile: eight waves to a block while (sequence, kv head) pairs are fewer than 512 (64 x 4: 35 us against 43 with four), else four (256 x 4: 186 against 197).
+//    With fewer than 128 pairs the entries are split for 512 of them, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six chunks); with more,
+//    down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
+//  - many columns: 768 blocks, three to a CU, parts of eight chunks at least (64 sequences, 8 rows: 79 us in 3 parts, 105 in one, 93 in 8).
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
     const int64_t max_kv = std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KV4_PAGE);
-    p.mt = cols <= 16 ? 1 : 2;
-    p.tiles = (int)ceil_div(cols, 16 * p.mt);
+    const int64_t chunks = std::max<int64_t>(1, ceil_div(max_kv, KV4_CHUNK));
+    p.many = cols > 32;
+    p.tiles = (int)ceil_div(cols, p.many ? 64 : 16);
     const int64_t base = (int64_t)c->batch * c->n_kv_heads * p.tiles;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(1024, base), ceil_div(max_kv, 256)));
-    p.split = (int)(ceil_div(ceil_div(std::max<int64_t>(max_kv, 1), want), 256) * 256);
-    p.splits = (int)std::max<int64_t>(1, ceil_div(max_kv, p.split));
+    p.waves = p.many ? 4 : (int)std::min<int64_t>(base < 512 ? 8 : 4, chunks);
+    const int64_t least = p.many ? 8 : (int64_t)p.waves * (base < 128 ? 2 : 6);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(p.many ? 768 : 512, base), chunks / least));
+    p.split = (int)(ceil_div(chunks, want) * KV4_CHUNK);
+    p.splits = (int)ceil_div(chunks * KV4_CHUNK, p.split);
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -149,14 +159,15 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
 }
 
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
-    const dim3 grid((unsigned)(k.c.batch * k.c.hkv * p.tiles), (unsigned)p.splits);
-    if (p.mt == 1) kv4_attn_kernel<T, HD, PLANES, 1><<<grid, 256, 0, st>>>(k);
-    else kv4_attn_kernel<T, HD, PLANES, 2><<<grid, 256, 0, st>>>(k);
+    const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
+    if (p.many) kv4_attn_many_kernel<T, HD, PLANES><<<grid, 256, 0, st>>>(k);
+    else kv4_attn_kernel<T, HD, PLANES><<<grid, 64 * p.waves, 0, st>>>(k);
     if (p.splits > 1)
-        kv4_join_kernel<T><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 4), 256, 0, st>>>(k, HD);
+        kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
     if (k.book.scores) {
         const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
-        if (n > 0) kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)(k.c.batch * k.c.hkv), (unsigned)ceil_div(n, 4 * KV4_CHUNK)), 256, 0, st>>>(k);
+        const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, blocks = std::min<int64_t>(ceil_div(n, 4 * KV4_CHUNK), ceil_div(1024, pairs));
+        if (n > 0) kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)(k.c.batch * k.c.hkv), (unsigned)blocks), 256, 0, st>>>(k);
     }
 }
 template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, hipStream_t st) {
@@ -270,10 +281,14 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.c = dev_cache(c);
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
     k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads, k.group = a->n_heads / c->n_kv_heads;
-    k.factor2 = (float)((double)a->scale * 1.4426950408889634);
+    k.factor2 = (float)(std::fabs((double)a->scale) * 1.4426950408889634);
+    k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse ? a->lse : scored ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
-    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.tiles = p.tiles;
+    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.hd = c->head_dim;
+    const int64_t vec = 16 / (int64_t)size_of(a->dtype);
+    k.q_wide = aligned(a->q, 16) && a->q_row % vec == 0 && a->q_head % vec == 0;
+    k.o_wide = aligned(a->out, 4 * size_of(a->dtype)) && a->out_row % 4 == 0 && a->out_head % 4 == 0;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);
