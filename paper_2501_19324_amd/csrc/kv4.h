@@ -713,8 +713,10 @@ struct Kv4Evict {
     Kv4Cache c;
     Kv4Book book;
     int budget, recent;
-    int* plan;              // [batch][hkv][2 + 2 * moves]: entries moved, entries before, targets, sources
+    int* plan;              // [batch][hkv]: entries moved, entries before, 0, 0; for each slot below the budget its rank among the freed ones
+                            // or -1; the kept slots above it in order (at most `moves`)
     int moves;
+    __host__ __device__ int64_t list_words() const { return 4 + (int64_t)((budget + 3) & ~3) + moves; }
 };
 // Scores as whole numbers of the same order; protected entries above all, NaN as -inf, both zeros alike
 __device__ __forceinline__ uint32_t kv4_rank_key(float score, bool safe) {
@@ -752,7 +754,8 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     __shared__ int hist[256], part[2][2][16], found[3], newest_w[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
-    int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
+    int* plan = a.plan + blockIdx.x * a.list_words();
+    int *place = plan + 4, *from = place + ((a.budget + 3) & ~3);
     const int n = min(max(a.c.kv_len[b], 0), a.c.max_pages * KV4_PAGE);
     if (tid == 0) plan[0] = 0, plan[1] = n;
     if (n <= a.budget) return;
@@ -831,52 +834,72 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     for (int s = s0; s < s1; ++s) {
         const uint32_t u = key_of(s);
         const bool keep = u > key || (u == key && rank++ < need);
-        if (s < a.budget && !keep) plan[2 + holes++] = s;
-        if (s >= a.budget && keep) plan[2 + a.moves + extras++] = s;
+        if (s < a.budget) place[s] = keep ? -1 : holes++;
+        else if (keep) from[extras++] = s;
     }
     if (tid == 0) plan[0] = all_a;
 }
 
-// The moves: 16 lanes take one entry, eight words of hd at a time, so that a wave has four entries' chains of latencies (plan, table, bytes) under way.
-// 64 sequences x 4 heads, 225000 moves: 96 us with a wave per entry and a byte per lane.
+// The moves, page by page of the target slots: a wave brings the new entries of a page together and writes its values back whole, because the
+// bytes of one token lie four apart.  64 sequences x 4 heads, 225000 moves: 24 us, 33 entry by entry with four byte stores to a lane, 30 with two pages
+// to a wave (fewer waves per SIMD); bound by the lines that it touches, about 150 MB through L2.
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int hkv) {
     constexpr int G = HD / 32;
     typedef typename u32vec<G>::type V;
-    const int l = threadIdx.x & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, quad = lane >> 4;
     const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
-    const int* plan = a.plan + (int64_t)blockIdx.x * (2 + 2 * (int64_t)a.moves);
+    const int* plan = a.plan + blockIdx.x * a.list_words();
+    const int *place = plan + 4, *from_list = place + ((a.budget + 3) & ~3);
     const int count = plan[0];
     if (blockIdx.y == 0 && h == 0 && threadIdx.x == 0) a.c.kv_len[b] = min(plan[1], a.budget);
+    if (count == 0) return;
     float* score = a.book.scores + b * a.book.score_b + h * a.book.score_h;
     int* pos = a.book.pos + b * a.book.pos_b + h * a.book.pos_h;
-    for (int i = blockIdx.y * 16 + (threadIdx.x >> 4); i < count; i += gridDim.y * 16) {
-        const int to = plan[2 + i], from = plan[2 + a.moves + i], t1 = to % KV4_PAGE, t0 = from % KV4_PAGE;
-        uint8_t* dst = kv4_page(a.c, HD, b, to / KV4_PAGE, h);
-        const uint8_t* src = kv4_page(a.c, HD, b, from / KV4_PAGE, h);
-        if (dst && src) {
-            // keys: HD/32 bytes at a time, of quarter l / 4
-            const int key = l / 4 * 2 * HD + l % 4 * G;
-            uint32_t k = 0;
-            if constexpr (G == 4) k = *reinterpret_cast<const uint32_t*>(src + key + t0 * (HD / 8));
-            else if constexpr (G == 2) k = *reinterpret_cast<const uint16_t*>(src + key + t0 * (HD / 8));
-            else k = src[key + t0 * (HD / 8)];
-            // values: lane l has the bytes of dim l of every group, among those of the four tokens of a quad
-            const V v = *reinterpret_cast<const V*>(src + 8 * HD + (t0 >> 2) * 2 * HD + l * (HD / 8));
-            uint32_t ks = 0, vs = 0, sc = 0;
-            int po = 0;
-            if (l < G) ks = src[kv4_key_scale_at(HD, t0, l)], vs = src[kv4_val_scale_at(HD, t0, l)];
-            if (l == 15) sc = __float_as_uint(score[from]), po = pos[from];
-            if constexpr (G == 4) *reinterpret_cast<uint32_t*>(dst + key + t1 * (HD / 8)) = k;
-            else if constexpr (G == 2) *reinterpret_cast<uint16_t*>(dst + key + t1 * (HD / 8)) = (uint16_t)k;
-            else dst[key + t1 * (HD / 8)] = (uint8_t)k;
-            uint8_t* d = dst + 8 * HD + (t1 >> 2) * 2 * HD + l * (HD / 8) + (t1 & 3);
-#pragma unroll
-            for (int g = 0; g < G; ++g) d[4 * g] = (uint8_t)(v[g] >> (8 * (t0 & 3)));
-            if (l < G) dst[kv4_key_scale_at(HD, t1, l)] = (uint8_t)ks, dst[kv4_val_scale_at(HD, t1, l)] = (uint8_t)vs;
-            if (l == 15) score[to] = __uint_as_float(sc), pos[to] = po;
-        } else if (l == 15) {
-            score[to] = score[from], pos[to] = pos[from];
+    for (int page = blockIdx.y * 4 + wave; page * KV4_PAGE < a.budget; page += gridDim.y * 4) {
+        // lane: token l of the page (for keys, scales, score and position), the same in every quad
+        const int to = page * KV4_PAGE + l, rank = to < a.budget ? place[to] : -1;
+        if (!__any(rank >= 0)) continue;
+        const int from = rank >= 0 ? from_list[rank] : -1;
+        uint8_t* dst = kv4_page(a.c, HD, b, page, h);
+        const uint8_t* src = from >= 0 ? kv4_page(a.c, HD, b, from / KV4_PAGE, h) : nullptr;
+        const int t0 = from >= 0 ? from % KV4_PAGE : 0;
+        if (quad == 0 && from >= 0) {
+            const float s = score[from];
+            const int p = pos[from];
+            score[to] = s;
+            pos[to] = p;
         }
+        const bool moved = src && dst;
+        if (!__any(moved)) continue;
+        V k = {}, v = {}, v0[4] = {};
+        int ks = 0, vs = 0, tv[4];
+        if (moved) {
+            k = reinterpret_cast<const V*>(src)[quad * 16 + t0];
+            if (quad < G) ks = src[kv4_key_scale_at(HD, t0, quad)], vs = src[kv4_val_scale_at(HD, t0, quad)];
+        }
+        // values: this lane holds dim l of every group for the tokens 4 quad + i; the sources' addresses come from the lanes of those tokens
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int who = quad * 4 + i;
+            const uint64_t at = moved ? reinterpret_cast<uint64_t>(src) : 0;
+            const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)at, who), hi = (uint32_t)__shfl((int)(uint32_t)(at >> 32), who);
+            const uint8_t* p = reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
+            const int t = __shfl(t0, who);
+            tv[i] = p ? t & 3 : -1;
+            if (p) v0[i] = reinterpret_cast<const V*>(p + 8 * HD)[(t >> 2) * 16 + l];
+        }
+        const bool writes = tv[0] >= 0 || tv[1] >= 0 || tv[2] >= 0 || tv[3] >= 0;
+        if (writes) v = reinterpret_cast<const V*>(dst + 8 * HD)[lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (tv[i] >= 0)
+#pragma unroll
+                for (int g = 0; g < G; ++g) v[g] = (v[g] & ~(255u << (8 * i))) | (((v0[i][g] >> (8 * tv[i])) & 255u) << (8 * i));
+        if (moved) {
+            reinterpret_cast<V*>(dst)[lane] = k;
+            if (quad < G) dst[kv4_key_scale_at(HD, l, quad)] = (uint8_t)ks, dst[kv4_val_scale_at(HD, l, quad)] = (uint8_t)vs;
+        }
+        if (writes) reinterpret_cast<V*>(dst + 8 * HD)[lane] = v;
     }
 }

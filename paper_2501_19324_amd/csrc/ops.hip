@@ -126,7 +126,7 @@ struct AttnPlan { int tiles, waves, split, splits; bool many; uint64_t o_bytes, 
 //  - one tile: eight waves to a block while (sequence, kv head) pairs are fewer than 512 (64 x 4: 35 us against 43 with four), else four (256 x 4: 186 against 197).
 //    With fewer than 128 pairs the entries are split for 512 of them, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six chunks); with more,
 //    down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
-//  - many columns: 768 blocks, three to a CU, parts of eight chunks at least (64 sequences, 8 rows: 79 us in 3 parts, 105 in one, 93 in 8).
+//  - many columns: up to 1024 blocks, parts of eight chunks at least (64 sequences x 4 kv heads, 8 rows, bf16: 105 us in two parts, 79 in four, 94 in eight).
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
@@ -137,7 +137,7 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     const int64_t base = (int64_t)c->batch * c->n_kv_heads * p.tiles;
     p.waves = p.many ? 4 : (int)std::min<int64_t>(base < 512 ? 8 : 4, chunks);
     const int64_t least = p.many ? 8 : (int64_t)p.waves * (base < 128 ? 2 : 6);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(p.many ? 768 : 512, base), chunks / least));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.many ? 1024 / base : ceil_div(512, base), chunks / least));
     p.split = (int)(ceil_div(chunks, want) * KV4_CHUNK);
     p.splits = (int)ceil_div(chunks * KV4_CHUNK, p.split);
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
@@ -175,8 +175,10 @@ template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan
     else if (hd == 64) attn_run<T, 64, PLANES>(k, p, st);
     else attn_run<T, 128, PLANES>(k, p, st);
 }
+uint64_t up4(uint64_t n) { return (n + 3) & ~3ull; }
+// the most entries of a list that can move, in whole vectors
 int evict_moves(const rsd_kv4_cache* c, int budget) {
-    return (int)std::max<int64_t>(0, std::min<int64_t>(budget, (int64_t)c->max_pages * KV4_PAGE - budget));
+    return (int)up4(std::max<int64_t>(0, std::min<int64_t>(budget, (int64_t)c->max_pages * KV4_PAGE - budget)));
 }
 
 }  // namespace
@@ -300,7 +302,7 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
 
 extern "C" uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache* c, int32_t budget) {
     if (check_cache(c, "evict") || budget < 1) return 0;
-    return up256((uint64_t)c->batch * c->n_kv_heads * (2 + 2 * (uint64_t)evict_moves(c, budget)) * 4);
+    return up256((uint64_t)c->batch * c->n_kv_heads * (4 + (uint64_t)up4(budget) + evict_moves(c, budget)) * 4);
 }
 
 extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, int32_t budget, int32_t recent, void* workspace,
@@ -319,8 +321,8 @@ extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, i
     const int64_t slots = (int64_t)c->max_pages * KV4_PAGE;
     if (slots <= 16384) kv4_select_kernel<true><<<lists, 1024, (size_t)slots * 4, st>>>(e, c->n_kv_heads);
     else kv4_select_kernel<false><<<lists, 1024, 0, st>>>(e, c->n_kv_heads);
-    // 16 moves to a block at a time; at most 64 blocks to a list, which then go on with the next 1024
-    const dim3 grid(lists, (unsigned)std::min<int64_t>(64, ceil_div(e.moves, 16)));
+    // four pages to a block at a time; at most 64 blocks to a list, which then go on with the next 256
+    const dim3 grid(lists, (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(budget, KV4_PAGE), 4)));
     if (c->head_dim == 32) kv4_move_kernel<32><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
     else if (c->head_dim == 64) kv4_move_kernel<64><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
     else kv4_move_kernel<128><<<grid, 256, 0, st>>>(e, c->n_kv_heads);

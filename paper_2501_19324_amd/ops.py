@@ -197,16 +197,17 @@ def _evict_bytes(n_pages, kv_heads, hd, batch, max_pages, budget) -> int:
 
 def _cache(c) -> Tuple[_Cache, torch.Tensor, int]:
     pool, table, kv_len = c
-    if pool.dtype != _u8 or pool.dim() != 3 or pool.shape[2] % 17 or not pool.is_contiguous():
-        _bad(f"cache: the pool is {pool.dtype} {tuple(pool.shape)}, needed uint8 [pages, kv heads, 17 * head_dim], contiguous")
-    if table.dim() != 2:
-        _bad(f"cache: the table has shape {tuple(table.shape)}, needed [batch, pages]")
-    batch, max_pages = table.shape
     st = _stream(pool)
-    tp = _flat("cache table", table, pool, _i32, (batch, max_pages))
-    lp = _flat("cache kv_len", kv_len, pool, _i32, (batch,))
-    n, h, b = pool.shape
-    return _Cache(pool.data_ptr(), tp, lp, n, h, b // 17, batch, max_pages), pool, st
+    shape, dev = pool.shape, pool.device
+    if pool.dtype is not _u8 or len(shape) != 3 or shape[2] % 17 or not pool.is_contiguous():
+        _bad(f"cache: the pool is {pool.dtype} {tuple(shape)}, needed uint8 [pages, kv heads, 17 * head_dim], contiguous")
+    n, h, b = shape
+    if table.dtype is not _i32 or table.device != dev or table.dim() != 2 or not table.is_contiguous():
+        _bad(f"cache: the table is {table.dtype} {tuple(table.shape)} on {table.device}, needed int32 [batch, pages] on {dev}, contiguous")
+    batch, max_pages = table.shape
+    if kv_len.dtype is not _i32 or kv_len.device != dev or kv_len.shape != (batch,) or not kv_len.is_contiguous():
+        _bad(f"cache: kv_len is {kv_len.dtype} {tuple(kv_len.shape)} on {kv_len.device}, needed int32 [{batch}] on {dev}, contiguous")
+    return _Cache(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n, h, b // 17, batch, max_pages), pool, st
 
 
 def _rows3(name: str, t: torch.Tensor, like: torch.Tensor, heads: Optional[int], hd: int) -> Tuple[int, int, int]:
