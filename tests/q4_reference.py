@@ -12,9 +12,11 @@ def quantize(x):
     g = np.where(bad[..., None], 0.0, g)
     amax = np.abs(g).max(-1)
     e = np.full(amax.shape, -125)
-    for i in np.ndindex(amax.shape):
-        while e[i] < 125 and amax[i] > np.ldexp(7.0, int(e[i])):
-            e[i] += 1
+    while True:
+        more = (e < 125) & (amax > np.ldexp(7.0, e))
+        if not more.any():
+            break
+        e = e + more
     m = np.minimum(np.abs(g) / np.ldexp(1.0, e)[..., None], 6.0)
     code = np.zeros(g.shape, np.int64)
     for j in range(7):                                     # past the midpoint, or on it when the upper code is the even one

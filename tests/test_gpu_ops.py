@@ -110,7 +110,8 @@ def linear_bound(x, w, k, dtype, y):
 
 
 LINEAR = [(1, 1, 1), (1, 16, 32), (1, 17, 33), (2, 15, 128), (3, 64, 129), (7, 100, 512), (1, 300, 1536), (16, 33, 513), (17, 48, 640), (31, 20, 1100), (32, 64, 2048),
-          (33, 70, 300), (64, 129, 260), (65, 31, 1536), (100, 40, 96), (128, 256, 384), (130, 33, 700), (257, 17, 130), (1, 40, 9000), (5, 5000, 70), (70, 2100, 1000)]
+          (33, 70, 300), (64, 129, 260), (65, 31, 1536), (100, 40, 96), (128, 256, 384), (130, 33, 700), (257, 17, 130), (1, 40, 9000), (5, 5000, 70), (70, 2100, 1000),
+          (20, 101, 5000), (40, 50, 2100), (6, 37, 2600), (12, 2050, 2200), (66, 18, 6200), (100, 600, 520)]
 
 
 @pytest.mark.parametrize("rows,n,k", LINEAR)
@@ -304,13 +305,18 @@ ATTENTION = [  # heads, kv heads, head dim, lengths, rows of each sequence (None
     (64, 8, 128, [90], None),
     (20, 1, 128, [70, 33], None),                          # more heads than columns of a tile
     (40, 1, 32, [50], None),
-    (7, 1, 128, [1100, 20], None),                         # long enough to be split
+    (7, 1, 128, [1100, 20], None),
+    (7, 1, 128, [2300, 20, 1030], None),                   # long enough to be split
+    (4, 2, 32, [2100], [3]),
     (4, 2, 32, [20, 64, 5, 0, 90], [3, 1, 5, 0, 17]),
     (12, 2, 128, [40, 100, 16], [5, 33, 16]),              # a sequence that consists of its rows alone
     (28, 4, 128, [300, 65], [9, 2]),
     (9, 3, 64, [70, 7, 130], [8, 7, 1]),
     (16, 16, 64, [80], [40]),
     (8, 1, 128, [700, 66], [20, 3]),
+    (8, 1, 128, [1100, 90], [20, 90]),                     # many columns, split; a whole prompt
+    (9, 3, 64, [1090, 0, 33], [30, 0, 12]),
+    (3, 1, 32, [1300], [40]),
     (6, 2, 64, [5, 3], [9, 4]),                            # more rows than entries: the first ones see nothing
 ]
 
@@ -376,12 +382,13 @@ def test_pages_outside_the_pool_are_not_seen(torch, R, rows):
 
 
 @pytest.mark.parametrize("hd", [32, 64, 128])
-def test_nan_entries_reach_only_what_sees_them(torch, R, hd):
+@pytest.mark.parametrize("rows", [5, 12, 40])
+def test_nan_entries_reach_only_what_sees_them(torch, R, hd, rows):
     """A value group that reads as NaN: its 32 dims of the rows that see the entry; a key group: those rows whole."""
     rng = np.random.default_rng(hd)
-    n, rows, heads = 90, 12, 6
+    n, heads = 90, 6
     cache, pool, table = make_cache(torch, R, rng, [n], 2, hd)
-    for what, slot in (("v", 85), ("k", 83)):
+    for what, slot in (("v", 85), ("k", 83), ("v", 88), ("v", 89), ("v", 20)):
         mine = pool.copy()
         place = ref.entry_places(hd, slot % 16)
         mine[table[0, slot // 16], 1, place[3 if what == "v" else 2][0]] = 255
