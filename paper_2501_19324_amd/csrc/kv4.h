@@ -615,13 +615,14 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
         kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum);
 }
 
-// Joins the parts of the entries: 16 lanes per (row, head), HD/16 dims each.
+// Joins the parts of the entries: 16 lanes per (row, head), HD/16 dims each.  The lanes read 16 parts' maxima and sums at once (one after the other they
+// were a chain of latencies, 6 us for a handful of rows).
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     constexpr int N = HD / 16;
     const int l = threadIdx.x & 15;
     const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    if (id >= (int64_t)a.c.batch * a.max_rows * a.heads) return;
+    if (id >= (int64_t)a.c.batch * a.max_rows * a.heads) return;        // 16 lanes leave together
     const int qh = (int)(id % a.heads), r = (int)(id / a.heads % a.max_rows), b = (int)(id / a.heads / a.max_rows);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
@@ -629,18 +630,27 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     // the blocks of this column wrote a part for every split (an empty one where there was nothing to see)
     const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;
     float best = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) best = fmaxf(best, a.part_ml[at + s].x);
+    for (int s = l; s < a.splits; s += 16) best = fmaxf(best, a.part_ml[at + s].x);
+    best = row16_max(best);
     const float base = best == -INFINITY ? 0.f : best;
     float total = 0.f, acc[N] = {};
+    for (int s0 = 0; s0 < a.splits; s0 += 16) {
+        float scale = 0.f;
+        if (s0 + l < a.splits) {
+            const float2 ml = a.part_ml[at + s0 + l];
+            scale = __builtin_amdgcn_exp2f(ml.x - base);
+            total += scale * ml.y;
+        }
+        const int m = min(16, a.splits - s0);
+        const float* p = a.part_o + (at + s0) * HD + l * N;
 #pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = a.part_ml[at + s];
-        const float scale = __builtin_amdgcn_exp2f(ml.x - base);
-        total += scale * ml.y;
-        const float* p = a.part_o + (at + s) * HD + l * N;
+        for (int s = 0; s < m; ++s) {
+            const float w = __shfl(scale, s, 16);
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] += scale * p[i];
+            for (int i = 0; i < N; ++i) acc[i] += w * p[s * HD + i];
+        }
     }
+    total = row16_sum(total);
     const float inv = total == 0.f ? 0.f : 1.f / total;
     T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + l * N;
 #pragma unroll

@@ -78,7 +78,7 @@ template <typename T, bool VEC> void w4_launch(const W4Plan& p, const W4Args& a,
         else w4_few_kernel<T, 2, 4, VEC><<<grid, threads, 0, st>>>(a);
         return;
     }
-    const dim3 grid((unsigned)p.splits, (unsigned)ceil_div(p.nt, 16), (unsigned)ceil_div(a.rows, p.xt * 16));
+    const unsigned grid = (unsigned)(p.splits * ceil_div(p.nt, 16) * ceil_div(a.rows, p.xt * 16));
     if (p.xt == 1) w4_many_kernel<T, 1, VEC><<<grid, 256, 0, st>>>(a);
     else if (p.xt == 2) w4_many_kernel<T, 2, VEC><<<grid, 256, 0, st>>>(a);
     else if constexpr (sizeof(T) == 2) w4_many_kernel<T, 4, VEC><<<grid, 256, 0, st>>>(a);
@@ -88,7 +88,7 @@ template <typename T> void w4_run(const W4Plan& p, const W4Args& a, hipStream_t 
     if (vec) w4_launch<T, true>(p, a, st);
     else w4_launch<T, false>(p, a, st);
     if (p.splits > 1)
-        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, st>>>(a, p.splits);
+        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, st>>>(a);
 }
 
 // ---- the cache
@@ -222,7 +222,7 @@ extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* 
         return fail(RSD_EINVAL, "w4_linear: the workspace holds %llu of %llu bytes, or is not 256-byte aligned",
                     (unsigned long long)workspace_bytes, (unsigned long long)p.part_bytes);
     const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks, x, ldx, rows, y, ldy,
-                   p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles,
+                   p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles, p.splits,
                    aligned(y, 4 * size_of(dtype)) && ldy % 4 == 0};
     Launches l;
     if (dtype == RSD_F32) w4_run<float>(p, a, static_cast<hipStream_t>(hip_stream));

@@ -17,7 +17,7 @@ struct W4Args {
     void* y;
     int64_t ldy;
     float* part;        // partial sums [split][rows][n], null: the block writes y
-    int tiles;          // tiles of 128 columns per split
+    int tiles, splits;  // tiles of 128 columns per split
     bool y_wide;        // rows of y start on multiples of four values
 };
 template <typename T> constexpr int w4_planes = sizeof(T) == 4 ? 3 : 1;
@@ -99,9 +99,8 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
     __shared__ u32x4_t lds[WAVES * (P * PLANE > NT * 64 ? P * PLANE : NT * 64)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int n0 = blockIdx.x * NT;
-    // the block's tiles of columns, dealt to the waves in runs
-    const int b0 = blockIdx.y * a.tiles, count = min(a.kt - b0, a.tiles);
-    const int t0 = b0 + count * wave / waves, t1 = b0 + count * (wave + 1) / waves;
+    // the tiles of columns, dealt to the waves in runs
+    const int t0 = (int)((int64_t)a.kt * wave / waves), t1 = (int)((int64_t)a.kt * (wave + 1) / waves);
     u32x4_t* stage = lds + wave * P * PLANE;                // [plane][j][q][row]
     const T* row[XL];
 #pragma unroll
@@ -151,7 +150,7 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
     for (int i = wave; i < NT; i += waves) {
         f32x4_t s = sums[i * 64 + lane];
         for (int v = 1; v < waves; ++v) s += sums[(v * NT + i) * 64 + lane];
-        w4_store<T>(a, blockIdx.y, lane & 15, (n0 + i) * 16 + (lane >> 4) * 4, s);
+        w4_store<T>(a, 0, lane & 15, (n0 + i) * 16 + (lane >> 4) * 4, s);
     }
 }
 
@@ -161,16 +160,19 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
 //  - Loads run three tiles ahead: a tile is 0.4 us of matrix work, less than a load takes.
 //  - 16 lanes load 256 consecutive bytes of one row of x (with 16 rows x 64 bytes the loads of x alone took 22 of 51 us at 64 rows of the 7B gate and up product).
 //    They write to 16 different operands: slot r of operand (j, q) is kept at r ^ (4 q + j), or all of them would hit the same banks.
-//  - Splits are the fastest index of the grid: with eight of them an XCD's L2 sees one part of x (256 rows, 7B down: 90 -> 70 us).
-// Bound by the issue of a single wave per SIMD: a product takes 25 clocks instead of 16 with the conversions, LDS operands and loads between.  256 rows,
-// 3584 x 18944: 44 us, 790 TFLOP/s, and 5 us for the sums.
+//  - Splits are the fastest index of the grid: with eight of them an XCD's L2 sees one part of x (256 rows, 7B down: 90 -> 70 us).  Then come the blocks of rows
+//    of x, which share their weights (256 rows, 7B gate and up: 99 -> 80 us).
+// 256 rows, 3584 x 18944: 45 us, 770 TFLOP/s, and 5 us for the sums; 37888 x 3584: 80 us, 870 TFLOP/s.  A plain bf16 product of 8192^3 reaches 1220 here.  Bound by
+// the products and the reads of LDS in turn: a wave takes 25 clocks for a product instead of 16, at the 1.8 GHz that such a load leaves; a second block per CU
+// changes little, reading the operands of a group ahead or twice the rows of W per wave nothing.
 template <typename T, int XT, bool VEC>
 __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
     constexpr int P = w4_planes<T>, NT = 4, DW = 4, DX = 4;
     __shared__ u32x4_t lds[2][P][XT * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = (blockIdx.y * 4 + wave) * NT, r0 = blockIdx.z * XT * 16;
-    const int t0 = blockIdx.x * a.tiles, t1 = min(a.kt, t0 + a.tiles);
+    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, row_blocks = (a.rows + XT * 16 - 1) / (XT * 16);
+    const int n0 = (rest / row_blocks * 4 + wave) * NT, r0 = rest % row_blocks * XT * 16;
+    const int t0 = split * a.tiles, t1 = min(a.kt, t0 + a.tiles);
     f32x4_t acc[NT][XT] = {};
     u32x4_t w[DW][NT];
     uint32_t scale[2][NT];
@@ -256,19 +258,19 @@ __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int e = 0; e < XT; ++e) w4_store<T>(a, blockIdx.x, r0 + e * 16 + (lane & 15), (n0 + i) * 16 + (lane >> 4) * 4, acc[i][e]);
+        for (int e = 0; e < XT; ++e) w4_store<T>(a, split, r0 + e * 16 + (lane & 15), (n0 + i) * 16 + (lane >> 4) * 4, acc[i][e]);
 }
 
 // the splits' sums, in order; four results to a thread
 template <typename T>
-__global__ __launch_bounds__(256) void w4_sum_kernel(W4Args a, int splits) {
+__global__ __launch_bounds__(256) void w4_sum_kernel(W4Args a) {
     const int quads = w4_padded(a.n) / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)a.rows * quads;
     if (id >= total) return;
     const f32x4_t* part = reinterpret_cast<const f32x4_t*>(a.part) + id;
     f32x4_t s = part[0];
 #pragma unroll 4
-    for (int i = 1; i < splits; ++i) s += part[i * total];
+    for (int i = 1; i < a.splits; ++i) s += part[i * total];
     W4Args y = a;
     y.part = nullptr;
     w4_store<T>(y, 0, (int)(id / quads), (int)(id % quads) * 4, s);
