@@ -390,13 +390,61 @@ template <int PP> __device__ __forceinline__ void kv4_weights(const f32x4_t s0, 
     }
 }
 
+// Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: lse2 is their logarithm to the base 2, +inf for a
+// column that does not exist.  WHOLE: every column sees every entry.
+template <int HD, int PLANES>
+__device__ __forceinline__ void kv4_add_weights(const Kv4Keys<HD>& k, const u32x4_t q[HD / 32][PLANES], bool whole, int there, int slot0, int limit, float factor2,
+                                                float lse2, f32x4_t weight[4]) {
+    const int quad = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q);
+        f32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor2, -lse2));
+        if (!whole) {
+            const int end = (there >> p) & 1 ? limit : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = slot0 + p * KV4_PAGE + quad * 4 + i < end ? w[i] : 0.f;
+        }
+        weight[p] += w;
+    }
+}
+// Each of the 16 lanes of a quad keeps one of its 16 entries: entry 4 p + i.  Its place among the scores, or -1
+__device__ __forceinline__ int kv4_score_slot(int slot0, int n, int there) {
+    const int lane = threadIdx.x & 63, slot = slot0 + (lane & 12) * 4 + (lane >> 4) * 4 + (lane & 3);
+    return slot < n && ((there >> ((lane & 15) >> 2)) & 1) ? slot : -1;
+}
+// One step of the sum over 16 lanes of 2 N values each: lanes whose numbers differ in a bit (CTRL pairs them) keep N values each and give the other N away
+template <int CTRL, int N> __device__ __forceinline__ void kv4_halve(float v[16], bool upper) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float keep = upper ? v[j + N] : v[j], give = upper ? v[j] : v[j + N];
+        v[j] = keep + __uint_as_float(dpp_move<CTRL>(__float_as_uint(give)));
+    }
+}
+// sum over the 16 columns of each entry, for the lane that keeps it: 15 additions instead of the 64 of a sum of every entry for every lane
+__device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
+    const int l = threadIdx.x;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = weight[e / 4][e % 4];
+    kv4_halve<0x140, 8>(v, l & 8);       // row_mirror: the lane 15 - l
+    kv4_halve<0x141, 4>(v, l & 4);       // row_half_mirror: 7 - l of its half
+    kv4_halve<0x4E, 2>(v, l & 2);        // quad_perm [2,3,0,1]
+    kv4_halve<0xB1, 1>(v, l & 1);        // quad_perm [1,0,3,2]
+    return v[0];
+}
+
 // Few columns (single tokens, verification of a few): a block owns a tile of 16 columns of one (sequence, kv head) and one part of its entries, of which
 // its waves take chunks of 64 in turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's bytes are requested before
 // this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (28 columns, 64 sequences: 62 us against 78 with
 // both tiles in one wave's registers).
 // 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 186 us, 4.6 TB/s, of the 4.9 that a copy reaches; 519 vector and 48 matrix instructions per chunk
 // keep a SIMD busy for two thirds of that.  Without the requests ahead 190 us, with them dropped for a third wave per SIMD 198.
-template <typename T, int HD, int PLANES>
+// SCORED: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
+// once more (64 sequences of 128 .. 5120 entries: 51 us instead of 56 in two launches; 256 blocks, so the longest sequence decides).
+template <typename T, int HD, int PLANES, bool SCORED>
 __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, WAVES = 8;
     __shared__ __align__(16) float lds_o[WAVES][G * 2][64][4];
@@ -490,6 +538,30 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
         if (col < cols) kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total);
+    }
+    if constexpr (SCORED) {
+        float best = -INFINITY, total = 0.f;
+        for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][lane & 15]);
+        const float base = best == -INFINITY ? 0.f : best;
+        for (int w = 0; w < waves; ++w) total += __builtin_amdgcn_exp2f(lds_ml[w][0][lane & 15] - base) * lds_ml[w][1][lane & 15];
+        const float lse2 = col < cols ? base + log2f(total) : INFINITY;
+        float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
+        slot0 = begin + wave * KV4_CHUNK;
+        kv4_pages<HD>(a.c, b, head, slot0, page[0], there[0]);
+        kv4_load_keys<HD>(page[0], lane, k[0]);
+        kv4_pages<HD>(a.c, b, head, slot0 + step, page[1], there[1]);
+        for (; slot0 < end; slot0 += step) {
+            kv4_load_keys<HD>(page[1], lane, k[1]);
+            const int slot = kv4_score_slot(slot0, end, there[0]), there1 = there[1];
+            const float before = slot >= 0 ? scores[slot] : 0.f;
+            kv4_pages<HD>(a.c, b, head, slot0 + 2 * step, page[1], there[1]);
+            f32x4_t weight[4] = {};
+            kv4_add_weights<HD, PLANES>(k[0], q, slot0 + KV4_CHUNK <= safe && there[0] == 15, there[0], slot0, limit, a.factor2, lse2, weight);
+            const float sum_ = kv4_sum_weights(weight);
+            if (slot >= 0) scores[slot] = before + sum_;
+            k[0] = k[1];
+            there[0] = there1;
+        }
     }
 }
 
@@ -643,7 +715,6 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
         }
         const int m = min(16, a.splits - s0);
         const float* p = a.part_o + (at + s0) * HD + l * N;
-#pragma unroll 4
         for (int s = 0; s < m; ++s) {
             const float w = __shfl(scale, s, 16);
 #pragma unroll
@@ -668,6 +739,7 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
     const int cols = count * a.group, step = gridDim.y * 4 * KV4_CHUNK;
+    const int safe = n - (count - 1);                       // every row sees the slots below
     int slot0 = (blockIdx.y * 4 + wave) * KV4_CHUNK;
     if (slot0 >= n || cols == 0) return;
     const uint8_t* page[4];
@@ -679,7 +751,7 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     auto column = [&](int c0) {
         const int col = c0 + (lane & 15), r = col / a.group;
         limit = col < cols ? n - (count - 1 - r) : 0;
-        lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : 0.f;
+        lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : INFINITY;
         kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
     };
     kv4_pages<HD>(a.c, b, head, slot0, page, there);
@@ -689,30 +761,15 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     for (; slot0 < n; slot0 += step) {
         kv4_pages<HD>(a.c, b, head, slot0 + step, page, next);
         kv4_load_keys<HD>(page, lane, k1);
-        // each of the 16 lanes of a quad keeps one of its 16 entries' sums: entry 4 p + i
-        const int slot = slot0 + (lane & 12) * 4 + quad * 4 + (lane & 3);
-        const bool there_l = slot < n && ((there >> ((lane & 15) >> 2)) & 1);
-        const float before = there_l ? scores[slot] : 0.f;
+        const int slot = kv4_score_slot(slot0, n, there);
+        const float before = slot >= 0 ? scores[slot] : 0.f;
         f32x4_t weight[4] = {};
         for (int c0 = 0; c0 < cols; c0 += 16) {
             if (cols > 16) column(c0);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q);
-                const int end = (there >> p) & 1 ? limit : 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) weight[p][i] += slot0 + p * KV4_PAGE + quad * 4 + i < end ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.factor2, -lse2)) : 0.f;
-            }
+            kv4_add_weights<HD, PLANES>(k, q, slot0 + KV4_CHUNK <= safe && there == 15, there, slot0, limit, a.factor2, lse2, weight);
         }
-        float mine = 0.f;
-#pragma unroll
-        for (int p = 0; p < 4; ++p)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = row16_sum(weight[p][i]);
-                mine = (lane & 15) == p * 4 + i ? w : mine;
-            }
-        if (there_l) scores[slot] = before + mine;
+        const float mine = kv4_sum_weights(weight);
+        if (slot >= 0) scores[slot] = before + mine;
         k = k1;
         there = next;
     }

@@ -160,11 +160,13 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
 
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
     const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
+    const bool fused = k.book.scores && !p.many && p.tiles == 1 && p.splits == 1;
     if (p.many) kv4_attn_many_kernel<T, HD, PLANES><<<grid, 256, 0, st>>>(k);
-    else kv4_attn_kernel<T, HD, PLANES><<<grid, 64 * p.waves, 0, st>>>(k);
+    else if (fused) kv4_attn_kernel<T, HD, PLANES, true><<<grid, 64 * p.waves, 0, st>>>(k);
+    else kv4_attn_kernel<T, HD, PLANES, false><<<grid, 64 * p.waves, 0, st>>>(k);
     if (p.splits > 1)
         kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
-    if (k.book.scores) {
+    if (k.book.scores && !fused) {
         const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
         const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, blocks = std::min<int64_t>(ceil_div(n, 4 * KV4_CHUNK), ceil_div(1024, pairs));
         if (n > 0) kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)(k.c.batch * k.c.hkv), (unsigned)blocks), 256, 0, st>>>(k);
