@@ -131,7 +131,7 @@ def _flat(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape) -> int:
 def _workspace(nbytes: int, like: torch.Tensor) -> Tuple[Optional[torch.Tensor], Optional[int]]:
     if not nbytes:
         return None, None
-    w = like.new_empty(nbytes, dtype=_u8)
+    w = like.new_empty(nbytes, dtype=_u8) if like.dtype is not _u8 else like.new_empty(nbytes)
     return w, w.data_ptr()
 
 
@@ -218,21 +218,20 @@ def _rows3(name: str, t: torch.Tensor, like: torch.Tensor, heads: Optional[int],
     return t.data_ptr(), stride[0], stride[1]
 
 
+def _entries(name: str, t: torch.Tensor, c: _Cache, pool, dtype) -> Tuple[int, int, int]:
+    """Address and strides of a [batch, n_kv_heads, slots] tensor."""
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is not dtype or t.device != pool.device or len(shape) != 3 or shape[0] != c.batch or shape[1] != c.n_kv_heads
+            or shape[2] < c.max_pages * PAGE or stride[2] != 1):
+        _bad(f"{name}: {t.dtype} {tuple(shape)} on {t.device}, strides {stride}; needed {dtype} [{c.batch}, {c.n_kv_heads}, {c.max_pages * PAGE} or more], "
+             f"contiguous in the slots, on {pool.device}")
+    return t.data_ptr(), stride[0], stride[1]
+
+
 def _book(c: _Cache, pool, scores, entry_pos) -> _Book:
-    book = _Book()
-    need = (c.batch, c.n_kv_heads)
-    for name, t, dtype in (("scores", scores, _f32), ("entry_pos", entry_pos, _i32)):
-        if t is None:
-            continue
-        _on(name, t, pool, dtype)
-        shape, stride = t.shape, t.stride()
-        if len(shape) != 3 or shape[:2] != need or shape[2] < c.max_pages * PAGE or stride[2] != 1:
-            _bad(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, needed {need + (c.max_pages * PAGE,)} or more slots, contiguous in them")
-        if t is scores:
-            book.scores, book.score_b, book.score_h = t.data_ptr(), stride[0], stride[1]
-        else:
-            book.positions, book.position_b, book.position_h = t.data_ptr(), stride[0], stride[1]
-    return book
+    sp, sb, sh = (None, 0, 0) if scores is None else _entries("scores", scores, c, pool, _f32)
+    pp, pb, ph = (None, 0, 0) if entry_pos is None else _entries("entry_pos", entry_pos, c, pool, _i32)
+    return _Book(sp, pp, sb, sh, pb, ph)
 
 
 def rsd_kv4_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, slot: torch.Tensor, position: Optional[torch.Tensor] = None,
@@ -315,7 +314,7 @@ def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Option
         max_kv = cap if max_kv is None else min(int(max_kv), cap)
         nbytes = _attn_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, rows, max_rows, heads, max_kv, t, rp is not None, want_lse,
                              scores is not None)
-        ws, wp = _workspace(nbytes, q)
+        ws, wp = _workspace(nbytes, pool)
         a = _Attn(qp, op, lse.data_ptr() if want_lse else None, qr, qh, orow, oh, rp, rows, max_rows, heads, max_kv, t, scale)
         book = None if scores is None else C.byref(_book(c, pool, scores, None))
         _done(lib.rsd_kv4_attention(C.byref(c), C.byref(a), book, wp, nbytes, st), lib)
