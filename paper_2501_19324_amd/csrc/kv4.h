@@ -37,25 +37,22 @@ struct Kv4Book {            // per entry: accumulated attention weight, position
     int64_t score_b, score_h, pos_b, pos_h;
 };
 
-// four consecutive values as they lie in memory; ALIGNED: the address is a multiple of their size together
-template <bool ALIGNED> __device__ __forceinline__ void kv4_load4(const float* p, float o[4]) {
-    if constexpr (ALIGNED) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
-    } else {
+// consecutive values at any address
+__device__ __forceinline__ void kv4_load4(const float* p, float o[4]) {
+    const f32x4_t v = *reinterpret_cast<const f32x4_any_t*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = p[i];
-    }
+    for (int i = 0; i < 4; ++i) o[i] = v[i];
 }
-template <bool ALIGNED> __device__ __forceinline__ void kv4_load4(const bf16_t* p, float o[4]) {
-    if constexpr (ALIGNED) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xFFFF0000u);
-        o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xFFFF0000u);
-    } else {
+__device__ __forceinline__ void kv4_load4(const bf16_t* p, float o[4]) {
+    const u32x2_t v = *reinterpret_cast<const u32x2_any_t*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = ld1(p + i);
-    }
+    for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
+}
+__device__ __forceinline__ void kv4_load8(const float* p, float o[8]) { kv4_load4(p, o); kv4_load4(p + 4, o + 4); }
+__device__ __forceinline__ void kv4_load8(const bf16_t* p, float o[8]) {
+    const u32x4_t v = *reinterpret_cast<const u32x4_any_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
 }
 // scale byte and codes of a group of 32 held by four neighbouring lanes, eight values each: x[i], x[i + 4] share byte i where PAIRED,
 // x[2 i], x[2 i + 1] otherwise
@@ -80,7 +77,7 @@ template <bool PAIRED> __device__ __forceinline__ uint32_t kv4_encode8(const flo
 // ---- entries in: four lanes take one group of 32 dims of one (row, head), keys and values.  What a lane has to wait for in turn (row numbers,
 // then the table, then the stores) is a chain of latencies: keys and values are requested before it, eight of each to a lane.
 // 7936 rows of 8 heads in fp32 (75 MB): 37 us with two values to a lane, requested behind the chain.
-template <typename T, bool ALIGNED>
+template <typename T>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int hd, const T* __restrict__ k, int64_t k_row, int64_t k_head, const T* __restrict__ v,
                                                          int64_t v_row, int64_t v_head, const int* __restrict__ seq, const int* __restrict__ slot,
                                                          const int* __restrict__ position, int rows, Kv4Book book) {
@@ -92,10 +89,10 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int hd, con
     const T* kr = k + row * k_row + h * k_head + g * 32 + 8 * l;
     const T* vr = v + row * v_row + h * v_head + g * 32 + 4 * l;
     float kx[8], vx[8];
-    kv4_load4<ALIGNED>(kr, kx);
-    kv4_load4<ALIGNED>(kr + 4, kx + 4);
-    kv4_load4<ALIGNED>(vr, vx);
-    kv4_load4<ALIGNED>(vr + 16, vx + 4);
+    kv4_load4(kr, kx);
+    kv4_load4(kr + 4, kx + 4);
+    kv4_load4(vr, vx);
+    kv4_load4(vr + 16, vx + 4);
     if ((unsigned)b >= (unsigned)c.batch || (unsigned)s >= (unsigned)c.max_pages * KV4_PAGE) return;
     uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
     if (!block) return;
@@ -159,7 +156,6 @@ struct Kv4Attn {
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
     int max_kv, split, splits, hd;
-    bool q_wide, o_wide;    // rows and heads of q start on multiples of 16 bytes, of out on multiples of four values
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
     Kv4Book book;
@@ -212,15 +208,8 @@ __device__ __forceinline__ void kv4_load_q(const Kv4Attn& a, int r0, int count, 
     // a column beyond the rows repeats the last one; its results are not used
     const T* p = static_cast<const T*>(a.q) + (int64_t)(r0 + min(r, count - 1)) * a.q_row + (int64_t)(head * a.group + g) * a.q_head + (lane >> 4) * (HD / 4);
     float x[HD / 32][8];
-    if (a.q_wide) {
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) load8(p + j * 8, x[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < HD / 32; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[j][i] = ld1(p + j * 8 + i);
-    }
+    for (int j = 0; j < HD / 32; ++j) kv4_load8(p + j * 8, x[j]);
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) {
         if (a.negative)
@@ -322,13 +311,8 @@ __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
-    if (a.o_wide) {
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv));
-        else *reinterpret_cast<f32x4_t*>(dst) = acc * inv;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st1(dst + i, acc[i] * inv);
-    }
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst) = u32x2_t{f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv)};
+    else *reinterpret_cast<f32x4_any_t*>(dst) = acc * inv;
     if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
 }
 

@@ -55,7 +55,7 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
     p.few = rows <= 16 && ceil_div(p.nt, 2) * rows * k * (int64_t)size_of(dtype) <= 64 << 20 && !(f32 && rows > 4 && p.kt > 16);
     int64_t splits = 1;
     if (!p.few) {
-        p.xt = rows <= 16 ? 1 : rows <= 32 || f32 ? 2 : 4;
+        p.xt = rows <= 16 || k < 8 ? 1 : rows <= 32 || f32 ? 2 : 4;
         const int64_t blocks = ceil_div(p.nt, 16) * ceil_div(rows, p.xt * 16);
         splits = std::max<int64_t>(1, std::min<int64_t>((p.xt == 4 ? 256 : 512) / blocks, p.kt / 4));
         if (splits > 5) splits = std::min<int64_t>((splits + 3) / 8 * 8, 16);
@@ -70,23 +70,23 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
     return p;
 }
 
-template <typename T, bool VEC> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
+template <typename T> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
+    const bool wide = a.k >= 8;
     if (p.few) {
-        const dim3 grid((unsigned)ceil_div(p.nt, 2));
-        const unsigned threads = 64 * p.waves;
-        if (a.rows <= 4) w4_few_kernel<T, 2, 1, VEC><<<grid, threads, 0, st>>>(a);
-        else w4_few_kernel<T, 2, 4, VEC><<<grid, threads, 0, st>>>(a);
+        const unsigned grid = (unsigned)ceil_div(p.nt, 2), threads = 64 * p.waves;
+        if (!wide) w4_few_kernel<T, 2, 4, false><<<grid, threads, 0, st>>>(a);
+        else if (a.rows <= 4) w4_few_kernel<T, 2, 1, true><<<grid, threads, 0, st>>>(a);
+        else w4_few_kernel<T, 2, 4, true><<<grid, threads, 0, st>>>(a);
         return;
     }
     const unsigned grid = (unsigned)(p.splits * ceil_div(p.nt, 16) * ceil_div(a.rows, p.xt * 16));
-    if (p.xt == 1) w4_many_kernel<T, 1, VEC><<<grid, 256, 0, st>>>(a);
-    else if (p.xt == 2) w4_many_kernel<T, 2, VEC><<<grid, 256, 0, st>>>(a);
-    else if constexpr (sizeof(T) == 2) w4_many_kernel<T, 4, VEC><<<grid, 256, 0, st>>>(a);
+    if (!wide) w4_many_kernel<T, 1, false><<<grid, 256, 0, st>>>(a);
+    else if (p.xt == 1) w4_many_kernel<T, 1, true><<<grid, 256, 0, st>>>(a);
+    else if (p.xt == 2) w4_many_kernel<T, 2, true><<<grid, 256, 0, st>>>(a);
+    else if constexpr (sizeof(T) == 2) w4_many_kernel<T, 4, true><<<grid, 256, 0, st>>>(a);
 }
 template <typename T> void w4_run(const W4Plan& p, const W4Args& a, hipStream_t st) {
-    const bool vec = aligned(a.x, 16) && a.ldx % (16 / sizeof(T)) == 0 && a.k % 128 == 0;
-    if (vec) w4_launch<T, true>(p, a, st);
-    else w4_launch<T, false>(p, a, st);
+    w4_launch<T>(p, a, st);
     if (p.splits > 1)
         w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, st>>>(a);
 }
@@ -107,16 +107,6 @@ Kv4Cache dev_cache(const rsd_kv4_cache* c) {
 }
 Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
-}
-
-// Four values at once where every row and head starts on a multiple of four values' size
-template <typename T>
-void append_run(const rsd_kv4_cache* c, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const int32_t* seq,
-                const int32_t* slot, const int32_t* position, int32_t rows, const rsd_kv4_book* book, unsigned blocks, hipStream_t st) {
-    const bool wide = aligned(k, 4 * sizeof(T)) && aligned(v, 4 * sizeof(T)) && !((k_row | k_head | v_row | v_head) & 3);
-    const T *kt = static_cast<const T*>(k), *vt = static_cast<const T*>(v);
-    if (wide) kv4_append_kernel<T, true><<<blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, kt, k_row, k_head, vt, v_row, v_head, seq, slot, position, rows, dev_book(book));
-    else kv4_append_kernel<T, false><<<blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, kt, k_row, k_head, vt, v_row, v_head, seq, slot, position, rows, dev_book(book));
 }
 
 struct AttnPlan { int tiles, waves, split, splits; bool many; uint64_t o_bytes, ml_bytes, lse_bytes; };
@@ -224,8 +214,7 @@ extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* 
         return fail(RSD_EINVAL, "w4_linear: the workspace holds %llu of %llu bytes, or is not 256-byte aligned",
                     (unsigned long long)workspace_bytes, (unsigned long long)p.part_bytes);
     const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks, x, ldx, rows, y, ldy,
-                   p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles, p.splits,
-                   aligned(y, 4 * size_of(dtype)) && ldy % 4 == 0};
+                   p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles, p.splits};
     Launches l;
     if (dtype == RSD_F32) w4_run<float>(p, a, static_cast<hipStream_t>(hip_stream));
     else w4_run<bf16_t>(p, a, static_cast<hipStream_t>(hip_stream));
@@ -244,8 +233,12 @@ extern "C" int rsd_kv4_append(const rsd_kv4_cache* c, const void* k, int64_t k_r
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "append: %d rows are too many", rows);
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (dtype == RSD_F32) append_run<float>(c, k, k_row, k_head, v, v_row, v_head, seq, slot, position, rows, book, (unsigned)blocks, st);
-    else append_run<bf16_t>(c, k, k_row, k_head, v, v_row, v_head, seq, slot, position, rows, book, (unsigned)blocks, st);
+    if (dtype == RSD_F32)
+        kv4_append_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const float*>(k), k_row, k_head,
+                                                                   static_cast<const float*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
+    else
+        kv4_append_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const bf16_t*>(k), k_row, k_head,
+                                                                    static_cast<const bf16_t*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
     return l.done("append");
 }
 
@@ -290,9 +283,6 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse ? a->lse : scored ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
     k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.hd = c->head_dim;
-    const int64_t vec = 16 / (int64_t)size_of(a->dtype);
-    k.q_wide = aligned(a->q, 16) && a->q_row % vec == 0 && a->q_head % vec == 0;
-    k.o_wide = aligned(a->out, 4 * size_of(a->dtype)) && a->out_row % 4 == 0 && a->out_head % 4 == 0;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);

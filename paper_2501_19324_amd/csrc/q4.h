@@ -15,6 +15,10 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+// the same at any address of a bf16 or an fp32 value: the memory serves such loads and stores, across lines too
+typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
+typedef u32x2_t u32x2_any_t __attribute__((aligned(2)));
+typedef f32x4_t f32x4_any_t __attribute__((aligned(4)));
 template <int N> struct u32vec;
 template <> struct u32vec<1> { typedef uint32_t type __attribute__((ext_vector_type(1))); };
 template <> struct u32vec<2> { typedef u32x2_t type; };
@@ -45,7 +49,8 @@ __device__ __forceinline__ u32x4_t q4_decode8(uint32_t codes, uint32_t scale_bit
 }
 // byte t of a dword of scale bytes, at the exponent's place (the bits around it are not looked at)
 template <int T> __device__ __forceinline__ uint32_t q4_scale_at(uint32_t bytes) {
-    return T == 3 ? bytes >> 1 : bytes << (23 - 8 * T);
+    if constexpr (T == 3) return bytes >> 1;
+    else return bytes << (23 - 8 * T);
 }
 
 __device__ __forceinline__ f32x4_t q4_mfma(u32x4_t a, u32x4_t b, f32x4_t c) {

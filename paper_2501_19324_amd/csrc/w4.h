@@ -18,17 +18,18 @@ struct W4Args {
     int64_t ldy;
     float* part;        // partial sums [split][rows][n], null: the block writes y
     int tiles, splits;  // tiles of 128 columns per split
-    bool y_wide;        // rows of y start on multiples of four values
 };
 template <typename T> constexpr int w4_planes = sizeof(T) == 4 ? 3 : 1;
 
-// Eight values of x.  VEC: the row's 16-byte pieces are aligned and k is a multiple of 128; otherwise value by value, zero from column k on.
+// Eight values of x from column k0 on.  WIDE (k >= 8): one or two loads of 16 bytes wherever the row starts (the memory takes them at any address of the type), the
+// last ones of a row moved back to end with it; w4_tail then brings their values to their places.  Else value by value.
+// (Rows of an odd length loaded value by value, the rule before: 256 rows, 5000 x 5001: 54 us, now 30; 16 rows: 22, now 9.)
 template <typename T> struct W4Piece;
 template <> struct W4Piece<bf16_t> { u32x4_t v; };
 template <> struct W4Piece<float> { f32x4_t a, b; };
-template <bool VEC> __device__ __forceinline__ void w4_load(const bf16_t* row, int k0, int k, W4Piece<bf16_t>& o) {
-    if constexpr (VEC) {
-        o.v = *reinterpret_cast<const u32x4_t*>(row + k0);
+template <bool WIDE> __device__ __forceinline__ void w4_load(const bf16_t* row, int k0, int k, W4Piece<bf16_t>& o) {
+    if constexpr (WIDE) {
+        o.v = *reinterpret_cast<const u32x4_any_t*>(row + min(k0, k - 8));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -37,10 +38,10 @@ template <bool VEC> __device__ __forceinline__ void w4_load(const bf16_t* row, i
         }
     }
 }
-template <bool VEC> __device__ __forceinline__ void w4_load(const float* row, int k0, int k, W4Piece<float>& o) {
-    if constexpr (VEC) {
-        o.a = *reinterpret_cast<const f32x4_t*>(row + k0);
-        o.b = *reinterpret_cast<const f32x4_t*>(row + k0 + 4);
+template <bool WIDE> __device__ __forceinline__ void w4_load(const float* row, int k0, int k, W4Piece<float>& o) {
+    if constexpr (WIDE) {
+        o.a = *reinterpret_cast<const f32x4_any_t*>(row + min(k0, k - 8));
+        o.b = *reinterpret_cast<const f32x4_any_t*>(row + min(k0, k - 8) + 4);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -49,6 +50,26 @@ template <bool VEC> __device__ __forceinline__ void w4_load(const float* row, in
             o.b[i] = k0 + 4 + i < k ? q : 0.f;
         }
     }
+}
+// the piece `by` values further on (0 .. 8 or more), zeros behind it
+__device__ __forceinline__ void w4_tail(W4Piece<bf16_t>& x, int by) {
+    uint64_t lo = u64_of(x.v[0], x.v[1]), hi = u64_of(x.v[2], x.v[3]);
+    const int bits = 16 * (by & 3);
+    if (by & 4) lo = hi, hi = 0;
+    if (bits) lo = (lo >> bits) | (hi << (64 - bits)), hi >>= bits;
+    if (by >= 8) lo = hi = 0;
+    x.v = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+__device__ __forceinline__ void w4_tail(W4Piece<float>& x, int by) {
+    float v[8] = {x.a[0], x.a[1], x.a[2], x.a[3], x.b[0], x.b[1], x.b[2], x.b[3]};
+#pragma unroll
+    for (int s = 1; s < 8; s *= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = by & s ? (i + s < 8 ? v[i + s] : 0.f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = by >= 8 ? 0.f : v[i];
+    x.a = f32x4_t{v[0], v[1], v[2], v[3]};
+    x.b = f32x4_t{v[4], v[5], v[6], v[7]};
 }
 // the piece as operands, one per plane, `stride` vectors apart
 __device__ __forceinline__ void w4_put(const W4Piece<bf16_t>& x, u32x4_t* at, int) { *at = x.v; }
@@ -69,7 +90,7 @@ template <int NT> __device__ __forceinline__ void w4_load(const W4Args& a, int n
         o.s[i] = a.scales[((int64_t)n * a.ks + (t >> 2)) * 64 + lane];
     }
 }
-// four results (rows of W n .. n + 3) of row `row` of x.  The splits' rows are padded to whole vectors; y takes vectors where it is aligned for them.
+// four results (rows of W n .. n + 3) of row `row` of x.  The splits' rows are padded to whole vectors.
 __host__ __device__ inline int w4_padded(int n) { return (n + 3) & ~3; }
 template <typename T> __device__ __forceinline__ void w4_store(const W4Args& a, int split, int row, int n, f32x4_t s) {
     if (row >= a.rows || n >= a.n) return;
@@ -78,9 +99,9 @@ template <typename T> __device__ __forceinline__ void w4_store(const W4Args& a, 
         return;
     }
     T* o = static_cast<T*>(a.y) + row * a.ldy + n;
-    if (n + 3 < a.n && a.y_wide) {
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(f2bf2(s[0], s[1]), f2bf2(s[2], s[3]));
-        else *reinterpret_cast<f32x4_t*>(o) = s;
+    if (n + 3 < a.n) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(o) = u32x2_t{f2bf2(s[0], s[1]), f2bf2(s[2], s[3])};
+        else *reinterpret_cast<f32x4_any_t*>(o) = s;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (n + i < a.n) st1(o + i, s[i]);
@@ -93,7 +114,7 @@ template <typename T> __device__ __forceinline__ void w4_store(const W4Args& a, 
 // Bound by the weights' bytes: 7B gate and up, one row: 72 MB in 14.5 us; what x costs is read once per block, from L2.
 // waves that a block may have: their parts of x, and their sums, share 64 KB (fp32 with up to 16 rows: 96 KB)
 template <typename T, int XL> constexpr int w4_few_waves = w4_planes<T> == 3 && XL == 4 ? 8 : 16;
-template <typename T, int NT, int XL, bool VEC>
+template <typename T, int NT, int XL, bool WIDE>
 __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Args a) {
     constexpr int P = w4_planes<T>, WAVES = w4_few_waves<T, XL>, XR = XL * 4, PLANE = 16 * XR;
     __shared__ u32x4_t lds[WAVES * (P * PLANE > NT * 64 ? P * PLANE : NT * 64)];
@@ -112,10 +133,13 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
     auto load = [&](int t, W4Tile<NT>& w_, W4Piece<T>(&x_)[XL]) {
         t = min(t, t1 - 1);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) w4_load<VEC>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
+        for (int i = 0; i < XL; ++i) w4_load<WIDE>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
         w4_load<NT>(a, n0, t, lane, w_);
     };
-    auto work = [&](int t, const W4Tile<NT>& w_, const W4Piece<T>(&x_)[XL]) {
+    auto work = [&](int t, const W4Tile<NT>& w_, W4Piece<T>(&x_)[XL]) {
+        if (WIDE && t * 128 + 128 > a.k)
+#pragma unroll
+            for (int i = 0; i < XL; ++i) w4_tail(x_[i], max(0, t * 128 + k8 * 8 - (a.k - 8)));
 #pragma unroll
         for (int i = 0; i < XL; ++i) w4_put(x_[i], stage + ((k8 & 3) * 4 + (k8 >> 2)) * XR + i * 4 + (lane >> 4), PLANE);
 #pragma unroll
@@ -165,7 +189,7 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
 // 256 rows, 3584 x 18944: 45 us, 770 TFLOP/s, and 5 us for the sums; 37888 x 3584: 80 us, 870 TFLOP/s.  A plain bf16 product of 8192^3 reaches 1220 here.  Bound by
 // the products and the reads of LDS in turn: a wave takes 25 clocks for a product instead of 16, at the 1.8 GHz that such a load leaves; a second block per CU
 // changes little, reading the operands of a group ahead or twice the rows of W per wave nothing.
-template <typename T, int XT, bool VEC>
+template <typename T, int XT, bool WIDE>
 __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
     constexpr int P = w4_planes<T>, NT = 4, DW = 4, DX = 4;
     __shared__ u32x4_t lds[2][P][XT * 256];
@@ -193,9 +217,12 @@ __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
     auto load_x = [&](int t, W4Piece<T>(&x_)[XT]) {
         t = min(t, t1 - 1);
 #pragma unroll
-        for (int i = 0; i < XT; ++i) w4_load<VEC>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
+        for (int i = 0; i < XT; ++i) w4_load<WIDE>(row[i], t * 128 + k8 * 8, a.k, x_[i]);
     };
-    auto put_x = [&](const W4Piece<T>(&x_)[XT], int buf) {
+    auto put_x = [&](int t, W4Piece<T>(&x_)[XT], int buf) {
+        if (WIDE && t < t1 && t * 128 + 128 > a.k)
+#pragma unroll
+            for (int i = 0; i < XT; ++i) w4_tail(x_[i], max(0, t * 128 + k8 * 8 - (a.k - 8)));
 #pragma unroll
         for (int i = 0; i < XT; ++i) w4_put(x_[i], &lds[buf][0][(i * 4 + (k8 & 3)) * 64 + (k8 >> 2) * 16 + slot], XT * 256);
     };
@@ -236,7 +263,7 @@ __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
     load_s(t0, scale[0]);
 #pragma unroll
     for (int s = 0; s < DW - 1; ++s) load_w(t0 + s, w[s]);
-    put_x(x[0], 0);
+    put_x(t0, x[0], 0);
     __syncthreads();
     for (int t = t0; t < t1; t += 2 * DW) {                 // two turns: the scales have two buffers
 #pragma unroll
@@ -248,7 +275,7 @@ __global__ __launch_bounds__(256) void w4_many_kernel(W4Args a) {
                 load_x(u + DX, x[s % DX]);
                 load_w(u + DW - 1, w[(s + DW - 1) % DW]);
                 if (u < t1) {
-                    put_x(x[(s + 1) % DX], (s + 1) & 1);
+                    put_x(u + 1, x[(s + 1) % DX], (s + 1) & 1);
                     work(8 * s, s & 1, w[s], scale[h]);
                 }
                 __syncthreads();
