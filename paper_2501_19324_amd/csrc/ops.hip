@@ -39,11 +39,13 @@ constexpr int64_t kMostBlocks = 1ll << 22;      // blocks of at most 512 threads
 
 // ---- products with 4-bit weights
 
-struct W4Plan { int nt, kt, ks; bool few; int waves, xt, splits, tiles; uint64_t part_bytes; };
+struct W4Plan { int nt, kt, ks; bool few; int ntile, waves, xt, splits, tiles; uint64_t part_bytes; };
 
 // Which kernel, and how the columns are split (by sizes and type alone; measured on both sides of each bound, times with launch):
 //  - few rows (<= 16): while its blocks together read at most 64 MB of x (16 rows bf16, 3584 x 3584: 8.2 us against 12.4; 8 rows, 8192 x 29568: 35.8 against 29.4),
-//    and for more than four rows of fp32, which its waves cut into three parts each for itself, up to 16 tiles of columns (1536 x 1536: 8.4 against 12.2, 3584 x 3584: 15.5 against 12.3).
+//    and with more than four rows while a wave has few tiles of columns: up to 80 in all (8 rows bf16, 8192 x 8192: 12.1 us against 13.6; 3584 x 18944: 21.6
+//    against 12.3), up to 16 in fp32, which its waves cut into three parts each for itself (1536 x 1536: 8.4 against 12.2, 3584 x 3584: 15.5 against 12.3).
+//    Four tiles of W to a block instead of two where two would give more blocks of 16 waves than CUs (8 rows, 10240 x 8192: 13.9 us against 21.2; 8192 x 8192: 12.9 against 12.5).
 //  - many rows: blocks for every CU, two where a tile of x is small (64 rows, 3584 x 18944: 73 us in 2 splits, 40 in 4, 24 in 8, 19 in 16; 256 rows: 73, 44, 44, 55),
 //    no split of fewer than four tiles.  From six on splits come in eights: one part of x per XCD.
 W4Plan w4_plan(int rows, int n, int k, int dtype) {
@@ -52,7 +54,8 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
     p.kt = (int)ceil_div(k, 128);
     p.ks = (int)ceil_div(k, 512);
     const bool f32 = dtype == RSD_F32;
-    p.few = rows <= 16 && ceil_div(p.nt, 2) * rows * k * (int64_t)size_of(dtype) <= 64 << 20 && !(f32 && rows > 4 && p.kt > 16);
+    p.few = rows <= 16 && ceil_div(p.nt, 2) * rows * k * (int64_t)size_of(dtype) <= 64 << 20 && !(rows > 4 && p.kt > (f32 ? 16 : 80));
+    p.ntile = rows > 4 && k >= 8 && p.nt > 512 ? 4 : 2;
     int64_t splits = 1;
     if (!p.few) {
         p.xt = rows <= 16 || k < 8 ? 1 : rows <= 32 || f32 ? 2 : 4;
@@ -64,7 +67,7 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
     if (!p.few) p.tiles = (p.tiles + 3) & ~3;
     p.splits = (int)ceil_div(p.kt, p.tiles);
     // waves of a few-row block: some 4096 in all, at least four, as many as take equally many tiles
-    p.waves = (int)std::min<int64_t>(std::min(f32 && rows > 4 ? 8 : 16, p.kt), std::max<int64_t>(4, ceil_div(4096, ceil_div(p.nt, 2))));
+    p.waves = (int)std::min<int64_t>(std::min(f32 && rows > 4 ? 8 : 16, p.kt), std::max<int64_t>(4, ceil_div(4096, ceil_div(p.nt, p.ntile))));
     p.waves = (int)ceil_div(p.kt, ceil_div(p.kt, p.waves));
     p.part_bytes = p.splits > 1 ? up256((uint64_t)p.splits * rows * w4_padded(n) * 4) : 0;
     return p;
@@ -73,10 +76,11 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
 template <typename T> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
     const bool wide = a.k >= 8;
     if (p.few) {
-        const unsigned grid = (unsigned)ceil_div(p.nt, 2), threads = 64 * p.waves;
+        const unsigned grid = (unsigned)ceil_div(p.nt, p.ntile), threads = 64 * p.waves;
         if (!wide) w4_few_kernel<T, 2, 4, false><<<grid, threads, 0, st>>>(a);
         else if (a.rows <= 4) w4_few_kernel<T, 2, 1, true><<<grid, threads, 0, st>>>(a);
-        else w4_few_kernel<T, 2, 4, true><<<grid, threads, 0, st>>>(a);
+        else if (p.ntile == 2) w4_few_kernel<T, 2, 4, true><<<grid, threads, 0, st>>>(a);
+        else w4_few_kernel<T, 4, 4, true><<<grid, threads, 0, st>>>(a);
         return;
     }
     const unsigned grid = (unsigned)(p.splits * ceil_div(p.nt, 16) * ceil_div(a.rows, p.xt * 16));

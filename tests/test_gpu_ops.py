@@ -111,7 +111,7 @@ def linear_bound(x, w, k, dtype, y):
 
 LINEAR = [(1, 1, 1), (1, 16, 32), (1, 17, 33), (2, 15, 128), (3, 64, 129), (7, 100, 512), (1, 300, 1536), (16, 33, 513), (17, 48, 640), (31, 20, 1100), (32, 64, 2048),
           (33, 70, 300), (64, 129, 260), (65, 31, 1536), (100, 40, 96), (128, 256, 384), (130, 33, 700), (257, 17, 130), (1, 40, 9000), (5, 5000, 70), (70, 2100, 1000),
-          (20, 101, 5000), (40, 50, 2100), (6, 37, 2600), (12, 2050, 2200), (66, 18, 6200), (100, 600, 520), (3, 20, 7), (40, 300, 5), (20, 33, 8), (9, 64, 15), (70, 40, 9)]
+          (20, 101, 5000), (40, 50, 2100), (6, 37, 2600), (12, 2050, 2200), (66, 18, 6200), (100, 600, 520), (3, 20, 7), (40, 300, 5), (20, 33, 8), (9, 64, 15), (70, 40, 9), (8, 8300, 150), (6, 20, 10500)]
 
 
 @pytest.mark.parametrize("rows,n,k", LINEAR)
