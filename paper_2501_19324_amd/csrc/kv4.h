@@ -156,6 +156,7 @@ struct Kv4Attn {
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
     int max_kv, split, splits, hd;
+    bool by_length;         // the blocks of the longest sequences go first
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
     Kv4Book book;
@@ -169,6 +170,20 @@ __device__ __forceinline__ void kv4_rows(const Kv4Attn& a, int b, int& r0, int& 
         count = min(min(max(a.row_start[b + 1], r0), a.total_rows) - r0, a.max_rows);
     }
     n = min(min(max(a.c.kv_len[b], 0), a.max_kv), a.c.max_pages * KV4_PAGE);
+}
+
+// Sequences of unlike lengths make blocks of unlike times; where the blocks do not all run at once the longest go first, so that the last to start are short
+// (16 sequences, the case at kv4_attn_many_kernel: 225 -> 150 us).  The i-th sequence in that order, among every 64 together: the same for all lanes of a
+// whole wave, about a microsecond at a block's start.
+__device__ __forceinline__ int kv4_by_length(const Kv4Attn& a, int i) {
+    if (!a.by_length) return i;
+    const int lane = threadIdx.x & 63, first = i & ~63;
+    const int len = first + lane < a.c.batch ? min(max(a.c.kv_len[first + lane], 0), 1 << 24) : -1;
+    const int key = len * 64 + 63 - lane;                   // no two alike
+    int before = 0;
+#pragma unroll 8
+    for (int u = 0; u < 64; ++u) before += __builtin_amdgcn_readlane(key, u) > key;
+    return first + __builtin_ctzll(__ballot(before == (i & 63)));
 }
 
 template <int HD> struct Kv4Keys { typename u32vec<HD / 32>::type w[4]; uint32_t scale[4]; };
@@ -424,8 +439,9 @@ __device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
 // its waves take chunks of 64 in turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's bytes are requested before
 // this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (28 columns, 64 sequences: 62 us against 78 with
 // both tiles in one wave's registers).
-// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 186 us, 4.6 TB/s, of the 4.9 that a copy reaches; 519 vector and 48 matrix instructions per chunk
-// keep a SIMD busy for two thirds of that.  Without the requests ahead 190 us, with them dropped for a third wave per SIMD 198.
+// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 181 us, 4.7 TB/s, of the 4.9 that a copy reaches (189 us in the order of the sequences); 519 vector
+// and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  In that order: 190 us without the requests ahead, 198 with them dropped for a
+// third wave per SIMD.
 // SCORED: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
 // once more (64 sequences of 128 .. 5120 entries: 51 us instead of 56 in two launches; 256 blocks, so the longest sequence decides).
 template <typename T, int HD, int PLANES, bool SCORED>
@@ -434,7 +450,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     __shared__ __align__(16) float lds_o[WAVES][G * 2][64][4];
     __shared__ float lds_ml[WAVES][2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, quad = lane >> 4;
-    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * 16, col = col0 + (lane & 15);
+    const int b = kv4_by_length(a, blockIdx.x / a.c.hkv), head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * 16, col = col0 + (lane & 15);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
     const int cols = count * a.group;
@@ -551,15 +567,17 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 
 // Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
 // need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
-// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows, 72B heads, fp32: 253 us with one buffer in LDS and three waves a SIMD,
-// 267 with two buffers and two waves, 365 with two tiles to a wave (half the reads of LDS, one wave a SIMD), 510 with four waves (registers spill).
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 150 us, 1.14 executed PFLOP/s (three bf16
+// parts of q and of the weights) of the 1.22 that a plain product reaches.  In the order of the sequences 225 us; in that order with two buffers in LDS and two waves
+// a SIMD 6 % more, with two tiles to a wave (half the reads of LDS, one wave a SIMD) 44 % more, with four waves a SIMD twice as much (registers spill).
 template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
     typedef typename u32vec<G>::type V;
     __shared__ u32x4_t lds_k[4 * G][64], lds_v[4 * G][64];              // keys [page][j], values [pair of pages][block of 16 dims]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
-    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * COLS;
+    const int id = blockIdx.x + gridDim.x * blockIdx.y, head = id % a.c.hkv, col0 = id / a.c.hkv % gridDim.y * COLS;
+    const int b = kv4_by_length(a, id / a.c.hkv / gridDim.y);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
     const int cols = count * a.group;

@@ -113,7 +113,7 @@ Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
 }
 
-struct AttnPlan { int tiles, waves, split, splits; bool many; uint64_t o_bytes, ml_bytes, lse_bytes; };
+struct AttnPlan { int tiles, waves, split, splits; bool many, by_length; uint64_t o_bytes, ml_bytes, lse_bytes; };
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
 //  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
@@ -121,6 +121,7 @@ struct AttnPlan { int tiles, waves, split, splits; bool many; uint64_t o_bytes, 
 //    With fewer than 128 pairs the entries are split for 512 of them, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six chunks); with more,
 //    down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
 //  - many columns: up to 1024 blocks, parts of eight chunks at least (64 sequences x 4 kv heads, 8 rows, bf16: 105 us in two parts, 79 in four, 94 in eight).
+//  - more blocks than run at once (512 of four waves): the longest sequences first (256 x 4: 181 us against 189); below, the order decides nothing and costs 1 us.
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
@@ -134,6 +135,7 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.many ? 1024 / base : ceil_div(512, base), chunks / least));
     p.split = (int)(ceil_div(chunks, want) * KV4_CHUNK);
     p.splits = (int)ceil_div(chunks * KV4_CHUNK, p.split);
+    p.by_length = base * p.splits > 512;
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -286,7 +288,7 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse ? a->lse : scored ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
-    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.hd = c->head_dim;
+    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.hd = c->head_dim;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);
