@@ -172,6 +172,9 @@ __device__ __forceinline__ void kv4_rows(const Kv4Attn& a, int b, int& r0, int& 
     n = min(min(max(a.c.kv_len[b], 0), a.max_kv), a.c.max_pages * KV4_PAGE);
 }
 
+// parts that the entries of a sequence make
+__device__ __forceinline__ int kv4_parts(const Kv4Attn& a, int n) { return a.splits == 1 ? 1 : (n - 1) / a.split + 1; }
+
 // Sequences of unlike lengths make blocks of unlike times; where the blocks do not all run at once the longest go first, so that the last to start are short
 // (16 sequences, the case at kv4_attn_many_kernel: 225 -> 150 us).  The i-th sequence in that order, among every 64 together: the same for all lanes of a
 // whole wave, about a microsecond at a block's start.
@@ -317,8 +320,8 @@ __device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int sa
 
 // what a column has gathered, for the join: rows (dims) 4 quad + i of every block d of 16 dims, column lane % 16
 template <typename T>
-__device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total) {
-    if (a.splits > 1) {
+__device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total, int parts) {
+    if (parts > 1) {
         const int64_t at = (row * a.heads + qh) * a.splits + blockIdx.z;
         *reinterpret_cast<f32x4_t*>(a.part_o + at * a.hd + dim) = acc;
         if (first) a.part_ml[at] = make_float2(top, total);
@@ -439,7 +442,7 @@ __device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
 // its waves take chunks of 64 in turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's bytes are requested before
 // this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (28 columns, 64 sequences: 62 us against 78 with
 // both tiles in one wave's registers).
-// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 181 us, 4.7 TB/s, of the 4.9 that a copy reaches (189 us in the order of the sequences); 519 vector
+// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 172 .. 181 us, 4.7 .. 5 TB/s, what a copy reaches (8 us more in the order of the sequences); 519 vector
 // and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  In that order: 190 us without the requests ahead, 198 with them dropped for a
 // third wave per SIMD.
 // SCORED: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
@@ -453,8 +456,8 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     const int b = kv4_by_length(a, blockIdx.x / a.c.hkv), head = blockIdx.x % a.c.hkv, col0 = blockIdx.y * 16, col = col0 + (lane & 15);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
-    const int cols = count * a.group;
-    if (col0 >= cols) return;
+    const int cols = count * a.group, parts = kv4_parts(a, n);
+    if (col0 >= cols || (int)blockIdx.z >= parts) return;
     const int begin = blockIdx.z * a.split, end = min(begin + a.split, n - (count - 1 - (min(cols, col0 + 16) - 1) / a.group));
     const int safe = min(end, n - (count - 1 - col0 / a.group));      // below: every column sees every entry
     const int limit = min(end, col < cols ? n - (count - 1 - col / a.group) : 0);      // entries seen by the column's row: slots below
@@ -537,7 +540,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
-        if (col < cols) kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total);
+        if (col < cols) kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, parts);
     }
     if constexpr (SCORED) {
         float best = -INFINITY, total = 0.f;
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 
 // Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
 // need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
-// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 150 us, 1.14 executed PFLOP/s (three bf16
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 150 us, 0.86 executed PFLOP/s (three bf16
 // parts of q and of the weights) of the 1.22 that a plain product reaches.  In the order of the sequences 225 us; in that order with two buffers in LDS and two waves
 // a SIMD 6 % more, with two tiles to a wave (half the reads of LDS, one wave a SIMD) 44 % more, with four waves a SIMD twice as much (registers spill).
 template <typename T, int HD, int PLANES>
@@ -580,8 +583,8 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     const int b = kv4_by_length(a, id / a.c.hkv / gridDim.y);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
-    const int cols = count * a.group;
-    if (col0 >= cols) return;
+    const int cols = count * a.group, parts = kv4_parts(a, n);
+    if (col0 >= cols || (int)blockIdx.z >= parts) return;
     const int begin = blockIdx.z * a.split, end = min(begin + a.split, n - (count - 1 - (min(cols, col0 + COLS) - 1) / a.group));
     const int safe = min(end, n - (count - 1 - col0 / a.group));
     const bool mine = col0 + wave * 16 < cols;              // some of this wave's columns exist
@@ -686,7 +689,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     if (col >= cols) return;
 #pragma unroll
     for (int d = 0; d < 2 * G; ++d)
-        kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum);
+        kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum, parts);
 }
 
 // Joins the parts of the entries: 16 lanes per (row, head), HD/16 dims each.  The lanes read 16 parts' maxima and sums at once (one after the other they
@@ -700,22 +703,23 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     const int qh = (int)(id % a.heads), r = (int)(id / a.heads % a.max_rows), b = (int)(id / a.heads / a.max_rows);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
-    if (r >= count) return;
-    // the blocks of this column wrote a part for every split (an empty one where there was nothing to see)
+    const int parts = kv4_parts(a, n);
+    if (r >= count || parts == 1) return;                   // a single part went to its place
+    // (a row that sees nothing of the last part has an empty one there)
     const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;
     float best = -INFINITY;
-    for (int s = l; s < a.splits; s += 16) best = fmaxf(best, a.part_ml[at + s].x);
+    for (int s = l; s < parts; s += 16) best = fmaxf(best, a.part_ml[at + s].x);
     best = row16_max(best);
     const float base = best == -INFINITY ? 0.f : best;
     float total = 0.f, acc[N] = {};
-    for (int s0 = 0; s0 < a.splits; s0 += 16) {
+    for (int s0 = 0; s0 < parts; s0 += 16) {
         float scale = 0.f;
-        if (s0 + l < a.splits) {
+        if (s0 + l < parts) {
             const float2 ml = a.part_ml[at + s0 + l];
             scale = __builtin_amdgcn_exp2f(ml.x - base);
             total += scale * ml.y;
         }
-        const int m = min(16, a.splits - s0);
+        const int m = min(16, parts - s0);
         const float* p = a.part_o + (at + s0) * HD + l * N;
         for (int s = 0; s < m; ++s) {
             const float w = __shfl(scale, s, 16);

@@ -117,11 +117,15 @@ struct AttnPlan { int tiles, waves, split, splits; bool many, by_length; uint64_
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
 //  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
-//  - one tile: eight waves to a block while (sequence, kv head) pairs are fewer than 512 (64 x 4: 35 us against 43 with four), else four (256 x 4: 186 against 197).
-//    With fewer than 128 pairs the entries are split for 512 of them, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six chunks); with more,
-//    down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
-//  - many columns: up to 1024 blocks, parts of eight chunks at least (64 sequences x 4 kv heads, 8 rows, bf16: 105 us in two parts, 79 in four, 94 in eight).
-//  - more blocks than run at once (512 of four waves): the longest sequences first (256 x 4: 181 us against 189); below, the order decides nothing and costs 1 us.
+//  - few columns: eight waves to a block up to 256 blocks (64 x 4 of 128 .. 5120 entries: 33 us against 37 with four), and up to 512 where lists are long
+//    (128 x 4 of 512 .. 8192: 75 us against 90; 256 x 2 of 128 .. 2048: 33 against 29); else four (150 x 4: 65 against 72).
+//    With fewer than 128 (sequence, kv head) pairs the entries are split for 512 blocks, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six
+//    chunks); with more, down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
+//  - many columns: up to 2048 blocks in parts of 20 chunks at least (16 sequences x 4 kv heads, 17 .. 128 rows of 512 .. 2560 entries, bf16: 77 us whole, 68 in two
+//    parts; 64 x 4, 8 rows of 128 .. 5120: 71 in four parts, 75 in seven, 118 whole), in smaller ones, down to six, only to give every CU a block (40 rows of one
+//    sequence, 2 x 2048 entries: 57 us whole, 20 in parts of six).
+//  - more blocks than run at once: the longest sequences first (64 x 4 x 2 tiles: 43 us against 56; 256 x 4 of 4096 .. 8192: 172 against 183); below that the order decides
+//    nothing and costs 1 us.
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
@@ -130,12 +134,17 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     p.many = cols > 32;
     p.tiles = (int)ceil_div(cols, p.many ? 64 : 16);
     const int64_t base = (int64_t)c->batch * c->n_kv_heads * p.tiles;
-    p.waves = p.many ? 4 : (int)std::min<int64_t>(base < 512 ? 8 : 4, chunks);
-    const int64_t least = p.many ? 8 : (int64_t)p.waves * (base < 128 ? 2 : 6);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.many ? 1024 / base : ceil_div(512, base), chunks / least));
-    p.split = (int)(ceil_div(chunks, want) * KV4_CHUNK);
+    int64_t parts;
+    if (p.many) {
+        p.waves = 4;
+        parts = std::max(std::min(ceil_div(2048, base), chunks / 20), std::min(ceil_div(256, base), chunks / 6));
+    } else {
+        p.waves = (int)std::min<int64_t>(base <= 256 || (base <= 512 && chunks >= 48) ? 8 : 4, chunks);
+        parts = std::min<int64_t>(ceil_div(512, base), chunks / (p.waves * (base < 128 ? 2 : 6)));
+    }
+    p.split = (int)(ceil_div(chunks, std::max<int64_t>(1, parts)) * KV4_CHUNK);
     p.splits = (int)ceil_div(chunks * KV4_CHUNK, p.split);
-    p.by_length = base * p.splits > 512;
+    p.by_length = base * p.splits * p.waves > 2048;
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;

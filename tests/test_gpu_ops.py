@@ -349,6 +349,45 @@ def test_attention(torch, R, heads, hkv, hd, lens, rows, dtype):
     check_attention(torch, R, cache, pool, table, lens, q, float(np.float32(scale)), starts, out2, lse2, dtype=dtype)
 
 
+# more blocks than run at once, lengths from none to long in any order; parts of which short sequences have one
+UNEQUAL = [
+    ("single tokens", 140, 4, 4, [300, 0, 17, 64, 1], 1),
+    ("pieces of steps", 140, 16, 4, [300, 0, 17, 64, 12], 10),
+    ("parts", 7, 16, 2, [2700, 0, 1290, 1344, 40, 1345, 2000], 9),
+    ("single tokens in parts", 9, 8, 2, [2700, 0, 511, 512, 513, 40, 1025], 1),
+]
+
+
+@pytest.mark.parametrize("batch,heads,hkv,some,most", [u[1:] for u in UNEQUAL], ids=[u[0] for u in UNEQUAL])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scored", [False, True])
+def test_attention_over_unequal_sequences(torch, R, batch, heads, hkv, some, most, dtype, scored):
+    rng = np.random.default_rng(batch + heads)
+    lens = [int(x) for x in rng.permutation(some + [int(n) for n in rng.integers(0, 70, batch - len(some))])]
+    hd = 32
+    # pages of arbitrary codes; NaN behind the last entry
+    need = [-(-n // 16) for n in lens]
+    pool = rng.integers(0, 256, (sum(need) + 3, hkv, 17 * hd)).astype(np.uint8)
+    pool[:, :, 16 * hd:] = rng.integers(122, 127, (len(pool), hkv, hd))
+    order, table = rng.permutation(len(pool)).astype(np.int32), np.full((batch, max(need)), -1, np.int32)
+    for b, n in enumerate(lens):
+        table[b, :need[b]] = order[sum(need[:b]):sum(need[:b + 1])]
+        for s in range(n, 16 * need[b]):
+            key, val, ks, vs = ref.entry_places(hd, s % 16)
+            pool[table[b, need[b] - 1]][:, np.concatenate([ks, vs])] = 255
+    cache = R.Kv4Cache(dev(torch, pool), dev(torch, table), dev(torch, np.array(lens, np.int32)))
+    counts = [min(int(rng.integers(0, most + 1)), n) if most > 1 else 1 for n in lens]
+    starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    q = dev(torch, (rng.normal(size=(int(starts[-1]), heads, hd)) * 1.5).astype(np.float32)).to(t)
+    kw = {} if most == 1 else dict(row_start=dev(torch, starts), max_rows=most)
+    scores = dev(torch, rng.random((batch, hkv, table.shape[1] * 16)).astype(np.float32)) if scored else None
+    before = host(scores) if scored else None
+    scale = 1 / np.sqrt(hd)
+    out, lse = R.rsd_kv4_attention(cache, q, scale, scores=scores, want_lse=True, **kw)
+    check_attention(torch, R, cache, pool, table, lens, q, float(np.float32(scale)), starts, out, lse, before, host(scores) if scored else None, dtype=dtype)
+
+
 @pytest.mark.parametrize("cap", [64, 4000])
 def test_attention_is_cut_to_max_kv_and_to_the_table(torch, R, cap):
     rng = np.random.default_rng(3)
