@@ -392,6 +392,11 @@ template <int PP> __device__ __forceinline__ void kv4_weights(const f32x4_t s0, 
     }
 }
 
+// weights of the slots from `slot` on, of which the column sees those below `end`
+__device__ __forceinline__ void kv4_seen_weights(f32x4_t& w, int slot, int end) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = slot + i < end ? w[i] : 0.f;
+}
 // Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: lse2 is their logarithm to the base 2, +inf for a
 // column that does not exist.  WHOLE: every column sees every entry.
 template <int HD, int PLANES>
@@ -404,11 +409,7 @@ __device__ __forceinline__ void kv4_add_weights(const Kv4Keys<HD>& k, const u32x
         f32x4_t w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor2, -lse2));
-        if (!whole) {
-            const int end = (there >> p) & 1 ? limit : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = slot0 + p * KV4_PAGE + quad * 4 + i < end ? w[i] : 0.f;
-        }
+        if (!whole) kv4_seen_weights(w, slot0 + p * KV4_PAGE + quad * 4, (there >> p) & 1 ? limit : 0);
         weight[p] += w;
     }
 }
@@ -739,8 +740,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
 // group's probabilities would move as many bytes), now with the final sum of every row.  A wave owns chunks of 64 entries of one (sequence, kv head): no atomics, one order.
 template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
-    constexpr int G = HD / 32;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15;
     const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
@@ -751,18 +751,12 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     const uint8_t* page[4];
     int there, next;
     Kv4Keys<HD> k, k1;
-    u32x4_t q[G][PLANES];
-    int limit;
-    float lse2;
-    auto column = [&](int c0) {
-        const int col = c0 + (lane & 15), r = col / a.group;
-        limit = col < cols ? n - (count - 1 - r) : 0;
-        lse2 = col < cols ? a.lse[(int64_t)(r0 + r) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : INFINITY;
-        kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
-    };
+    u32x4_t q[HD / 32][PLANES];
     kv4_pages<HD>(a.c, b, head, slot0, page, there);
     kv4_load_keys<HD>(page, lane, k);
-    column(0);
+    const int limit = col < cols ? n - (count - 1 - col / a.group) : 0;
+    const float lse2 = col < cols ? a.lse[(int64_t)(r0 + col / a.group) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : INFINITY;
+    kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
     float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
     for (; slot0 < n; slot0 += step) {
         kv4_pages<HD>(a.c, b, head, slot0 + step, page, next);
@@ -770,14 +764,110 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
         const int slot = kv4_score_slot(slot0, n, there);
         const float before = slot >= 0 ? scores[slot] : 0.f;
         f32x4_t weight[4] = {};
-        for (int c0 = 0; c0 < cols; c0 += 16) {
-            if (cols > 16) column(c0);
-            kv4_add_weights<HD, PLANES>(k, q, slot0 + KV4_CHUNK <= safe && there == 15, there, slot0, limit, a.factor2, lse2, weight);
-        }
+        kv4_add_weights<HD, PLANES>(k, q, slot0 + KV4_CHUNK <= safe && there == 15, there, slot0, limit, a.factor2, lse2, weight);
         const float mine = kv4_sum_weights(weight);
         if (slot >= 0) scores[slot] = before + mine;
         k = k1;
         there = next;
+    }
+}
+
+// The same for more than one tile of columns: a wave keeps its chunk's keys decoded and goes over the tiles, whose q the block cuts into operands in LDS, one
+// (tile, 32 dims) by each wave, the next ones while these are worked on.  16 sequences of 17 .. 128 rows and 512 .. 2560
+// entries, 72B heads, fp32: 145 us, 315 with every wave cutting q for itself, chunk by chunk.
+template <typename T, int HD, int PLANES>
+__global__ __launch_bounds__(256, 2) void kv4_weight_many_kernel(Kv4Attn a) {
+    constexpr int G = HD / 32, TILES = 4 / G;
+    __shared__ u32x4_t lds_q[2][4][PLANES][64];             // [buffer][tile * G + 32 dims]
+    __shared__ float lds_lse2[2][TILES][16];
+    __shared__ int lds_limit[2][TILES][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int cols = count * a.group, safe = n - (count - 1);
+    if (cols == 0) return;
+    float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
+    // this lane's column of the tile that its wave cuts: its row, its head of the group, and where q and the logarithm of the sum lie
+    const int first = wave / G * 16 + (lane & 15), rows_on = 16 * TILES / a.group, heads_on = 16 * TILES % a.group;
+    int col, head_at, limit, buf = 0;
+    const T* at;
+    const float* lse;
+    float raw[8] = {}, lse2;
+    auto request = [&]() {                                  // a column beyond the last one keeps the values of the one before it; it sees nothing
+        const bool is = col < cols;
+        if (is) kv4_load8(at, raw);
+        lse2 = is ? *lse * 1.4426950408889634f : INFINITY;
+    };
+    auto advance = [&]() {
+        const bool over = (head_at += heads_on) >= a.group;
+        const int rows = rows_on + over, heads = heads_on - (over ? a.group : 0);
+        head_at -= over ? a.group : 0;
+        col += 16 * TILES;
+        limit = col < cols ? limit + rows : 0;
+        at += rows * a.q_row + heads * a.q_head;
+        lse += (int64_t)rows * a.heads + heads;
+    };
+    for (int base = blockIdx.y * 4 * KV4_CHUNK; base < n; base += gridDim.y * 4 * KV4_CHUNK) {      // the same for all waves: they meet below
+        const int slot0 = base + wave * KV4_CHUNK;
+        const uint8_t* page[4];
+        int there;
+        Kv4Keys<HD> raw_k;
+        u32x4_t k[4][G];
+        col = first, head_at = first % a.group;
+        limit = col < cols ? n - (count - 1 - col / a.group) : 0;
+        at = static_cast<const T*>(a.q) + (int64_t)(r0 + col / a.group) * a.q_row + (int64_t)(head * a.group + head_at) * a.q_head + quad * (HD / 4) + wave % G * 8;
+        lse = a.lse + (int64_t)(r0 + col / a.group) * a.heads + head * a.group + head_at;
+        request();
+        kv4_pages<HD>(a.c, b, head, slot0, page, there);
+        kv4_load_keys<HD>(page, lane, raw_k);
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int j = 0; j < G; ++j) k[p][j] = q4_decode8(raw_k.w[p][j], raw_k.scale[p] << 23);
+        const bool whole = slot0 + KV4_CHUNK <= safe && there == 15;
+        f32x4_t weight[4] = {};
+        for (int c0 = 0; c0 < cols; c0 += 16 * TILES, buf ^= 1) {
+            // the readers of this buffer's last contents have passed the barrier of the step in between
+            u32x4_t o[PLANES];
+            if (a.negative)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[i] = -raw[i];
+            q4_operand<PLANES>(raw, o);
+#pragma unroll
+            for (int x = 0; x < PLANES; ++x) lds_q[buf][wave][x][lane] = o[x];
+            if (wave % G == 0 && quad == 0) lds_lse2[buf][wave / G][lane] = lse2, lds_limit[buf][wave / G][lane] = limit;
+            __syncthreads();
+            advance();
+            request();
+            if (slot0 >= n) continue;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                if (c0 + t * 16 >= cols) break;
+                const float sum2 = lds_lse2[buf][t][lane & 15];
+                f32x4_t s[4] = {};
+#pragma unroll
+                for (int j = 0; j < G; ++j)
+#pragma unroll
+                    for (int x = 0; x < PLANES; ++x) {
+                        const u32x4_t q = lds_q[buf][t * G + j][x][lane];
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) s[p] = q4_mfma(k[p][j], q, s[p]);
+                    }
+                const int sees = lds_limit[buf][t][lane & 15];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    f32x4_t w;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], a.factor2, -sum2));
+                    if (!whole) kv4_seen_weights(w, slot0 + p * KV4_PAGE + quad * 4, (there >> p) & 1 ? sees : 0);
+                    weight[p] += w;
+                }
+            }
+        }
+        const int slot = kv4_score_slot(slot0, n, there);
+        const float mine = kv4_sum_weights(weight);
+        if (slot >= 0) scores[slot] += mine;
     }
 }
 

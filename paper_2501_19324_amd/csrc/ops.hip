@@ -173,8 +173,11 @@ template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const 
         kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
     if (k.book.scores && !fused) {
         const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
-        const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, blocks = std::min<int64_t>(ceil_div(n, 4 * KV4_CHUNK), ceil_div(1024, pairs));
-        if (n > 0) kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)(k.c.batch * k.c.hkv), (unsigned)blocks), 256, 0, st>>>(k);
+        const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, chunks = ceil_div(n, 4 * KV4_CHUNK);
+        if (n > 0 && (int64_t)k.max_rows * k.group <= 16)
+            kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, (unsigned)std::min(chunks, ceil_div(1024, pairs))), 256, 0, st>>>(k);
+        else if (n > 0)
+            kv4_weight_many_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, (unsigned)std::min<int64_t>(chunks, 32768)), 256, 0, st>>>(k);
     }
 }
 template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, hipStream_t st) {
