@@ -160,6 +160,9 @@ struct Kv4Attn {
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
     Kv4Book book;
+    int w_cols, w_groups;   // attention weights: the columns are dealt in groups of w_cols, at most w_groups of them
+    int64_t w_slots;        // of a part below
+    float* part_w;          // [w_groups][batch][kv heads][w_slots]: a group's weight of each entry
 };
 // rows of sequence b: the first one and how many; entries it has
 __device__ __forceinline__ void kv4_rows(const Kv4Attn& a, int b, int& r0, int& count, int& n) {
@@ -773,10 +776,11 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
 }
 
 // The same for more than one tile of columns: a wave keeps its chunk's keys decoded and goes over the tiles, whose q the block cuts into operands in LDS, one
-// (tile, 32 dims) by each wave, the next ones while these are worked on.  16 sequences of 17 .. 128 rows and 512 .. 2560
-// entries, 72B heads, fp32: 145 us, 315 with every wave cutting q for itself, chunk by chunk.
+// (tile, 32 dims) by each wave, the next ones while these are worked on.  Where blocks are few or unlike the columns are dealt in groups, whose weights the next
+// kernel adds up.  16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 113 us with the sum; 145 in one group; 315 with every wave cutting q
+// for itself, chunk by chunk.  216 vector instructions a tile and chunk beside 48 matrix instructions; three waves a SIMD (two: 15 % more).
 template <typename T, int HD, int PLANES>
-__global__ __launch_bounds__(256, 2) void kv4_weight_many_kernel(Kv4Attn a) {
+__global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, TILES = 4 / G;
     __shared__ u32x4_t lds_q[2][4][PLANES][64];             // [buffer][tile * G + 32 dims]
     __shared__ float lds_lse2[2][TILES][16];
@@ -785,11 +789,11 @@ __global__ __launch_bounds__(256, 2) void kv4_weight_many_kernel(Kv4Attn a) {
     const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
-    const int cols = count * a.group, safe = n - (count - 1);
-    if (cols == 0) return;
+    const int begin = blockIdx.z * a.w_cols, cols = min(count * a.group, begin + a.w_cols), safe = n - (count - 1);
+    if (begin >= cols) return;
     float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
     // this lane's column of the tile that its wave cuts: its row, its head of the group, and where q and the logarithm of the sum lie
-    const int first = wave / G * 16 + (lane & 15), rows_on = 16 * TILES / a.group, heads_on = 16 * TILES % a.group;
+    const int first = begin + wave / G * 16 + (lane & 15), rows_on = 16 * TILES / a.group, heads_on = 16 * TILES % a.group;
     int col, head_at, limit, buf = 0;
     const T* at;
     const float* lse;
@@ -827,7 +831,7 @@ __global__ __launch_bounds__(256, 2) void kv4_weight_many_kernel(Kv4Attn a) {
             for (int j = 0; j < G; ++j) k[p][j] = q4_decode8(raw_k.w[p][j], raw_k.scale[p] << 23);
         const bool whole = slot0 + KV4_CHUNK <= safe && there == 15;
         f32x4_t weight[4] = {};
-        for (int c0 = 0; c0 < cols; c0 += 16 * TILES, buf ^= 1) {
+        for (int c0 = begin; c0 < cols; c0 += 16 * TILES, buf ^= 1) {
             // the readers of this buffer's last contents have passed the barrier of the step in between
             u32x4_t o[PLANES];
             if (a.negative)
@@ -865,9 +869,28 @@ __global__ __launch_bounds__(256, 2) void kv4_weight_many_kernel(Kv4Attn a) {
                 }
             }
         }
-        const int slot = kv4_score_slot(slot0, n, there);
         const float mine = kv4_sum_weights(weight);
-        if (slot >= 0) scores[slot] += mine;
+        if (a.w_groups == 1) {
+            const int slot = kv4_score_slot(slot0, n, there);
+            if (slot >= 0) scores[slot] += mine;
+        } else {
+            const int slot = kv4_score_slot(slot0, n, 15);
+            if (slot >= 0) a.part_w[((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * a.w_slots + slot] = kv4_score_slot(slot0, n, there) >= 0 ? mine : -0.f;
+        }
+    }
+}
+// adds the groups' weights to the scores, in the order of the groups
+__global__ __launch_bounds__(256) void kv4_weight_sum_kernel(Kv4Attn a) {
+    const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
+    int r0, count, n;
+    kv4_rows(a, b, r0, count, n);
+    const int groups = (count * a.group + a.w_cols - 1) / a.w_cols;
+    if (groups == 0) return;
+    float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
+    for (int64_t s = (int64_t)blockIdx.y * 256 + threadIdx.x; s < n; s += (int64_t)gridDim.y * 256) {
+        float sum = scores[s];
+        for (int g = 0; g < groups; ++g) sum += a.part_w[((int64_t)g * gridDim.x + blockIdx.x) * a.w_slots + s];
+        scores[s] = sum;
     }
 }
 

@@ -113,7 +113,7 @@ Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
 }
 
-struct AttnPlan { int tiles, waves, split, splits; bool many, by_length; uint64_t o_bytes, ml_bytes, lse_bytes; };
+struct AttnPlan { int tiles, waves, split, splits; bool many, by_length, fused; int w_cols, w_groups; uint64_t o_bytes, ml_bytes, lse_bytes, w_bytes; uint64_t bytes() const { return o_bytes + ml_bytes + lse_bytes + w_bytes; } };
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
 //  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
@@ -126,6 +126,7 @@ struct AttnPlan { int tiles, waves, split, splits; bool many, by_length; uint64_
 //    sequence, 2 x 2048 entries: 57 us whole, 20 in parts of six).
 //  - more blocks than run at once: the longest sequences first (64 x 4 x 2 tiles: 43 us against 56; 256 x 4 of 4096 .. 8192: 172 against 183); below that the order decides
 //    nothing and costs 1 us.
+//  - attention weights of more than one tile: the columns in groups of eight tiles at least, up to 4096 blocks of four chunks.
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);
@@ -149,6 +150,12 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
     p.lse_bytes = scored && !a->lse ? up256(lines * 4) : 0;
+    p.fused = scored && !p.many && p.tiles == 1 && p.splits == 1;
+    const int64_t tiles = ceil_div(cols, 16), pairs = (int64_t)c->batch * c->n_kv_heads;
+    const int64_t groups = tiles == 1 ? 1 : std::max<int64_t>(1, std::min(4096 / (pairs * ceil_div(chunks, 4)), tiles / 8));
+    p.w_cols = (int)(ceil_div(tiles, groups) * 16);
+    p.w_groups = (int)ceil_div(tiles * 16, p.w_cols);
+    p.w_bytes = scored && p.w_groups > 1 ? up256((uint64_t)(p.w_groups * pairs * chunks) * KV4_CHUNK * 4) : 0;
     return p;
 }
 int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
@@ -165,19 +172,21 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
 
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
     const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
-    const bool fused = k.book.scores && !p.many && p.tiles == 1 && p.splits == 1;
     if (p.many) kv4_attn_many_kernel<T, HD, PLANES><<<grid, 256, 0, st>>>(k);
-    else if (fused) kv4_attn_kernel<T, HD, PLANES, true><<<grid, 64 * p.waves, 0, st>>>(k);
+    else if (p.fused) kv4_attn_kernel<T, HD, PLANES, true><<<grid, 64 * p.waves, 0, st>>>(k);
     else kv4_attn_kernel<T, HD, PLANES, false><<<grid, 64 * p.waves, 0, st>>>(k);
     if (p.splits > 1)
         kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
-    if (k.book.scores && !fused) {
+    if (k.book.scores && !p.fused) {
         const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
         const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, chunks = ceil_div(n, 4 * KV4_CHUNK);
         if (n > 0 && (int64_t)k.max_rows * k.group <= 16)
             kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, (unsigned)std::min(chunks, ceil_div(1024, pairs))), 256, 0, st>>>(k);
-        else if (n > 0)
-            kv4_weight_many_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, (unsigned)std::min<int64_t>(chunks, 32768)), 256, 0, st>>>(k);
+        else if (n > 0) {
+            const unsigned y = (unsigned)std::min<int64_t>(chunks, 32768);
+            kv4_weight_many_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, y, (unsigned)p.w_groups), 256, 0, st>>>(k);
+            if (p.w_groups > 1) kv4_weight_sum_kernel<<<dim3((unsigned)pairs, y), 256, 0, st>>>(k);
+        }
     }
 }
 template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, hipStream_t st) {
@@ -278,7 +287,7 @@ extern "C" int rsd_kv4_read(const rsd_kv4_cache* c, const int32_t* seq, const in
 extern "C" uint64_t rsd_kv4_attention_workspace(const rsd_kv4_cache* c, const rsd_kv4_attn* a, int32_t scored) {
     if (check_attn(c, a)) return 0;
     const AttnPlan p = attn_plan(c, a, scored != 0);
-    return p.o_bytes + p.ml_bytes + p.lse_bytes;
+    return p.bytes();
 }
 
 extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, const rsd_kv4_book* book, void* workspace,
@@ -288,7 +297,7 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     if (!aligned(a->q, size_of(a->dtype)) || !aligned(a->out, size_of(a->dtype))) return fail(RSD_EINVAL, "attention: q or out is not aligned to its type");
     const bool scored = book && book->scores;
     const AttnPlan p = attn_plan(c, a, scored);
-    const uint64_t need = p.o_bytes + p.ml_bytes + p.lse_bytes;
+    const uint64_t need = p.bytes();
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
         return fail(RSD_EINVAL, "attention: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
     char* ws = static_cast<char*>(workspace);
@@ -304,6 +313,9 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);
+    k.w_cols = p.w_cols, k.w_groups = p.w_groups;
+    k.w_slots = ceil_div(std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KV4_PAGE), KV4_CHUNK) * KV4_CHUNK;
+    k.part_w = reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes + p.lse_bytes);
     Launches l;
     if (a->dtype == RSD_F32) attn_run<float, 3>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
     else attn_run<bf16_t, 1>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
