@@ -356,14 +356,15 @@ __device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there,
         for (int i = 0; i < 4; ++i) best = fmaxf(best, s[p][i]);
     best = rows4_max(best);
     best = fmaxf(top, best == -INFINITY ? best : best * factor2);      // (0 * inf is no maximum)
-    const float base = best == -INFINITY ? 0.f : best;
-    if (__any(best != top)) {                               // a new maximum somewhere in the tile
-        const float scale = __builtin_amdgcn_exp2f(top - base);
+    // The maximum moves only where some column of the tile passes it by 2^8 (probabilities up to 2^8 lose nothing in 32 bits): seldom after the first chunks.
+    if (__any(best > top + 8.f)) {
+        const float scale = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.f : best));
         sum *= scale;
 #pragma unroll
         for (int d = 0; d < NB; ++d) o[d] *= scale;
         top = best;
     }
+    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
