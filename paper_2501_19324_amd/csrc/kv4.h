@@ -575,9 +575,9 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 
 // Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
 // need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
-// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 150 us, 0.86 executed PFLOP/s (three bf16
-// parts of q and of the weights) of the 1.22 that a plain product reaches.  In the order of the sequences 225 us; in that order with two buffers in LDS and two waves
-// a SIMD 6 % more, with two tiles to a wave (half the reads of LDS, one wave a SIMD) 44 % more, with four waves a SIMD twice as much (registers spill).
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 140 .. 148 us, 0.9 executed PFLOP/s (three
+// bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 107 us.  (4 % more in fp32 with the sums of a tile one after the other; 225 in the
+// order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 177, bf16 115.
 template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
@@ -666,26 +666,38 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
                 }
                 kv4_nan_values<HD>(v, slot0, safe, limit, o);
             }
+            // four sums side by side: a matrix instruction that waits for the one before it leaves the unit idle
             f32x4_t s[4] = {};
+            u32x4_t k[2][4];
 #pragma unroll
-            for (int p = 0; p < 4; ++p)
+            for (int p = 0; p < 4; ++p) k[0][p] = lds_k[p * G][lane];
 #pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    const u32x4_t k = lds_k[p * G + j][lane];
+            for (int j = 0; j < G; ++j) {
+                if (j + 1 < G)
 #pragma unroll
-                    for (int x = 0; x < PLANES; ++x) s[p] = q4_mfma(k, q[j][x], s[p]);
-                }
+                    for (int p = 0; p < 4; ++p) k[(j + 1) & 1][p] = lds_k[p * G + j + 1][lane];
+#pragma unroll
+                for (int x = 0; x < PLANES; ++x)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) s[p] = q4_mfma(k[j & 1][p], q[j][x], s[p]);
+            }
+            constexpr int AT = G == 1 ? 2 : 4, STEPS = 4 * G / AT;       // values: operands of a pair of pages, then those of the other
+            u32x4_t v[2][AT];
+#pragma unroll
+            for (int d = 0; d < AT; ++d) v[0][d] = lds_v[d][lane];
             kv4_softmax<2 * G>(s, slot0 + KV4_CHUNK <= safe && there0 == 15, there0, slot0, limit, quad, a.factor2, top, sum, o);
+            u32x4_t w[PP];
 #pragma unroll
-            for (int p = 0; p < 4; p += 2) {
-                u32x4_t w[PP];
-                kv4_weights<PP>(s[p], s[p + 1], w);
+            for (int t = 0; t < STEPS; ++t) {
+                if (t == 0) kv4_weights<PP>(s[0], s[1], w);
+                if (t == STEPS / 2) kv4_weights<PP>(s[2], s[3], w);
+                if (t + 1 < STEPS)
 #pragma unroll
-                for (int d = 0; d < 2 * G; ++d) {
-                    const u32x4_t v = lds_v[p * G + d][lane];
+                    for (int d = 0; d < AT; ++d) v[(t + 1) & 1][d] = lds_v[(t + 1) * AT + d][lane];
 #pragma unroll
-                    for (int x = 0; x < PP; ++x) o[d] = q4_mfma(v, w[x], o[d]);
-                }
+                for (int x = 0; x < PP; ++x)
+#pragma unroll
+                    for (int d = 0; d < AT; ++d) o[(t * AT + d) % (2 * G)] = q4_mfma(v[t & 1][d], w[x], o[(t * AT + d) % (2 * G)]);
             }
         }
         __syncthreads();
