@@ -76,32 +76,60 @@ template <bool PAIRED> __device__ __forceinline__ uint32_t kv4_encode8(const flo
 
 // ---- entries in: four lanes take one group of 32 dims of one (row, head), keys and values.  What a lane has to wait for in turn (row numbers,
 // then the table, then the stores) is a chain of latencies: keys and values are requested before it, eight of each to a lane.
-// 7936 rows of 8 heads in fp32 (75 MB): 37 us with two values to a lane, requested behind the chain.
+// Four rows lie side by side in a wave: where they are four tokens of a page that share their values' dwords (pieces of prompts), the lanes exchange bytes and store whole
+// dwords.  7936 rows of 8 heads in fp32 (75 MB): 17 us, 21.5 byte by byte, 37 with two values to a lane, requested behind the chain.
+struct Kv4Line { int row, h, g, l, r, first; };
+__device__ __forceinline__ Kv4Line kv4_line(int hkv, int groups) {
+    const uint32_t item = (blockIdx.x * 256 + threadIdx.x) >> 2, four = item / groups;       // [row / 4][head][row % 4][group]
+    Kv4Line t;
+    t.l = threadIdx.x & 3, t.g = (int)(item % groups), t.r = (int)(four & 3);
+    t.h = (int)((four >> 2) % hkv), t.row = (int)((four >> 2) / hkv * 4) + t.r;
+    t.first = (threadIdx.x & 63) - t.r * 4 * groups;        // the lane of row % 4 = 0
+    return t;
+}
+// all four rows exist (`is`) and their slots share the values' dwords; every lane of the wave takes part
+__device__ __forceinline__ bool kv4_together(const Kv4Line& t, int groups, bool is, int b, int s) {
+    const int b0 = __shfl(b, t.first), s0 = __shfl(s, t.first);
+    const uint64_t fits = __ballot(is && b == b0 && s == s0 + t.r && (s0 & 3) == 0), four = 1ull | 1ull << 4 * groups | 1ull << 8 * groups | 1ull << 12 * groups;
+    return ((fits >> t.first) & four) == four;
+}
+// byte i of row r's lane <-> byte r of row i's lane
+__device__ __forceinline__ uint32_t kv4_exchange(const Kv4Line& t, int groups, uint32_t x) {
+    uint32_t y = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y |= (((uint32_t)__shfl((int)x, t.first + i * 4 * groups) >> (8 * t.r)) & 255u) << (8 * i);
+    return y;
+}
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Cache c, int hd, const T* __restrict__ k, int64_t k_row, int64_t k_head, const T* __restrict__ v,
                                                          int64_t v_row, int64_t v_head, const int* __restrict__ seq, const int* __restrict__ slot,
                                                          const int* __restrict__ position, int rows, Kv4Book book) {
-    const int l = threadIdx.x & 3, groups = hd / 32;
-    const uint32_t item = (blockIdx.x * 256 + threadIdx.x) >> 2, line = item / groups;
-    const int g = (int)(item % groups), h = (int)(line % c.hkv), row = (int)(line / c.hkv);
-    if (row >= rows) return;                              // four lanes leave together
-    const int b = seq[row], s = slot[row];
-    const T* kr = k + row * k_row + h * k_head + g * 32 + 8 * l;
-    const T* vr = v + row * v_row + h * v_head + g * 32 + 4 * l;
-    float kx[8], vx[8];
-    kv4_load4(kr, kx);
-    kv4_load4(kr + 4, kx + 4);
-    kv4_load4(vr, vx);
-    kv4_load4(vr + 16, vx + 4);
-    if ((unsigned)b >= (unsigned)c.batch || (unsigned)s >= (unsigned)c.max_pages * KV4_PAGE) return;
-    uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
+    const int groups = hd / 32;
+    const Kv4Line at = kv4_line(c.hkv, groups);
+    const int l = at.l, g = at.g, h = at.h, row = at.row;
+    float kx[8] = {}, vx[8] = {};
+    int b = -1, s = -1;
+    if (row < rows) {
+        b = seq[row], s = slot[row];
+        const T* kr = k + row * k_row + h * k_head + g * 32 + 8 * l;
+        const T* vr = v + row * v_row + h * v_head + g * 32 + 4 * l;
+        kv4_load4(kr, kx);
+        kv4_load4(kr + 4, kx + 4);
+        kv4_load4(vr, vx);
+        kv4_load4(vr + 16, vx + 4);
+    }
+    uint8_t* block = nullptr;
+    if ((unsigned)b < (unsigned)c.batch && (unsigned)s < (unsigned)c.max_pages * KV4_PAGE) block = kv4_page(c, hd, b, s / KV4_PAGE, h);
+    const bool together = kv4_together(at, groups, block != nullptr, b, s);
+    int ke, ve;
+    const uint32_t kc = kv4_encode8<false>(kx, ke), vc = kv4_encode8<true>(vx, ve), vc4 = kv4_exchange(at, groups, vc);
     if (!block) return;
     const int t = s % KV4_PAGE;
-    int ke, ve;
-    const uint32_t kc = kv4_encode8<false>(kx, ke), vc = kv4_encode8<true>(vx, ve);
     *reinterpret_cast<uint32_t*>(block + kv4_key_at(hd, t, g * 32 + 8 * l)) = kc;
+    if (together) *reinterpret_cast<uint32_t*>(block + kv4_val_at(hd, t & ~3, g, 4 * l + at.r)) = vc4;
+    else
 #pragma unroll
-    for (int i = 0; i < 4; ++i) block[kv4_val_at(hd, t, g, 4 * l + i)] = (uint8_t)(vc >> (8 * i));
+        for (int i = 0; i < 4; ++i) block[kv4_val_at(hd, t, g, 4 * l + i)] = (uint8_t)(vc >> (8 * i));
     if (l == 0) {
         block[kv4_key_scale_at(hd, t, g)] = (uint8_t)ke;
         block[kv4_val_scale_at(hd, t, g)] = (uint8_t)ve;
@@ -118,24 +146,29 @@ template <typename T> __device__ __forceinline__ void kv4_store4(T* p, const uin
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache c, int hd, const int* __restrict__ seq, const int* __restrict__ slot, int rows,
                                                        T* __restrict__ k, T* __restrict__ v) {
-    const int l = threadIdx.x & 3, groups = hd / 32;
-    const uint32_t item = (blockIdx.x * 256 + threadIdx.x) >> 2, line = item / groups;
-    const int g = (int)(item % groups), h = (int)(line % c.hkv), row = (int)(line / c.hkv);
-    if (row >= rows) return;
-    const int b = seq[row], s = slot[row], t = s % KV4_PAGE;
-    u32x4_t kk = {}, vv = {};
-    if ((unsigned)b < (unsigned)c.batch && (unsigned)s < (unsigned)c.max_pages * KV4_PAGE) {
-        const uint8_t* block = kv4_page(c, hd, b, s / KV4_PAGE, h);
-        if (block) {
-            const uint32_t kc = *reinterpret_cast<const uint32_t*>(block + kv4_key_at(hd, t, g * 32 + 8 * l));
-            uint32_t vc = 0;
+    const int groups = hd / 32;
+    const Kv4Line at = kv4_line(c.hkv, groups);
+    const int l = at.l, g = at.g, h = at.h, row = at.row;
+    const int b = row < rows ? seq[row] : -1, s = row < rows ? slot[row] : -1, t = s % KV4_PAGE;
+    const uint8_t* block = nullptr;
+    if ((unsigned)b < (unsigned)c.batch && (unsigned)s < (unsigned)c.max_pages * KV4_PAGE) block = kv4_page(c, hd, b, s / KV4_PAGE, h);
+    const bool together = kv4_together(at, groups, block != nullptr, b, s);
+    uint32_t kc = 0, vc = 0;
+    int ke = 0, ve = 0;
+    if (block) {
+        kc = *reinterpret_cast<const uint32_t*>(block + kv4_key_at(hd, t, g * 32 + 8 * l));
+        ke = block[kv4_key_scale_at(hd, t, g)];
+        ve = block[kv4_val_scale_at(hd, t, g)];
+        if (together) vc = *reinterpret_cast<const uint32_t*>(block + kv4_val_at(hd, t & ~3, g, 4 * l + at.r));
+        else
 #pragma unroll
             for (int i = 0; i < 4; ++i) vc |= (uint32_t)block[kv4_val_at(hd, t, g, 4 * l + i)] << (8 * i);
-            kk = q4_decode8(kc, (uint32_t)block[kv4_key_scale_at(hd, t, g)] << 23);
-            vv = q4_decode8(vc, (uint32_t)block[kv4_val_scale_at(hd, t, g)] << 23);
-        }
     }
-    const int64_t o = (int64_t)line * hd + g * 32;
+    const uint32_t vc4 = kv4_exchange(at, groups, vc);
+    if (row >= rows) return;
+    u32x4_t kk = {}, vv = {};
+    if (block) kk = q4_decode8(kc, (uint32_t)ke << 23), vv = q4_decode8(together ? vc4 : vc, (uint32_t)ve << 23);
+    const int64_t o = ((int64_t)row * c.hkv + h) * hd + g * 32;
     kv4_store4(k + o + 8 * l, kk[0], kk[1]);
     kv4_store4(k + o + 8 * l + 4, kk[2], kk[3]);
     // pairs (m, m + 16): the low halves are dims 4 l .. + 3, the high ones those 16 further on

@@ -100,7 +100,7 @@ template <typename T> void w4_run(const W4Plan& p, const W4Args& a, hipStream_t 
 int check_cache(const rsd_kv4_cache* c, const char* what) {
     if (!c || !c->pool || !c->table || !c->kv_len) return fail(RSD_EINVAL, "%s: null cache array", what);
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return fail(RSD_EINVAL, "%s: head_dim %d (32, 64 or 128)", what, c->head_dim);
-    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1 || c->max_pages > INT32_MAX / KV4_PAGE)
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1 || c->max_pages > INT32_MAX / (2 * KV4_PAGE))
         return fail(RSD_EINVAL, "%s: pages %d, kv heads %d, batch %d, pages per sequence %d", what, c->n_pages, c->n_kv_heads, c->batch, c->max_pages);
     if ((int64_t)c->batch * c->n_kv_heads > kMostBlocks / 4) return fail(RSD_EINVAL, "%s: batch %d x %d kv heads", what, c->batch, c->n_kv_heads);
     if (!aligned(c->pool, 16)) return fail(RSD_EINVAL, "%s: the pool is not 16-byte aligned", what);
@@ -113,7 +113,12 @@ Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
 }
 
-struct AttnPlan { int tiles, waves, split, splits; bool many, by_length, fused; int w_cols, w_groups; uint64_t o_bytes, ml_bytes, lse_bytes, w_bytes; uint64_t bytes() const { return o_bytes + ml_bytes + lse_bytes + w_bytes; } };
+struct AttnPlan {
+    int tiles, waves, split, splits, w_cols, w_groups;
+    bool many, by_length, fused;
+    uint64_t o_bytes, ml_bytes, lse_bytes, w_bytes;
+    uint64_t bytes() const { return o_bytes + ml_bytes + lse_bytes + w_bytes; }
+};
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
 //  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
@@ -256,7 +261,7 @@ extern "C" int rsd_kv4_append(const rsd_kv4_cache* c, const void* k, int64_t k_r
     if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "append: type %d, %d rows", dtype, rows);
     if (book && book->positions && !position) return fail(RSD_EINVAL, "append: positions are kept but none are given");
     if (!aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: k or v is not aligned to its type");
-    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 64);
+    const int64_t blocks = ceil_div(ceil_div(rows, 4) * 4 * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "append: %d rows are too many", rows);
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -275,7 +280,7 @@ extern "C" int rsd_kv4_read(const rsd_kv4_cache* c, const int32_t* seq, const in
     if (!k || !v || !seq || !slot) return fail(RSD_EINVAL, "read: null array");
     if (!is_type(dtype) || rows < 1) return fail(RSD_EINVAL, "read: type %d, %d rows", dtype, rows);
     if (!aligned(k, 16) || !aligned(v, 16)) return fail(RSD_EINVAL, "read: k or v is not 16-byte aligned");
-    const int64_t blocks = ceil_div((int64_t)rows * c->n_kv_heads * (c->head_dim / 32), 64);
+    const int64_t blocks = ceil_div(ceil_div(rows, 4) * 4 * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "read: %d rows are too many", rows);
     Launches l;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
