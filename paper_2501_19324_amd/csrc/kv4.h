@@ -983,7 +983,7 @@ __device__ __forceinline__ void kv4_block_scan(int& a, int& b, int& all_a, int& 
 template <bool CACHED>
 __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     extern __shared__ uint32_t kv4_keys[];
-    __shared__ int hist[256], part[2][2][16], found[3], newest_w[16];
+    __shared__ __align__(16) int hist[256][8], part[2][2][16], found[3], newest_w[16];     // eight lanes' counts of a bin side by side
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = blockIdx.x / hkv, h = blockIdx.x % hkv;
     int* plan = a.plan + blockIdx.x * a.list_words();
@@ -1017,18 +1017,22 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     uint32_t key = 0;
     int need = a.budget;                                    // entries still to be kept among those that agree with `key` so far
     for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+        for (int i = tid; i < 2048; i += 1024) hist[i >> 3][i & 7] = 0;
         __syncthreads();
         const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
         for (int s = tid; s < n; s += 1024) {
             const uint32_t u = key_of(s);
-            if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255], 1);
+            if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255][lane & 7], 1);
         }
         __syncthreads();
         if (wave == 0) {                                    // lane l: bins 255 - 4 l .. 252 - 4 l, from the top
             int c[4], mine = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] = hist[255 - 4 * lane - i], mine += c[i];
+            for (int i = 0; i < 4; ++i) {
+                const int4 x = *reinterpret_cast<const int4*>(hist[255 - 4 * lane - i]), y = *reinterpret_cast<const int4*>(&hist[255 - 4 * lane - i][4]);
+                c[i] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+                mine += c[i];
+            }
             int before = mine;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) { const int x = __shfl_up(before, d); if (lane >= d) before += x; }

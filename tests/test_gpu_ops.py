@@ -561,6 +561,29 @@ def test_evict(torch, R, lens, budget, recent, kind, hd, hkv):
         assert np.array_equal(ds.cpu().numpy().view(np.int32), ws.view(np.int32)) and np.array_equal(dp.cpu().numpy(), wp)
 
 
+@pytest.mark.parametrize("n", [12300, 16383, 16384, 16400, 17600])
+def test_evict_from_long_lists(torch, R, n):
+    """Lists whose keys fill the shared memory, and longer ones, which are read again instead."""
+    rng = np.random.default_rng(n)
+    hd, budget, recent, pages = 32, 600, 50, -(-n // 16)
+    pool = rng.integers(0, 256, (pages, 1, 17 * hd)).astype(np.uint8)
+    table = rng.permutation(pages).astype(np.int32)[None]
+    score = np.floor(rng.normal(size=(1, 1, pages * 16)) * 50).astype(np.float32)
+    pos = rng.permutation(pages * 16).astype(np.int32)[None, None]
+    cache = R.Kv4Cache(dev(torch, pool), dev(torch, table), dev(torch, np.array([n], np.int32)))
+    ds, dp = dev(torch, score), dev(torch, pos)
+    _, moves = ref.evict(score[0, 0], pos[0, 0].astype(np.int64), n, budget, recent)
+    want, ws, wp = pool.copy(), score.copy(), pos.copy()
+    for fr, to in moves:
+        for a, c in zip(ref.entry_places(hd, fr % 16), ref.entry_places(hd, to % 16)):
+            want[table[0, to // 16], 0][c] = pool[table[0, fr // 16], 0][a]
+        ws[0, 0, to], wp[0, 0, to] = score[0, 0, fr], pos[0, 0, fr]
+    R.rsd_kv4_evict(cache, ds, dp, budget, recent)
+    assert int(cache.kv_len[0]) == budget
+    assert np.array_equal(cache.pool.cpu().numpy(), want)
+    assert np.array_equal(ds.cpu().numpy(), ws) and np.array_equal(dp.cpu().numpy(), wp)
+
+
 def test_evict_with_lengths_outside_the_table(torch, R):
     rng = np.random.default_rng(20)
     cache, pool, table = make_cache(torch, R, rng, [64, 64], 1, 32)
