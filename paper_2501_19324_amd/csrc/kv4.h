@@ -608,7 +608,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 
 // Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
 // need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
-// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 140 .. 148 us, 0.9 executed PFLOP/s (three
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 137 .. 148 us, 0.9 executed PFLOP/s (three
 // bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 107 us.  (4 % more in fp32 with the sums of a tile one after the other; 225 in the
 // order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 177, bf16 115.
 template <typename T, int HD, int PLANES>
