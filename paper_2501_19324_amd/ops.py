@@ -143,7 +143,7 @@ def _w4_bytes(rows: int, n: int, k: int, dtype: int) -> int:
 
 
 def rsd_w4_pack(w: torch.Tensor) -> W4:
-    """Weights ``[n, k]`` (fp32 or bf16, rows of any stride) in 4 bits."""
+    """Weights ``[n, k]`` (fp32 or bf16, rows k elements apart or more) in 4 bits."""
     lib = _lib or _load()
     if w.dim() != 2 or w.dtype not in _TYPE or w.numel() == 0 or (w.shape[1] > 1 and w.stride(1) != 1):
         _bad(f"w4_pack: {w.dtype} {tuple(w.shape)}, needed fp32 or bf16 [n, k] with contiguous rows")
@@ -151,7 +151,7 @@ def rsd_w4_pack(w: torch.Tensor) -> W4:
     n, k = w.shape
     codes = torch.empty(-(-n // 16), -(-k // 128), 4, 16, 16, dtype=_u8, device=w.device)
     scales = torch.empty(-(-n // 16), -(-k // 512), 4, 16, 4, dtype=_u8, device=w.device)
-    _done(lib.rsd_w4_pack(w.data_ptr(), _TYPE[w.dtype], max(w.stride(0), k), n, k, codes.data_ptr(), scales.data_ptr(), st), lib)
+    _done(lib.rsd_w4_pack(w.data_ptr(), _TYPE[w.dtype], w.stride(0) if n > 1 else k, n, k, codes.data_ptr(), scales.data_ptr(), st), lib)
     return W4(codes, scales, n, k)
 
 
