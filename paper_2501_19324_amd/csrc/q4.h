@@ -85,6 +85,12 @@ template <int PLANES> __device__ __forceinline__ void q4_operand(const float x[8
         }
     }
 }
+// Where lanes of one wave exchange through LDS: its operations stay in the order of the program, whose order this keeps the compiler from
+// changing (no instruction).
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 // maximum over the 16 lanes of a row
 __device__ __forceinline__ float row16_max(float v) {
     row16_moves([&](auto c) { v = fmaxf(v, __uint_as_float(dpp_move<decltype(c)::value>(__float_as_uint(v)))); });

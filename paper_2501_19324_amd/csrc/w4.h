@@ -140,8 +140,10 @@ __global__ __launch_bounds__((64 * w4_few_waves<T, XL>)) void w4_few_kernel(W4Ar
         if (WIDE && t * 128 + 128 > a.k)
 #pragma unroll
             for (int i = 0; i < XL; ++i) w4_tail(x_[i], max(0, t * 128 + k8 * 8 - (a.k - 8)));
+        wave_order();                                       // behind the reads of the tile before
 #pragma unroll
         for (int i = 0; i < XL; ++i) w4_put(x_[i], stage + ((k8 & 3) * 4 + (k8 >> 2)) * XR + i * 4 + (lane >> 4), PLANE);
+        wave_order();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4_t b[P];
