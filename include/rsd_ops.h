@@ -111,7 +111,8 @@ int rsd_kv4_attention(const rsd_kv4_cache *c, const rsd_kv4_attn *a, const rsd_k
                       uint64_t workspace_bytes, void *hip_stream);
 
 /* Eviction: of the entries of every (sequence, kv head) that has more than `budget`, keeps the ones whose position is
- * within `recent` of the newest, then those of the highest score (NaN: lowest), ties to the lower slot, `budget` in all.  Kept entries in slots
+ * within `recent` of the newest, then those of the highest score (NaN: lowest), ties to the lower slot, `budget` in all.  Positions may repeat: where more than
+ * `budget` entries are that new, those of the highest score among them stay.  Kept entries in slots
  * >= budget move, with score and position, into the slots freed below it: the i-th of them in slot order into the i-th
  * freed one.  kv_len becomes min(kv_len, budget); what lies behind it is left as it was.  0 <= recent <= budget, budget >= 1; book with both arrays. */
 uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache *c, int32_t budget);

@@ -1013,42 +1013,57 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(Kv4Evict a, int hkv) {
     if constexpr (CACHED) {
         for (int s = tid; s < n; s += 1024) kv4_keys[s] = kv4_rank_key(score[s], a.recent > 0 && (int)kv4_keys[s] > bound);
     }
-    auto key_of = [&](int s) { return CACHED ? kv4_keys[s] : kv4_rank_key(score[s], a.recent > 0 && pos[s] > bound); };
-    uint32_t key = 0;
-    int need = a.budget;                                    // entries still to be kept among those that agree with `key` so far
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 2048; i += 1024) hist[i >> 3][i & 7] = 0;
-        __syncthreads();
-        const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
-        for (int s = tid; s < n; s += 1024) {
-            const uint32_t u = key_of(s);
-            if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255][lane & 7], 1);
-        }
-        __syncthreads();
-        if (wave == 0) {                                    // lane l: bins 255 - 4 l .. 252 - 4 l, from the top
-            int c[4], mine = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int4 x = *reinterpret_cast<const int4*>(hist[255 - 4 * lane - i]), y = *reinterpret_cast<const int4*>(&hist[255 - 4 * lane - i][4]);
-                c[i] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
-                mine += c[i];
+    // Protected entries are above all others, and alike, until there are more of them than the budget: the selection then ends at their key, and a second
+    // one ranks them by their scores, above all others (0).
+    bool crowded = false;
+    auto rank_of = [&](int s) {
+        const bool safe = a.recent > 0 && pos[s] > bound;
+        return crowded && !safe ? 0u : kv4_rank_key(score[s], safe && !crowded);
+    };
+    auto key_of = [&](int s) { return CACHED ? kv4_keys[s] : rank_of(s); };
+    uint32_t key;
+    int need;                                               // entries still to be kept among those that agree with `key` so far
+    for (;;) {
+        key = 0, need = a.budget;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 2048; i += 1024) hist[i >> 3][i & 7] = 0;
+            __syncthreads();
+            const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
+            for (int s = tid; s < n; s += 1024) {
+                const uint32_t u = key_of(s);
+                if ((u & above) == key) atomicAdd(&hist[(u >> shift) & 255][lane & 7], 1);
             }
-            int before = mine;
+            __syncthreads();
+            if (wave == 0) {                                // lane l: bins 255 - 4 l .. 252 - 4 l, from the top
+                int c[4], mine = 0;
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) { const int x = __shfl_up(before, d); if (lane >= d) before += x; }
-            before -= mine;
+                for (int i = 0; i < 4; ++i) {
+                    const int4 x = *reinterpret_cast<const int4*>(hist[255 - 4 * lane - i]), y = *reinterpret_cast<const int4*>(&hist[255 - 4 * lane - i][4]);
+                    c[i] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+                    mine += c[i];
+                }
+                int before = mine;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (before < need && before + c[i] >= need) found[0] = 255 - 4 * lane - i, found[1] = need - before, found[2] = c[i];
-                before += c[i];
+                for (int d = 1; d < 64; d <<= 1) { const int x = __shfl_up(before, d); if (lane >= d) before += x; }
+                before -= mine;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (before < need && before + c[i] >= need) found[0] = 255 - 4 * lane - i, found[1] = need - before, found[2] = c[i];
+                    before += c[i];
+                }
+            }
+            __syncthreads();
+            key |= (uint32_t)found[0] << shift;
+            need = found[1];
+            if (need == found[2]) {                         // the bin is kept whole: every key from `key` on
+                key -= 1, need = 0;                         // (key > 0: not every entry is kept)
+                break;
             }
         }
-        __syncthreads();
-        key |= (uint32_t)found[0] << shift;
-        need = found[1];
-        if (need == found[2]) {                             // the bin is kept whole: every key from `key` on
-            key -= 1, need = 0;                             // (key > 0: not every entry is kept)
-            break;
+        if (key != 0xFFFFFFFFu || crowded) break;           // (no score has the key of the protected)
+        crowded = true;
+        if constexpr (CACHED) {
+            for (int s = tid; s < n; s += 1024) kv4_keys[s] = rank_of(s);
         }
     }
     // keep: keys above, and the first `need` of those equal to it
