@@ -94,8 +94,8 @@ int rsd_kv4_read(const rsd_kv4_cache *c, const int32_t *seq, const int32_t *slot
 /* Attention of new tokens over the cache (their own entries included).  Sequence b has the rows row_start[b] .. row_start[b + 1] - 1 (dev
  * [batch + 1]; NULL: row b alone), at most max_rows of them (further ones are not computed), and n = min(kv_len[b], max_kv) entries.  Row j of its q rows sees the entries in
  * slots < n - (q - 1 - j).  q, out dev [rows][n_heads][head_dim] with row and head strides; head h reads kv head h / (n_heads /
- * n_kv_heads).  out = softmax(scale q.K) V; a row that sees nothing gives 0.  lse (dev [rows][n_heads] or NULL) = log of the sum of
- * exp(scale q.k), -inf where nothing is seen.  With scores in book (NULL: none) every entry's score grows by the softmax weights it received, summed over the rows
+ * n_kv_heads).  out = softmax(scale q.K) V; a row that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of
+ * the sum of exp(scale q.k), -inf for such rows, which deal out no weight either.  With scores in book (NULL: none) every entry's score grows by the softmax weights it received, summed over the rows
  * and the heads of its group. */
 typedef struct rsd_kv4_attn {
     const void *q;

@@ -177,6 +177,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache c, int hd, const
 }
 
 // ---- attention
+// what becomes of the weights in a launch of the attention: none are asked for; it adds them to the scores; it leaves the logarithms that they are taken with
+enum { KV4_NO_WEIGHTS, KV4_WEIGHTS, KV4_LOGS };
 struct Kv4Attn {
     Kv4Cache c;
     const void* q;
@@ -188,6 +190,7 @@ struct Kv4Attn {
     void* out;
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
+    float* lse2;            // kv4_weight_log of every row and head, for the kernels that add the weights afterwards (KV4_LOGS), or null
     int max_kv, split, splits, hd;
     bool by_length;         // the blocks of the longest sequences go first
     float* part_o;          // [rows][heads][splits][hd], unnormalised
@@ -354,8 +357,11 @@ __device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int sa
         for (int g = 0; g < HD / 32; ++g) v.scale[p][g] &= ~((marks[p][g] >> 7) * 255u);
 }
 
+// The logarithm, to the base 2, of the sum that a column's weights are divided by.  A column that deals out nothing, because it sees nothing or all its scores are
+// -inf, has +inf: its weights are 0 (with -inf, the logarithm of its sum, those of the scores -inf were NaN).
+__device__ __forceinline__ float kv4_weight_log(float top, float total) { return total == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top) + log2f(total); }
 // what a column has gathered, for the join: rows (dims) 4 quad + i of every block d of 16 dims, column lane % 16
-template <typename T>
+template <typename T, int WEIGHTS>
 __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total, int parts) {
     if (parts > 1) {
         const int64_t at = (row * a.heads + qh) * a.splits + blockIdx.z;
@@ -368,6 +374,7 @@ __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh
     if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst) = u32x2_t{f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv)};
     else *reinterpret_cast<f32x4_any_t*>(dst) = acc * inv;
     if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
+    if (WEIGHTS == KV4_LOGS && first) a.lse2[row * a.heads + qh] = kv4_weight_log(top, total);
 }
 
 // One chunk against one tile of columns: scores q.k (masked where `whole` is false), new maximum, probabilities in place of the scores; what was gathered is scaled.
@@ -434,7 +441,7 @@ __device__ __forceinline__ void kv4_seen_weights(f32x4_t& w, int slot, int end) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = slot + i < end ? w[i] : 0.f;
 }
-// Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: lse2 is their logarithm to the base 2, +inf for a
+// Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: lse2 is their kv4_weight_log, +inf for a
 // column that does not exist.  WHOLE: every column sees every entry.
 template <int HD, int PLANES>
 __device__ __forceinline__ void kv4_add_weights(const Kv4Keys<HD>& k, const u32x4_t q[HD / 32][PLANES], bool whole, int there, int slot0, int limit, float factor2,
@@ -483,9 +490,9 @@ __device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
 // 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 172 .. 181 us, 4.7 .. 5 TB/s, what a copy reaches (8 us more in the order of the sequences); 519 vector
 // and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  In that order: 190 us without the requests ahead, 198 with them dropped for a
 // third wave per SIMD.
-// SCORED: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
+// KV4_WEIGHTS: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
 // once more (64 sequences of 128 .. 5120 entries: 51 us instead of 56 in two launches; 256 blocks, so the longest sequence decides).
-template <typename T, int HD, int PLANES, bool SCORED>
+template <typename T, int HD, int PLANES, int WEIGHTS>
 __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, WAVES = 8;
     __shared__ __align__(16) float lds_o[WAVES][G * 2][64][4];
@@ -578,14 +585,14 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
-        if (col < cols) kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, parts);
+        if (col < cols) kv4_finish<T, WEIGHTS>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, parts);
     }
-    if constexpr (SCORED) {
+    if constexpr (WEIGHTS == KV4_WEIGHTS) {
         float best = -INFINITY, total = 0.f;
         for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][lane & 15]);
         const float base = best == -INFINITY ? 0.f : best;
         for (int w = 0; w < waves; ++w) total += __builtin_amdgcn_exp2f(lds_ml[w][0][lane & 15] - base) * lds_ml[w][1][lane & 15];
-        const float lse2 = col < cols ? base + log2f(total) : INFINITY;
+        const float lse2 = col < cols ? kv4_weight_log(best, total) : INFINITY;
         float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
         slot0 = begin + wave * KV4_CHUNK;
         kv4_pages<HD>(a.c, b, head, slot0, page[0], there[0]);
@@ -611,7 +618,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 // Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 137 .. 148 us, 0.9 executed PFLOP/s (three
 // bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 107 us.  (4 % more in fp32 with the sums of a tile one after the other; 225 in the
 // order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 177, bf16 115.
-template <typename T, int HD, int PLANES>
+template <typename T, int HD, int PLANES, int WEIGHTS>
 __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
     typedef typename u32vec<G>::type V;
@@ -739,7 +746,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     if (col >= cols) return;
 #pragma unroll
     for (int d = 0; d < 2 * G; ++d)
-        kv4_finish<T>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum, parts);
+        kv4_finish<T, WEIGHTS>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[d], top, sum, parts);
 }
 
 // Joins the parts of the entries: 16 lanes per (row, head), HD/16 dims each.  The lanes read 16 parts' maxima and sums at once (one after the other they
@@ -783,6 +790,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) st1(dst + i, acc[i] * inv);
     if (l == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+    if (l == 0 && a.lse2) a.lse2[row * a.heads + qh] = kv4_weight_log(best, total);
 }
 
 // Attention weight per entry, added to the accumulated one: the scores are computed a second time (keys are half of the cache; storing a
@@ -804,7 +812,7 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     kv4_pages<HD>(a.c, b, head, slot0, page, there);
     kv4_load_keys<HD>(page, lane, k);
     const int limit = col < cols ? n - (count - 1 - col / a.group) : 0;
-    const float lse2 = col < cols ? a.lse[(int64_t)(r0 + col / a.group) * a.heads + head * a.group + col % a.group] * 1.4426950408889634f : INFINITY;
+    const float lse2 = col < cols ? a.lse2[(int64_t)(r0 + col / a.group) * a.heads + head * a.group + col % a.group] : INFINITY;
     kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
     float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
     for (; slot0 < n; slot0 += step) {
@@ -847,7 +855,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
     auto request = [&]() {                                  // a column beyond the last one keeps the values of the one before it; it sees nothing
         const bool is = col < cols;
         if (is) kv4_load8(at, raw);
-        lse2 = is ? *lse * 1.4426950408889634f : INFINITY;
+        lse2 = is ? *lse : INFINITY;
     };
     auto advance = [&]() {
         const bool over = (head_at += heads_on) >= a.group;
@@ -867,7 +875,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
         col = first, head_at = first % a.group;
         limit = col < cols ? n - (count - 1 - col / a.group) : 0;
         at = static_cast<const T*>(a.q) + (int64_t)(r0 + col / a.group) * a.q_row + (int64_t)(head * a.group + head_at) * a.q_head + quad * (HD / 4) + wave % G * 8;
-        lse = a.lse + (int64_t)(r0 + col / a.group) * a.heads + head * a.group + head_at;
+        lse = a.lse2 + (int64_t)(r0 + col / a.group) * a.heads + head * a.group + head_at;
         request();
         kv4_pages<HD>(a.c, b, head, slot0, page, there);
         kv4_load_keys<HD>(page, lane, raw_k);

@@ -154,8 +154,8 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
-    p.lse_bytes = scored && !a->lse ? up256(lines * 4) : 0;
     p.fused = scored && !p.many && p.tiles == 1 && p.splits == 1;
+    p.lse_bytes = scored && !p.fused ? up256(lines * 4) : 0;
     const int64_t tiles = ceil_div(cols, 16), pairs = (int64_t)c->batch * c->n_kv_heads;
     const int64_t groups = tiles == 1 ? 1 : std::max<int64_t>(1, std::min(4096 / (pairs * ceil_div(chunks, 4)), tiles / 8));
     p.w_cols = (int)(ceil_div(tiles, groups) * 16);
@@ -177,9 +177,11 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
 
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
     const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
-    if (p.many) kv4_attn_many_kernel<T, HD, PLANES><<<grid, 256, 0, st>>>(k);
-    else if (p.fused) kv4_attn_kernel<T, HD, PLANES, true><<<grid, 64 * p.waves, 0, st>>>(k);
-    else kv4_attn_kernel<T, HD, PLANES, false><<<grid, 64 * p.waves, 0, st>>>(k);
+    if (p.many && k.lse2) kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS><<<grid, 256, 0, st>>>(k);
+    else if (p.many) kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS><<<grid, 256, 0, st>>>(k);
+    else if (p.fused) kv4_attn_kernel<T, HD, PLANES, KV4_WEIGHTS><<<grid, 64 * p.waves, 0, st>>>(k);
+    else if (k.lse2) kv4_attn_kernel<T, HD, PLANES, KV4_LOGS><<<grid, 64 * p.waves, 0, st>>>(k);
+    else kv4_attn_kernel<T, HD, PLANES, KV4_NO_WEIGHTS><<<grid, 64 * p.waves, 0, st>>>(k);
     if (p.splits > 1)
         kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
     if (k.book.scores && !p.fused) {
@@ -313,7 +315,8 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.factor2 = (float)(std::fabs((double)a->scale) * 1.4426950408889634);
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
-    k.lse = a->lse ? a->lse : scored ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
+    k.lse = a->lse;
+    k.lse2 = p.lse_bytes ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
     k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.hd = c->head_dim;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);

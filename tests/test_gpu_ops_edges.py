@@ -71,3 +71,77 @@ def test_evict_where_positions_repeat(torch, R, lens, budget, recent, scores):
             pos[b, h] = -1000
             pos[b, h, rng.permutation(n)[:budget + h - 2]] = 2 ** 31 - 1
     check_evict(torch, R, rng, lens, budget, recent, score, pos, 32, hkv)
+
+
+# ---------------------------------------------------------------- attention
+
+def check_columns(cache, pool, table, lens, rows, q, scale, out, lse, score0=None, score1=None, dtype="f32"):
+    """Every (row, head) by itself, with the bounds of test_gpu_ops.check_attention; a column whose scores are all -inf deals out nothing."""
+    hd, hkv = pool.shape[2] // 17, pool.shape[1]
+    group, starts = q.shape[1] // hkv, starts_of(rows)
+    q, out, lse = host(q), host(out), host(lse)
+    for b, n in enumerate(lens):
+        for h in range(hkv):
+            k, v, there = ref.entries(pool, table[b], n, h, hd)
+            total, slack = np.zeros(n), np.zeros(n)
+            for r in range(rows[b]):
+                m = max(n - (rows[b] - 1 - r), 0)          # entries that the row sees
+                for g in range(group):
+                    at = (starts[b] + r, h * group + g)
+                    with np.errstate(invalid="ignore"):
+                        z = scale * (k[:m][there[:m]] @ q[at])
+                    if (z == -np.inf).all():               # nothing is seen, or nothing has a weight
+                        assert not out[at].any() and lse[at] == -np.inf, at
+                        continue
+                    if np.isnan(z).any() or (z == np.inf).any():
+                        assert np.isnan(out[at]).all() and np.isnan(lse[at]), at
+                        total[:m][there[:m]] = np.nan
+                        continue
+                    want, want_lse, weight, mass, spread = ref.attention(q[at][None, None], k[:m], v[:m], there[:m], scale, 1)
+                    rel = 2 * (2 * (3 * hd / 32 + 48) * U * spread + 4 * U * spread) + (n / 64 + 80) * 2 * U + 8 * U
+                    bound = rel * mass + U * np.abs(want) * 4 + 1e-37
+                    if dtype == "bf16":
+                        bound = bound + 2.0 ** -16 * mass + 2.0 ** -8 * np.abs(want)
+                    bad = np.isnan(want[0, 0])             # dims of a value that reads as NaN
+                    assert np.array_equal(np.isnan(out[at]), bad) and np.all((np.abs(out[at] - want[0, 0]) <= bound)[0, 0][~bad]), at
+                    assert abs(lse[at] - want_lse[0, 0]) <= rel + 4 * U * (1 + abs(want_lse[0, 0])), at
+                    total[:m] += weight
+                    slack[:m] += (2 * rel + 8 * U * spread) * weight
+            if score0 is not None:
+                got, was = score1[b, h, :n], score0[b, h, :n]
+                assert np.array_equal(np.isnan(got), np.isnan(total)), (b, h)
+                fine = ~np.isnan(total)
+                assert np.all(np.abs(got - was - total)[fine] <= (slack + 2 * U * np.abs(got) + 1e-37)[fine]), (b, h)
+                assert np.array_equal(score1[b, h, n:], score0[b, h, n:])
+
+
+def columns_with_first_dimension_alike(pool, hd):
+    """Every key gets 1.5 units as its first number: q with an infinity there scores the same infinity everywhere."""
+    for t in range(16):
+        pool[:, :, t * (hd // 8)] = (pool[:, :, t * (hd // 8)] & 0xF0) | 3
+
+
+# heads, kv heads, head dim, lengths, rows: one tile (weights added by the attention kernel itself), in parts, two tiles, many columns, columns in groups
+KINDS = [(8, 2, 64, [128, 70, 3], [1, 1, 1]), (8, 2, 128, [2304, 40], [1, 1]), (28, 2, 32, [64, 133], [1, 2]), (10, 1, 128, [192, 90], [9, 7]),
+         (8, 1, 128, [400, 130], [34, 40])]
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_whose_scores_are_all_minus_infinity(torch, R, heads, hkv, hd, lens, rows, dtype):
+    rng = np.random.default_rng(heads + hd)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    columns_with_first_dimension_alike(pool, hd)
+    cache = R.Kv4Cache(dev(torch, pool), cache.table, cache.kv_len)
+    starts = starts_of(rows)
+    q = rng.normal(size=(int(starts[-1]), heads, hd)).astype(np.float32)
+    q[0, 1, 0] = q[starts[1], heads - 1, 0] = q[-1, 0, 0] = -np.inf
+    q = dev(torch, q).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    scores = dev(torch, rng.random((len(lens), hkv, table.shape[1] * 16)).astype(np.float32))
+    before = host(scores)
+    out, lse = R.rsd_kv4_attention(cache, q, 0.125, row_start=dev(torch, starts), max_rows=max(rows), scores=scores, want_lse=True)
+    check_columns(cache, pool, table, lens, rows, q, 0.125, out, lse, before, host(scores), dtype)
+    assert np.isfinite(host(scores)).all()
+    scores.copy_(dev(torch, before))                       # and without the logarithms asked for
+    again = R.rsd_kv4_attention(cache, q, 0.125, row_start=dev(torch, starts), max_rows=max(rows), scores=scores)
+    assert torch.equal(again, out) and bool(torch.isfinite(scores).all())
