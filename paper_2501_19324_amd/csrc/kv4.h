@@ -185,8 +185,10 @@ struct Kv4Attn {
     int64_t q_row, q_head;
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
     int total_rows, max_rows, heads, group;
-    float factor2;          // |scale| * log2(e): exponents are taken to the base 2
+    float factor2;          // |scale| * log2(e): exponents are taken to the base 2; never 0 or NaN
     bool negative;          // scale < 0: q changes its sign instead
+    bool plain;             // scale is 0 or NaN: q is multiplied by it and factor2 is 1, so that -inf means "not seen" and nothing else (0 times an infinite score is NaN)
+    float scale;
     void* out;
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
@@ -258,6 +260,15 @@ template <int HD> __device__ __forceinline__ void kv4_load_vals(const uint8_t* c
         v.scale[p] = reinterpret_cast<const V*>(page[p] + 16 * HD + HD / 2)[lane >> 4];
     }
 }
+// what q is multiplied by, beside factor2
+__device__ __forceinline__ void kv4_scale_q(const Kv4Attn& a, float x[8]) {
+    if (a.negative)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = -x[i];
+    if (a.plain)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= a.scale;
+}
 // q of one tile of 16 columns as B operands [HD/32][plane]; column c of a (sequence, kv head) is row c / group, head c % group
 template <typename T, int HD, int PLANES>
 __device__ __forceinline__ void kv4_load_q(const Kv4Attn& a, int r0, int count, int head, int col, int lane, u32x4_t q[HD / 32][PLANES]) {
@@ -269,9 +280,7 @@ __device__ __forceinline__ void kv4_load_q(const Kv4Attn& a, int r0, int count, 
     for (int j = 0; j < HD / 32; ++j) kv4_load8(p + j * 8, x[j]);
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) {
-        if (a.negative)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[j][i] = -x[j][i];
+        kv4_scale_q(a, x[j]);
         q4_operand<PLANES>(x[j], q[j]);
     }
 }
@@ -378,7 +387,7 @@ __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh
 }
 
 // One chunk against one tile of columns: scores q.k (masked where `whole` is false), new maximum, probabilities in place of the scores; what was gathered is scaled.
-// factor2 >= 0; top is in units of the exponent.
+// factor2 > 0; top is in units of the exponent.
 template <int NB>
 __device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there, int slot0, int limit, int quad, float factor2, float& top, float& sum, f32x4_t o[NB]) {
     if (!whole) {
@@ -395,7 +404,7 @@ __device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there,
 #pragma unroll
         for (int i = 0; i < 4; ++i) best = fmaxf(best, s[p][i]);
     best = rows4_max(best);
-    best = fmaxf(top, best == -INFINITY ? best : best * factor2);      // (0 * inf is no maximum)
+    best = fmaxf(top, best * factor2);
     // The maximum moves only where some column of the tile passes it by 2^8 (probabilities up to 2^8 lose nothing in 32 bits): seldom after the first chunks.
     if (__any(best > top + 8.f)) {
         const float scale = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.f : best));
@@ -409,9 +418,7 @@ __device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there,
     for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float e = __builtin_fmaf(s[p][i], factor2, -base);
-            if (!whole) e = s[p][i] == -INFINITY ? -INFINITY : e;       // factor2 = 0
-            s[p][i] = __builtin_amdgcn_exp2f(e);
+            s[p][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], factor2, -base));
             sum += s[p][i];
         }
 }
@@ -888,9 +895,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
         for (int c0 = begin; c0 < cols; c0 += 16 * TILES, buf ^= 1) {
             // the readers of this buffer's last contents have passed the barrier of the step in between
             u32x4_t o[PLANES];
-            if (a.negative)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) raw[i] = -raw[i];
+            kv4_scale_q(a, raw);
             q4_operand<PLANES>(raw, o);
 #pragma unroll
             for (int x = 0; x < PLANES; ++x) lds_q[buf][wave][x][lane] = o[x];

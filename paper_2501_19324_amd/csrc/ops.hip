@@ -312,7 +312,9 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.c = dev_cache(c);
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
     k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads, k.group = a->n_heads / c->n_kv_heads;
-    k.factor2 = (float)(std::fabs((double)a->scale) * 1.4426950408889634);
+    k.scale = a->scale;
+    k.plain = !(std::fabs(a->scale) > 0.f);
+    k.factor2 = k.plain ? 1.f : (float)(std::fabs((double)a->scale) * 1.4426950408889634);
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;

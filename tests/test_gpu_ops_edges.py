@@ -145,3 +145,22 @@ def test_rows_whose_scores_are_all_minus_infinity(torch, R, heads, hkv, hd, lens
     scores.copy_(dev(torch, before))                       # and without the logarithms asked for
     again = R.rsd_kv4_attention(cache, q, 0.125, row_start=dev(torch, starts), max_rows=max(rows), scores=scores)
     assert torch.equal(again, out) and bool(torch.isfinite(scores).all())
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS)
+@pytest.mark.parametrize("scale", [0.0, float("nan")])
+def test_factor_of_zero_or_nan(torch, R, heads, hkv, hd, lens, rows, scale):
+    """0 times an infinite score is NaN, whatever the length; rows that see nothing stay empty; else every entry weighs the same."""
+    rng = np.random.default_rng(heads + 2 * hd)
+    lens = lens + [2]
+    rows = rows + [4]                                      # (two of these rows see nothing)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    columns_with_first_dimension_alike(pool, hd)
+    cache = R.Kv4Cache(dev(torch, pool), cache.table, cache.kv_len)
+    starts = starts_of(rows)
+    q = rng.normal(size=(int(starts[-1]), heads, hd)).astype(np.float32)
+    q[0, 0, 0], q[starts[1], 1, 0], q[starts[-2] - 1, heads - 1, 0] = -np.inf, np.inf, -np.inf
+    q = dev(torch, q)
+    scores = torch.zeros(len(lens), hkv, table.shape[1] * 16, device="cuda")
+    out, lse = R.rsd_kv4_attention(cache, q, scale, row_start=dev(torch, starts), max_rows=max(rows), scores=scores, want_lse=True)
+    check_columns(cache, pool, table, lens, rows, q, scale, out, lse, np.zeros(scores.shape), host(scores))
