@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <type_traits>
 
 #include "rsd_ops.h"
 #include "q4.h"
@@ -22,12 +23,21 @@ int fail(int code, const char* fmt, ...) {
     va_end(ap);
     return code;
 }
-// the launches before this call: an error that an earlier, unrelated call left behind is not this call's
-struct Launches {
-    Launches() { (void)hipGetLastError(); }
+// The launches of a call, by the status that each returns: the runtime's last error may be one that the caller has not read yet, and stays.
+class Launches {
+    hipStream_t st_;
+    hipError_t first_ = hipSuccess;
+public:
+    explicit Launches(void* stream) : st_(static_cast<hipStream_t>(stream)) {}
+    template <typename... P> void run(void (*kernel)(P...), dim3 grid, unsigned threads, size_t lds, std::common_type_t<P>... args) {
+        if (first_ != hipSuccess) return;
+        void* at[] = {&args...};
+        first_ = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, lds, st_);
+    }
     int done(const char* what) {
-        const hipError_t e = hipGetLastError();
-        return e == hipSuccess ? RSD_OK : fail(RSD_EHIP, "%s: %s", what, hipGetErrorString(e));
+        if (first_ == hipSuccess) return RSD_OK;
+        (void)hipGetLastError();                            // reported here
+        return fail(RSD_EHIP, "%s: %s", what, hipGetErrorString(first_));
     }
 };
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -73,26 +83,26 @@ W4Plan w4_plan(int rows, int n, int k, int dtype) {
     return p;
 }
 
-template <typename T> void w4_launch(const W4Plan& p, const W4Args& a, hipStream_t st) {
+template <typename T> void w4_launch(const W4Plan& p, const W4Args& a, Launches& l) {
     const bool wide = a.k >= 8;
     if (p.few) {
         const unsigned grid = (unsigned)ceil_div(p.nt, p.ntile), threads = 64 * p.waves;
-        if (!wide) w4_few_kernel<T, 2, 4, false><<<grid, threads, 0, st>>>(a);
-        else if (a.rows <= 4) w4_few_kernel<T, 2, 1, true><<<grid, threads, 0, st>>>(a);
-        else if (p.ntile == 2) w4_few_kernel<T, 2, 4, true><<<grid, threads, 0, st>>>(a);
-        else w4_few_kernel<T, 4, 4, true><<<grid, threads, 0, st>>>(a);
+        if (!wide) l.run(w4_few_kernel<T, 2, 4, false>, grid, threads, 0, a);
+        else if (a.rows <= 4) l.run(w4_few_kernel<T, 2, 1, true>, grid, threads, 0, a);
+        else if (p.ntile == 2) l.run(w4_few_kernel<T, 2, 4, true>, grid, threads, 0, a);
+        else l.run(w4_few_kernel<T, 4, 4, true>, grid, threads, 0, a);
         return;
     }
     const unsigned grid = (unsigned)(p.splits * ceil_div(p.nt, 16) * ceil_div(a.rows, p.xt * 16));
-    if (!wide) w4_many_kernel<T, 1, false><<<grid, 256, 0, st>>>(a);
-    else if (p.xt == 1) w4_many_kernel<T, 1, true><<<grid, 256, 0, st>>>(a);
-    else if (p.xt == 2) w4_many_kernel<T, 2, true><<<grid, 256, 0, st>>>(a);
-    else if constexpr (sizeof(T) == 2) w4_many_kernel<T, 4, true><<<grid, 256, 0, st>>>(a);
+    if (!wide) l.run(w4_many_kernel<T, 1, false>, grid, 256, 0, a);
+    else if (p.xt == 1) l.run(w4_many_kernel<T, 1, true>, grid, 256, 0, a);
+    else if (p.xt == 2) l.run(w4_many_kernel<T, 2, true>, grid, 256, 0, a);
+    else if constexpr (sizeof(T) == 2) l.run(w4_many_kernel<T, 4, true>, grid, 256, 0, a);
 }
-template <typename T> void w4_run(const W4Plan& p, const W4Args& a, hipStream_t st) {
-    w4_launch<T>(p, a, st);
+template <typename T> void w4_run(const W4Plan& p, const W4Args& a, Launches& l) {
+    w4_launch<T>(p, a, l);
     if (p.splits > 1)
-        w4_sum_kernel<T><<<(unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, st>>>(a);
+        l.run(w4_sum_kernel<T>, (unsigned)ceil_div((int64_t)a.rows * (w4_padded(a.n) / 4), 256), 256, 0, a);
 }
 
 // ---- the cache
@@ -175,31 +185,31 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
     return RSD_OK;
 }
 
-template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, hipStream_t st) {
+template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, Launches& l) {
     const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
-    if (p.many && k.lse2) kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS><<<grid, 256, 0, st>>>(k);
-    else if (p.many) kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS><<<grid, 256, 0, st>>>(k);
-    else if (p.fused) kv4_attn_kernel<T, HD, PLANES, KV4_WEIGHTS><<<grid, 64 * p.waves, 0, st>>>(k);
-    else if (k.lse2) kv4_attn_kernel<T, HD, PLANES, KV4_LOGS><<<grid, 64 * p.waves, 0, st>>>(k);
-    else kv4_attn_kernel<T, HD, PLANES, KV4_NO_WEIGHTS><<<grid, 64 * p.waves, 0, st>>>(k);
+    if (p.many && k.lse2) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS>, grid, 256, 0, k);
+    else if (p.many) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, grid, 256, 0, k);
+    else if (p.fused) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_WEIGHTS>, grid, 64 * p.waves, 0, k);
+    else if (k.lse2) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_LOGS>, grid, 64 * p.waves, 0, k);
+    else l.run(kv4_attn_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, grid, 64 * p.waves, 0, k);
     if (p.splits > 1)
-        kv4_join_kernel<T, HD><<<(unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, st>>>(k);
+        l.run(kv4_join_kernel<T, HD>, (unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, k);
     if (k.book.scores && !p.fused) {
         const int64_t n = std::min<int64_t>(k.max_kv, (int64_t)k.c.max_pages * KV4_PAGE);
         const int64_t pairs = (int64_t)k.c.batch * k.c.hkv, chunks = ceil_div(n, 4 * KV4_CHUNK);
         if (n > 0 && (int64_t)k.max_rows * k.group <= 16)
-            kv4_weight_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, (unsigned)std::min(chunks, ceil_div(1024, pairs))), 256, 0, st>>>(k);
+            l.run(kv4_weight_kernel<T, HD, PLANES>, dim3((unsigned)pairs, (unsigned)std::min(chunks, ceil_div(1024, pairs))), 256, 0, k);
         else if (n > 0) {
             const unsigned y = (unsigned)std::min<int64_t>(chunks, 32768);
-            kv4_weight_many_kernel<T, HD, PLANES><<<dim3((unsigned)pairs, y, (unsigned)p.w_groups), 256, 0, st>>>(k);
-            if (p.w_groups > 1) kv4_weight_sum_kernel<<<dim3((unsigned)pairs, y), 256, 0, st>>>(k);
+            l.run(kv4_weight_many_kernel<T, HD, PLANES>, dim3((unsigned)pairs, y, (unsigned)p.w_groups), 256, 0, k);
+            if (p.w_groups > 1) l.run(kv4_weight_sum_kernel, dim3((unsigned)pairs, y), 256, 0, k);
         }
     }
 }
-template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, hipStream_t st) {
-    if (hd == 32) attn_run<T, 32, PLANES>(k, p, st);
-    else if (hd == 64) attn_run<T, 64, PLANES>(k, p, st);
-    else attn_run<T, 128, PLANES>(k, p, st);
+template <typename T, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, int hd, Launches& l) {
+    if (hd == 32) attn_run<T, 32, PLANES>(k, p, l);
+    else if (hd == 64) attn_run<T, 64, PLANES>(k, p, l);
+    else attn_run<T, 128, PLANES>(k, p, l);
 }
 uint64_t up4(uint64_t n) { return (n + 3) & ~3ull; }
 // the most entries of a list that can move, in whole vectors
@@ -218,12 +228,11 @@ extern "C" int rsd_w4_pack(const void* w, int32_t dtype, int64_t ld, int32_t n, 
     const int nt = (int)ceil_div(n, 16), kt = (int)ceil_div(k, 128), ks = (int)ceil_div(k, 512);
     const int64_t blocks = (int64_t)nt * ks * 16;        // 16 rows x 16 groups x 16 lanes of every 512 columns
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "w4_pack: [%d][%d] is too large", n, k);
-    Launches l;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    Launches l(hip_stream);
     if (dtype == RSD_F32)
-        w4_pack_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(static_cast<const float*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+        l.run(w4_pack_kernel<float>, (unsigned)blocks, 256, 0, static_cast<const float*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
     else
-        w4_pack_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(static_cast<const bf16_t*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+        l.run(w4_pack_kernel<bf16_t>, (unsigned)blocks, 256, 0, static_cast<const bf16_t*>(w), ld, n, k, nt, kt, ks, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
     return l.done("w4_pack");
 }
 
@@ -249,9 +258,9 @@ extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* 
                     (unsigned long long)workspace_bytes, (unsigned long long)p.part_bytes);
     const W4Args a{static_cast<const u32x4_t*>(w->codes), static_cast<const uint32_t*>(w->scales), w->n, w->k, p.nt, p.kt, p.ks, x, ldx, rows, y, ldy,
                    p.splits > 1 ? static_cast<float*>(workspace) : nullptr, p.tiles, p.splits};
-    Launches l;
-    if (dtype == RSD_F32) w4_run<float>(p, a, static_cast<hipStream_t>(hip_stream));
-    else w4_run<bf16_t>(p, a, static_cast<hipStream_t>(hip_stream));
+    Launches l(hip_stream);
+    if (dtype == RSD_F32) w4_run<float>(p, a, l);
+    else w4_run<bf16_t>(p, a, l);
     return l.done("w4_linear");
 }
 
@@ -265,13 +274,12 @@ extern "C" int rsd_kv4_append(const rsd_kv4_cache* c, const void* k, int64_t k_r
     if (!aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: k or v is not aligned to its type");
     const int64_t blocks = ceil_div(ceil_div(rows, 4) * 4 * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "append: %d rows are too many", rows);
-    Launches l;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    Launches l(hip_stream);
     if (dtype == RSD_F32)
-        kv4_append_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const float*>(k), k_row, k_head,
+        l.run(kv4_append_kernel<float>, (unsigned)blocks, 256, 0, dev_cache(c), c->head_dim, static_cast<const float*>(k), k_row, k_head,
                                                                    static_cast<const float*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
     else
-        kv4_append_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, static_cast<const bf16_t*>(k), k_row, k_head,
+        l.run(kv4_append_kernel<bf16_t>, (unsigned)blocks, 256, 0, dev_cache(c), c->head_dim, static_cast<const bf16_t*>(k), k_row, k_head,
                                                                     static_cast<const bf16_t*>(v), v_row, v_head, seq, slot, position, rows, dev_book(book));
     return l.done("append");
 }
@@ -284,10 +292,9 @@ extern "C" int rsd_kv4_read(const rsd_kv4_cache* c, const int32_t* seq, const in
     if (!aligned(k, 16) || !aligned(v, 16)) return fail(RSD_EINVAL, "read: k or v is not 16-byte aligned");
     const int64_t blocks = ceil_div(ceil_div(rows, 4) * 4 * c->n_kv_heads * (c->head_dim / 32), 64);
     if (blocks > kMostBlocks) return fail(RSD_EINVAL, "read: %d rows are too many", rows);
-    Launches l;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (dtype == RSD_F32) kv4_read_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, seq, slot, rows, static_cast<float*>(k), static_cast<float*>(v));
-    else kv4_read_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(dev_cache(c), c->head_dim, seq, slot, rows, static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
+    Launches l(hip_stream);
+    if (dtype == RSD_F32) l.run(kv4_read_kernel<float>, (unsigned)blocks, 256, 0, dev_cache(c), c->head_dim, seq, slot, rows, static_cast<float*>(k), static_cast<float*>(v));
+    else l.run(kv4_read_kernel<bf16_t>, (unsigned)blocks, 256, 0, dev_cache(c), c->head_dim, seq, slot, rows, static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
     return l.done("read");
 }
 
@@ -326,9 +333,9 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.w_cols = p.w_cols, k.w_groups = p.w_groups;
     k.w_slots = ceil_div(std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KV4_PAGE), KV4_CHUNK) * KV4_CHUNK;
     k.part_w = reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes + p.lse_bytes);
-    Launches l;
-    if (a->dtype == RSD_F32) attn_run<float, 3>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
-    else attn_run<bf16_t, 1>(k, p, c->head_dim, static_cast<hipStream_t>(hip_stream));
+    Launches l(hip_stream);
+    if (a->dtype == RSD_F32) attn_run<float, 3>(k, p, c->head_dim, l);
+    else attn_run<bf16_t, 1>(k, p, c->head_dim, l);
     return l.done("attention");
 }
 
@@ -347,16 +354,15 @@ extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, i
         return fail(RSD_EINVAL, "evict: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
     const Kv4Evict e{dev_cache(c), dev_book(book), budget, recent, static_cast<int*>(workspace), evict_moves(c, budget)};
     if (e.moves == 0) return RSD_OK;                     // no sequence can hold more than the budget
-    Launches l;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    Launches l(hip_stream);
     const unsigned lists = (unsigned)(c->batch * c->n_kv_heads);
     const int64_t slots = (int64_t)c->max_pages * KV4_PAGE;
-    if (slots <= 16384) kv4_select_kernel<true><<<lists, 1024, (size_t)slots * 4, st>>>(e, c->n_kv_heads);
-    else kv4_select_kernel<false><<<lists, 1024, 0, st>>>(e, c->n_kv_heads);
+    if (slots <= 16384) l.run(kv4_select_kernel<true>, lists, 1024, (size_t)slots * 4, e, c->n_kv_heads);
+    else l.run(kv4_select_kernel<false>, lists, 1024, 0, e, c->n_kv_heads);
     // four pages to a block at a time; at most 64 blocks to a list, which then go on with the next 256
     const dim3 grid(lists, (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(budget, KV4_PAGE), 4)));
-    if (c->head_dim == 32) kv4_move_kernel<32><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
-    else if (c->head_dim == 64) kv4_move_kernel<64><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
-    else kv4_move_kernel<128><<<grid, 256, 0, st>>>(e, c->n_kv_heads);
+    if (c->head_dim == 32) l.run(kv4_move_kernel<32>, grid, 256, 0, e, c->n_kv_heads);
+    else if (c->head_dim == 64) l.run(kv4_move_kernel<64>, grid, 256, 0, e, c->n_kv_heads);
+    else l.run(kv4_move_kernel<128>, grid, 256, 0, e, c->n_kv_heads);
     return l.done("evict");
 }

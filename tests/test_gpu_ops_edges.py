@@ -164,3 +164,25 @@ def test_factor_of_zero_or_nan(torch, R, heads, hkv, hd, lens, rows, scale):
     scores = torch.zeros(len(lens), hkv, table.shape[1] * 16, device="cuda")
     out, lse = R.rsd_kv4_attention(cache, q, scale, row_start=dev(torch, starts), max_rows=max(rows), scores=scores, want_lse=True)
     check_columns(cache, pool, table, lens, rows, q, scale, out, lse, np.zeros(scores.shape), host(scores))
+
+
+# ---------------------------------------------------------------- arguments
+
+def test_an_error_the_caller_has_not_read_stays(torch, R):
+    """The runtime's last error belongs to the caller's own call before; an operator that succeeds neither reports nor clears it."""
+    import ctypes as C
+    rng = np.random.default_rng(3)
+    cache, pool, table = make_cache(torch, R, rng, [20], 1, 32)
+    x, idx = torch.ones(1, 1, 32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    hip = C.CDLL([line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line][0])
+    assert hip.hipGetLastError() == 0
+    refused = hip.hipSetDevice(10_000)
+    assert refused != 0 and hip.hipPeekAtLastError() == refused
+    try:
+        R.rsd_kv4_append(cache, x, x, idx, idx)
+        assert hip.hipPeekAtLastError() == refused
+    finally:
+        hip.hipGetLastError()
+    k, v = R.rsd_kv4_read(cache, idx, idx)
+    assert bool((k == 1).all()) and bool((v == 1).all())
