@@ -9,7 +9,8 @@
  *    Device memory that a call needs beside its arguments is a workspace of the caller's, 256-byte aligned, of at least the size the
  *    matching ..._workspace function returns for the same sizes (0: none).  It is free again once the stream has passed the
  *    call; calls that may run at the same time need one each.
- *  - Strides count elements.  The innermost dimension of every array is contiguous.
+ *  - Strides count elements.  The innermost dimension of every array is contiguous.  Rows of q, k and v may overlap; rows of an array that a call
+ *    writes to may not: the products, the attention and the eviction refuse such arrays.
  *  - Every entry point returns RSD_OK (0), RSD_EINVAL (bad shape or argument; nothing was enqueued) or RSD_EHIP;
  *    rsd_op_last_error() is the text of the calling thread's last failure.  Nothing aborts or throws.
  *  - Values that live on the device (lengths, tables, row numbers) cannot be checked before the launch.  The kernels check them: a

@@ -47,6 +47,22 @@ uint64_t up256(uint64_t n) { return (n + 255) & ~255ull; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kMostBlocks = 1ll << 22;      // blocks of at most 512 threads: a launch counts threads in 32 bits per dimension
 
+// Pieces of `len` elements at i s0 + j s1, i < n0, j < n1: whether two of them share an element.  Mostly one stride passes the other's pieces, which is seen
+// at once; else every distance in the shorter dimension is set against the nearest ones in the other.
+bool pieces_overlap(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t len) {
+    typedef __int128 wide;
+    if (n0 > n1) std::swap(n0, n1), std::swap(s0, s1);
+    const wide a = s0 < 0 ? -(wide)s0 : s0, b = s1 < 0 ? -(wide)s1 : s1;      // distances count in both directions
+    if (n0 == 1) return n1 > 1 && b < len;
+    if (a < len || b < len) return true;
+    if (b >= (n0 - 1) * a + len || a >= (n1 - 1) * b + len) return false;
+    for (wide i = 1; i < n0; ++i) {
+        const wide j = i * a / b;
+        if ((j < n1 && i * a - j * b < len) || (j + 1 < n1 && (j + 1) * b - i * a < len)) return true;
+    }
+    return false;
+}
+
 // ---- products with 4-bit weights
 
 struct W4Plan { int nt, kt, ks; bool few; int ntile, waves, xt, splits, tiles; uint64_t part_bytes; };
@@ -121,6 +137,11 @@ Kv4Cache dev_cache(const rsd_kv4_cache* c) {
 }
 Kv4Book dev_book(const rsd_kv4_book* b) {
     return b ? Kv4Book{b->scores, b->positions, b->score_b, b->score_h, b->position_b, b->position_h} : Kv4Book{};
+}
+
+// what is known of the entries, where it is changed: a list for each (sequence, kv head)
+bool lists_overlap(const rsd_kv4_cache* c, int64_t batch_stride, int64_t head_stride) {
+    return pieces_overlap(c->batch, batch_stride, c->n_kv_heads, head_stride, (int64_t)c->max_pages * KV4_PAGE);
 }
 
 struct AttnPlan {
@@ -310,6 +331,10 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     if (!a->q || !a->out) return fail(RSD_EINVAL, "attention: null array");
     if (!aligned(a->q, size_of(a->dtype)) || !aligned(a->out, size_of(a->dtype))) return fail(RSD_EINVAL, "attention: q or out is not aligned to its type");
     const bool scored = book && book->scores;
+    if (pieces_overlap(a->rows, a->out_row, a->n_heads, a->out_head, c->head_dim))
+        return fail(RSD_EINVAL, "attention: rows of out overlap (strides %lld, %lld)", (long long)a->out_row, (long long)a->out_head);
+    if (scored && lists_overlap(c, book->score_b, book->score_h))
+        return fail(RSD_EINVAL, "attention: lists of scores overlap (strides %lld, %lld)", (long long)book->score_b, (long long)book->score_h);
     const AttnPlan p = attn_plan(c, a, scored);
     const uint64_t need = p.bytes();
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
@@ -349,6 +374,9 @@ extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, i
     if (int rc = check_cache(c, "evict")) return rc;
     if (!book || !book->scores || !book->positions) return fail(RSD_EINVAL, "evict: scores and positions are needed");
     if (budget < 1 || recent < 0 || recent > budget) return fail(RSD_EINVAL, "evict: budget %d, recent %d", budget, recent);
+    if (lists_overlap(c, book->score_b, book->score_h) || lists_overlap(c, book->position_b, book->position_h))
+        return fail(RSD_EINVAL, "evict: lists of scores or positions overlap (strides %lld, %lld and %lld, %lld)", (long long)book->score_b, (long long)book->score_h,
+                    (long long)book->position_b, (long long)book->position_h);
     const uint64_t need = rsd_kv4_evict_workspace(c, budget);
     if (workspace_bytes < need || !workspace || !aligned(workspace, 256))
         return fail(RSD_EINVAL, "evict: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);

@@ -35,3 +35,77 @@ def test_weights_whose_rows_overlap_are_refused(on_host, shape, strides):
     import torch
     w = torch.zeros(4096).as_strided(shape, strides)
     assert refused(lambda: on_host.rsd_w4_pack(w), on_host)
+
+
+def _cache(ops, batch=3, n_kv_heads=2, max_pages=4):
+    return ops._Cache(4096, 4096, 4096, 8, n_kv_heads, 64, batch, max_pages)
+
+
+def _attn(ops, **kw):
+    a = dict(q=1 << 20, out=1 << 24, lse=None, q_row=512, q_head=64, out_row=512, out_head=64, row_start=4096, rows=3, max_rows=2, n_heads=8, max_kv=64, dtype=1, scale=0.1)
+    a.update(kw)
+    return ops._Attn(**a)
+
+
+def _no_workspace(lib, call):
+    """What a call without room for its workspace says: the last refusal before a launch."""
+    assert call() == -1
+    return b"workspace" in lib.rsd_op_last_error()
+
+
+# rows, heads, strides of both in elements, pieces of 64
+STRIDES = [(3, 8, 512, 64), (3, 8, 64, 192), (3, 8, 1000, 70), (1, 8, 0, 64), (3, 1, 64, 0), (1, 1, 0, 0), (3, 8, -512, 64), (2, 2, 192, 128), (3, 2, 128, 192), (4, 3, 150, 230),
+           (3, 8, 0, 64), (3, 8, 512, 0), (3, 8, 511, 64), (3, 8, 512, 63), (3, 8, 64, 64), (3, 8, 64, 128), (3, 8, 128, 192), (2, 8, 400, 100), (3, 1, 63, 0), (1, 2, 0, -63),
+           (8, 3, 64, 500)]
+
+
+def _share(rows, heads, row, head, length):
+    taken = set()
+    for r in range(rows):
+        for h in range(heads):
+            piece = set(range(r * row + h * head, r * row + h * head + length))
+            if taken & piece:
+                return True
+            taken |= piece
+    return False
+
+
+@pytest.mark.parametrize("rows,heads,row,head", STRIDES)
+def test_outputs_whose_rows_overlap_are_refused(lib, rows, heads, row, head):
+    """Blocks would write to one place in any order."""
+    from paper_2501_19324_amd import ops
+    # (accepted: as far as the workspace, which is not there)
+    c = _cache(ops, batch=1, n_kv_heads=1, max_pages=512)
+    a = _attn(ops, rows=rows, n_heads=heads, out_row=row, out_head=head, max_kv=8192, max_rows=rows)
+    good = _no_workspace(lib, lambda: lib.rsd_kv4_attention(C.byref(c), C.byref(a), None, None, 0, None))
+    assert good != _share(rows, heads, row, head, 64), lib.rsd_op_last_error()
+
+
+@pytest.mark.parametrize("batch,heads,b,h", STRIDES)
+def test_lists_that_overlap_are_refused(lib, batch, heads, b, h):
+    from paper_2501_19324_amd import ops
+    c, fine = _cache(ops, batch, heads, 4), (heads * 64, 64)
+    ok = not _share(batch, heads, b, h, 64)
+    for scores, positions in (((b, h), fine), (fine, (b, h))):
+        book = ops._Book(1 << 20, 1 << 24, *scores, *positions)
+        assert _no_workspace(lib, lambda: lib.rsd_kv4_evict(C.byref(c), C.byref(book), 5, 0, None, 0, None)) == ok
+    # attention: scores alone; positions are not looked at
+    c = _cache(ops, batch, heads, 4)
+    a = _attn(ops, rows=batch, n_heads=17 * heads, out_row=17 * heads * 64, max_kv=64, max_rows=batch)
+    book = ops._Book(1 << 20, None, b, h, 0, 0)
+    assert _no_workspace(lib, lambda: lib.rsd_kv4_attention(C.byref(c), C.byref(a), C.byref(book), None, 0, None)) == ok
+
+
+def test_expanded_outputs_are_refused_by_the_binding(on_host):
+    import torch
+    ops = on_host
+    cache = ops.Kv4Cache(torch.zeros(8, 2, 17 * 64, dtype=torch.uint8), torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32))
+    q = torch.zeros(3, 4, 64)
+    lists, pos = torch.zeros(3, 2, 64), torch.zeros(3, 2, 64, dtype=torch.int32)
+    for out in (q[:1].clone().expand(3, 4, 64), q[:, :1].clone().expand(3, 4, 64)):
+        assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, out=out), ops)
+    for bad in (lists[:1].expand(3, 2, 64), lists[:, :1].expand(3, 2, 64)):
+        assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, scores=bad), ops)
+        assert refused(lambda: ops.rsd_kv4_evict(cache, bad, pos, 8), ops)
+    for bad in (pos[:1].expand(3, 2, 64), pos[:, :1].expand(3, 2, 64)):
+        assert refused(lambda: ops.rsd_kv4_evict(cache, lists, bad, 8), ops)
