@@ -63,6 +63,31 @@ bool pieces_overlap(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t len)
     return false;
 }
 
+// Two arrays of one type, pieces at i s0 + j s1 of each (i < n0, j < n1), of `len` elements
+struct Pieces { const void* at; int64_t s0, s1, len; };
+// Whether they share an element.  Views of one buffer (heads of q beside those of out) mostly have the same s0; where that differs, arrays that lie between
+// each other's ends count as sharing.
+bool share_memory(Pieces p, Pieces q, int64_t n0, int64_t n1, size_t size) {
+    typedef __int128 wide;
+    if (n0 == 1) p.s0 = q.s0 = 0;
+    if (n1 == 1) p.s1 = q.s1 = 0;
+    const wide d = ((wide)reinterpret_cast<uintptr_t>(q.at) - (wide)reinterpret_cast<uintptr_t>(p.at)) / (int64_t)size;
+    auto low = [&](const Pieces& x) { return std::min<wide>(0, (wide)(n0 - 1) * x.s0) + std::min<wide>(0, (wide)(n1 - 1) * x.s1); };
+    auto high = [&](const Pieces& x) { return std::max<wide>(0, (wide)(n0 - 1) * x.s0) + std::max<wide>(0, (wide)(n1 - 1) * x.s1) + x.len; };
+    if (d + low(q) >= high(p) || d + high(q) <= low(p)) return false;
+    if (p.s0 != q.s0) return true;
+    const wide s0 = p.s0 < 0 ? -(wide)p.s0 : p.s0;         // distances in i count in both directions
+    auto floor_div = [](wide a, wide b) { return a / b - (a % b < 0); };
+    for (int64_t j = 0; j < n1; ++j)
+        for (int64_t i = 0; i < n1; ++i) {
+            // q's piece starts `c` behind p's, and a multiple of s0: somewhere between -q.len and p.len?
+            const wide c = d + (wide)j * q.s1 - (wide)i * p.s1;
+            if (s0 == 0 ? c > -q.len && c < p.len
+                        : std::max<wide>(-floor_div(q.len - 1 + c, s0), 1 - n0) <= std::min<wide>(floor_div(p.len - 1 - c, s0), n0 - 1)) return true;
+        }
+    return false;
+}
+
 // ---- products with 4-bit weights
 
 struct W4Plan { int nt, kt, ks; bool few; int ntile, waves, xt, splits, tiles; uint64_t part_bytes; };
@@ -336,6 +361,11 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     if (scored && lists_overlap(c, book->score_b, book->score_h))
         return fail(RSD_EINVAL, "attention: lists of scores overlap (strides %lld, %lld)", (long long)book->score_b, (long long)book->score_h);
     const AttnPlan p = attn_plan(c, a, scored);
+    // A block has read its columns of q before it writes them, so out may be q itself; but weights that are added by a kernel of their own need q once more.
+    const bool same = a->out == a->q && (a->rows == 1 || a->out_row == a->q_row) && (a->n_heads == 1 || a->out_head == a->q_head);
+    if (same ? scored && !p.fused
+             : share_memory({a->q, a->q_row, a->q_head, c->head_dim}, {a->out, a->out_row, a->out_head, c->head_dim}, a->rows, a->n_heads, size_of(a->dtype)))
+        return fail(RSD_EINVAL, "attention: out shares memory with q%s", same ? ", which the weights need again" : "");
     const uint64_t need = p.bytes();
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
         return fail(RSD_EINVAL, "attention: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);

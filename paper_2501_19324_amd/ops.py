@@ -287,7 +287,7 @@ def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Option
     Without ``row_start`` row b is sequence b's newest token; with it (``[batch + 1]`` int32) sequence b has the rows
     ``row_start[b] .. row_start[b + 1] - 1``, at most ``max_rows``, and each sees one entry more than the row before it.  ``max_kv`` bounds
     ``kv_len`` (default: what the table can hold); the tighter it is, the better the work is dealt.  ``scores`` ``[batch, n_kv_heads, slots]``
-    grows by the weight each entry received.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
+    grows by the weight each entry received.  ``out`` may be ``q`` itself, without ``scores``.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
     lib = _lib or _load()
     c, pool, st = _cache(cache)
     t = _TYPE.get(q.dtype)

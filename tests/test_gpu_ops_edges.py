@@ -186,3 +186,28 @@ def test_an_error_the_caller_has_not_read_stays(torch, R):
         hip.hipGetLastError()
     k, v = R.rsd_kv4_read(cache, idx, idx)
     assert bool((k == 1).all()) and bool((v == 1).all())
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS)
+def test_out_may_be_q_where_no_weights_need_it_again(torch, R, heads, hkv, hd, lens, rows):
+    rng = np.random.default_rng(heads + 7 * hd)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    starts = dev(torch, starts_of(rows))
+    q = dev(torch, rng.normal(size=(sum(rows), heads, hd)).astype(np.float32))
+    kw = dict(row_start=starts, max_rows=max(rows))
+    scores = torch.zeros(len(lens), hkv, table.shape[1] * 16, device="cuda")
+    want = R.rsd_kv4_attention(cache, q, 0.2, scores=scores, **kw)
+    got = q.clone()
+    assert R.rsd_kv4_attention(cache, got, 0.2, out=got, **kw).data_ptr() == got.data_ptr() and torch.equal(got, want)
+    got, sums = q.clone(), torch.zeros_like(scores)
+    try:
+        R.rsd_kv4_attention(cache, got, 0.2, out=got, scores=sums, **kw)
+    except R.RsdError:
+        assert torch.equal(got, q) and not bool(sums.any())
+    else:
+        assert torch.equal(got, want) and torch.equal(sums, scores)
+    with pytest.raises(R.RsdError):                        # a row further on
+        R.rsd_kv4_attention(cache, got[1:], 0.2, out=got[:-1], **kw)
+    both = torch.zeros(sum(rows), 2 * heads, hd, device="cuda")         # beside each other in one buffer
+    both[:, ::2] = q
+    assert torch.equal(R.rsd_kv4_attention(cache, both[:, ::2], 0.2, out=both[:, 1::2], scores=sums, **kw), want) and torch.equal(both[:, ::2], q)

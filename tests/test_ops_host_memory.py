@@ -109,3 +109,32 @@ def test_expanded_outputs_are_refused_by_the_binding(on_host):
         assert refused(lambda: ops.rsd_kv4_evict(cache, bad, pos, 8), ops)
     for bad in (pos[:1].expand(3, 2, 64), pos[:, :1].expand(3, 2, 64)):
         assert refused(lambda: ops.rsd_kv4_evict(cache, lists, bad, 8), ops)
+
+
+# out's start behind q's, strides of q, strides of out (rows, heads), rows, heads; pieces of 64
+PAIRS = [(0, (512, 64), (512, 64), 3, 8), (1024, (2048, 64), (2048, 64), 3, 8), (64, (1024, 128), (1024, 128), 3, 8), (63, (1024, 128), (1024, 128), 3, 8),
+         (65, (1024, 128), (1024, 128), 3, 8), (-64, (1024, 128), (1024, 128), 3, 8), (1536, (512, 64), (512, 64), 3, 8), (1535, (512, 64), (512, 64), 3, 8),
+         (-1536, (512, 64), (512, 64), 3, 8), (-1473, (512, 64), (512, 64), 3, 8), (512, (1024, 64), (1024, 64), 3, 8), (448, (1024, 64), (1024, 64), 3, 8),
+         (0, (512, 64), (64, 192), 3, 8), (1024, (2048, 64), (2048, 128), 2, 8), (1024, (2048, 64), (2048, 120), 2, 9), (960, (2048, 64), (2048, 128), 2, 8),
+         (0, (0, 64), (512, 64), 3, 8), (1536, (0, 64), (512, 64), 3, 8), (64, (0, 64), (0, 128), 1, 1), (63, (7, 9), (0, 128), 1, 1), (2, (64, 192), (64, 192), 3, 2),
+         (2048, (1024, -64), (1024, 64), 2, 8), (192, (64, 300), (64, 300), 3, 2), (130, (64, 300), (64, 300), 3, 2), (172, (64, 300), (64, 300), 2, 2)]
+
+
+@pytest.mark.parametrize("d,q,out,rows,heads", PAIRS)
+@pytest.mark.parametrize("scored", [False, True])
+def test_out_that_shares_memory_with_q_is_refused(lib, d, q, out, rows, heads, scored):
+    """Elsewhere a block would read what another has written.  q itself is read before it is written, except where the weights need it again."""
+    from paper_2501_19324_amd import ops
+    at = 1 << 24
+
+    def elements(first, strides):
+        return {first + r * strides[0] + h * strides[1] + i for r in range(rows) for h in range(heads) for i in range(64)}
+
+    shared = elements(0, q) & elements(d, out)
+    if (d, q) == (0, out):
+        shared = shared if scored else set()               # (in parts: the weights are added by a kernel of their own)
+    c = _cache(ops, batch=1, n_kv_heads=1, max_pages=512)
+    a = _attn(ops, q=at, out=at + 2 * d, q_row=q[0], q_head=q[1], out_row=out[0], out_head=out[1], rows=rows, n_heads=heads, max_kv=8192, max_rows=rows)
+    book = ops._Book(1 << 30, None, 8192, 8192, 0, 0)
+    good = _no_workspace(lib, lambda: lib.rsd_kv4_attention(C.byref(c), C.byref(a), C.byref(book) if scored else None, None, 0, None))
+    assert good == (not shared) or _share(rows, heads, *out, 64), lib.rsd_op_last_error()
