@@ -206,8 +206,9 @@ def test_out_may_be_q_where_no_weights_need_it_again(torch, R, heads, hkv, hd, l
         assert torch.equal(got, q) and not bool(sums.any())
     else:
         assert torch.equal(got, want) and torch.equal(sums, scores)
+    more = torch.zeros(sum(rows) + 1, heads, hd, device="cuda")
     with pytest.raises(R.RsdError):                        # a row further on
-        R.rsd_kv4_attention(cache, got[1:], 0.2, out=got[:-1], **kw)
+        R.rsd_kv4_attention(cache, more[1:], 0.2, out=more[:-1], **kw)
     both = torch.zeros(sum(rows), 2 * heads, hd, device="cuda")         # beside each other in one buffer
     both[:, ::2] = q
     assert torch.equal(R.rsd_kv4_attention(cache, both[:, ::2], 0.2, out=both[:, 1::2], scores=sums, **kw), want) and torch.equal(both[:, ::2], q)
