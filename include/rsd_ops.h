@@ -50,7 +50,7 @@ typedef struct rsd_w4 {
 int rsd_w4_pack(const void *w, int32_t dtype, int64_t ld, int32_t n, int32_t k, void *codes, void *scales, void *hip_stream);
 
 /* y[r][i] = sum_j x[r][j] W[i][j] for rows of x, any number >= 1.  x dev [rows][k] (rows ldx apart) and y dev [rows][n] (rows ldy apart)
- * are of one type.  Products are exact and summed in fp32 (an fp32 x enters with all its 24 bits); y is rounded once.  The order of the
+ * are of one type and share no memory.  Products are exact and summed in fp32 (an fp32 x enters with all its 24 bits); y is rounded once.  The order of the
  * sum depends on the sizes only. */
 uint64_t rsd_w4_linear_workspace(int32_t rows, int32_t n, int32_t k, int32_t dtype);
 int rsd_w4_linear(const rsd_w4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t rows, int32_t dtype,

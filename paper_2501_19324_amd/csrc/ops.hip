@@ -298,6 +298,7 @@ extern "C" int rsd_w4_linear(const rsd_w4* w, const void* x, int64_t ldx, void* 
     if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(dtype))) return fail(RSD_EINVAL, "w4_linear: x or y is not aligned to its type");
     if ((int64_t)rows * w->n > kMostBlocks * 256 || rows > 1 << 20 || w->n > 1 << 26)
         return fail(RSD_EINVAL, "w4_linear: %d rows with [%d][%d] are too many", rows, w->n, w->k);
+    if (share_memory({x, ldx, 0, w->k}, {y, ldy, 0, w->n}, rows, 1, size_of(dtype))) return fail(RSD_EINVAL, "w4_linear: y shares memory with x");
     const W4Plan p = w4_plan(rows, w->n, w->k, dtype);
     if (workspace_bytes < p.part_bytes || (p.part_bytes && (!workspace || !aligned(workspace, 256))))
         return fail(RSD_EINVAL, "w4_linear: the workspace holds %llu of %llu bytes, or is not 256-byte aligned",

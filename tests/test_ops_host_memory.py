@@ -138,3 +138,28 @@ def test_out_that_shares_memory_with_q_is_refused(lib, d, q, out, rows, heads, s
     book = ops._Book(1 << 30, None, 8192, 8192, 0, 0)
     good = _no_workspace(lib, lambda: lib.rsd_kv4_attention(C.byref(c), C.byref(a), C.byref(book) if scored else None, None, 0, None))
     assert good == (not shared) or _share(rows, heads, *out, 64), lib.rsd_op_last_error()
+
+
+# y's start behind x's, n, distance of the rows of y and of x; 20 rows of 1024 (long enough for a workspace)
+PRODUCTS = [(0, 1024, 1024, 1024), (1024, 1024, 2048, 2048), (1023, 1024, 2048, 2048), (-1024, 1024, 2048, 2048), (-1023, 1024, 2048, 2048), (20480, 16, 16, 1024),
+            (20479, 16, 16, 1024), (-320, 16, 16, 1024), (-319, 16, 16, 1024), (1024, 10, 1034, 1034), (1025, 10, 1034, 1034), (-10, 10, 1034, 1034), (2000, 20, 1044, 1044)]
+
+
+@pytest.mark.parametrize("d,n,ldy,ldx", PRODUCTS)
+@pytest.mark.parametrize("dtype,size", [(0, 4), (1, 2)])
+def test_products_into_memory_of_x_are_refused(lib, d, n, ldy, ldx, dtype, size):
+    """Every block reads all of x while others write."""
+    from paper_2501_19324_amd import ops
+    w, at, rows, k = ops._W4(4096, 4096, n, 1024), 1 << 24, 20, 1024
+    shared = {r * ldx + i for r in range(rows) for i in range(k)} & {d + r * ldy + i for r in range(rows) for i in range(n)}
+    good = _no_workspace(lib, lambda: lib.rsd_w4_linear(C.byref(w), at, ldx, at + size * d, ldy, rows, dtype, None, 0, None))
+    assert good == (not shared), lib.rsd_op_last_error()
+
+
+def test_products_into_their_activations_are_refused_by_the_binding(on_host):
+    import torch
+    ops = on_host
+    w = ops.W4(torch.zeros(2, 1, 4, 16, 16, dtype=torch.uint8), torch.zeros(2, 1, 4, 16, 4, dtype=torch.uint8), 32, 32)
+    x = torch.zeros(6, 32)
+    assert refused(lambda: ops.rsd_w4_linear(x, w, out=x), ops)
+    assert refused(lambda: ops.rsd_w4_linear(x[1:], w, out=x[:-1]), ops)
