@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes as C
 from functools import lru_cache
+from operator import index
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -126,6 +127,17 @@ def _flat(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape) -> int:
     if t.shape != shape or not t.is_contiguous():
         _bad(f"{name}: shape {tuple(t.shape)}, needed {tuple(shape)}, contiguous")
     return t.data_ptr()
+
+
+def _int(name: str, v, least: int) -> int:
+    """A whole number from ``least`` on that the entry points' 32 bits hold (ctypes would take it modulo 2^32)."""
+    try:
+        n = index(v)
+    except TypeError:
+        n = -1
+    if not least <= n < 1 << 31:
+        _bad(f"{name}: {v!r}, needed a whole number from {least} to 2^31 - 1")
+    return n
 
 
 def _workspace(nbytes: int, like: torch.Tensor) -> Tuple[Optional[torch.Tensor], Optional[int]]:
@@ -310,8 +322,9 @@ def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Option
     op, orow, oh = _rows3("out", out, pool, heads, c.head_dim)
     lse = q.new_empty(rows, heads, dtype=_f32) if want_lse else None
     if rows:
+        max_rows = _int("attention: max_rows", max_rows, 1)
         cap = c.max_pages * PAGE
-        max_kv = cap if max_kv is None else min(int(max_kv), cap)
+        max_kv = cap if max_kv is None else min(max(int(max_kv), -1), cap)
         nbytes = _attn_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, rows, max_rows, heads, max_kv, t, rp is not None, want_lse,
                              scores is not None)
         ws, wp = _workspace(nbytes, pool)
@@ -327,7 +340,8 @@ def rsd_kv4_evict(cache, scores: torch.Tensor, entry_pos: torch.Tensor, budget: 
     lib = _lib or _load()
     c, pool, st = _cache(cache)
     book = _book(c, pool, scores, entry_pos)
-    if not 0 <= recent <= budget or budget < 1:
+    budget, recent = _int("evict: budget", budget, 1), _int("evict: recent", recent, 0)
+    if recent > budget:
         _bad(f"evict: budget {budget}, recent {recent}")
     nbytes = _evict_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, budget)
     ws, wp = _workspace(nbytes, pool)

@@ -163,3 +163,24 @@ def test_products_into_their_activations_are_refused_by_the_binding(on_host):
     x = torch.zeros(6, 32)
     assert refused(lambda: ops.rsd_w4_linear(x, w, out=x), ops)
     assert refused(lambda: ops.rsd_w4_linear(x[1:], w, out=x[:-1]), ops)
+
+
+# ---- sizes beyond 32 bits: ctypes takes them modulo 2^32
+
+def small_cache(ops, batch=3, pages=4):
+    import torch
+    return ops.Kv4Cache(torch.zeros(8, 2, 17 * 64, dtype=torch.uint8), torch.zeros(batch, pages, dtype=torch.int32), torch.zeros(batch, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("big", [(1 << 32) + 2, 1 << 31, -(1 << 32) + 2, 2.0, 2.5, None], ids=str)
+def test_sizes_beyond_32_bits_are_refused(on_host, big):
+    import torch
+    ops = on_host
+    cache, q = small_cache(ops), torch.zeros(3, 4, 64)
+    lists, pos, starts = torch.zeros(3, 2, 64), torch.zeros(3, 2, 64, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    assert refused(lambda: ops.rsd_kv4_evict(cache, lists, pos, big), ops)
+    assert refused(lambda: ops.rsd_kv4_evict(cache, lists, pos, 60, big), ops)
+    if big is not None:
+        assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, row_start=starts, max_rows=big), ops)
+    if isinstance(big, int) and big < 0:
+        assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, max_kv=big), ops)
