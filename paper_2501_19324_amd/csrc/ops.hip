@@ -397,7 +397,8 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
 
 extern "C" uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache* c, int32_t budget) {
     if (check_cache(c, "evict") || budget < 1) return 0;
-    return up256((uint64_t)c->batch * c->n_kv_heads * (4 + (uint64_t)up4(budget) + evict_moves(c, budget)) * 4);
+    const int moves = evict_moves(c, budget);
+    return moves ? up256((uint64_t)c->batch * c->n_kv_heads * (4 + up4(budget) + moves) * 4) : 0;      // (none: no list can hold more than the budget)
 }
 
 extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, int32_t budget, int32_t recent, void* workspace,
@@ -409,10 +410,10 @@ extern "C" int rsd_kv4_evict(const rsd_kv4_cache* c, const rsd_kv4_book* book, i
         return fail(RSD_EINVAL, "evict: lists of scores or positions overlap (strides %lld, %lld and %lld, %lld)", (long long)book->score_b, (long long)book->score_h,
                     (long long)book->position_b, (long long)book->position_h);
     const uint64_t need = rsd_kv4_evict_workspace(c, budget);
-    if (workspace_bytes < need || !workspace || !aligned(workspace, 256))
+    if (need && (workspace_bytes < need || !workspace || !aligned(workspace, 256)))
         return fail(RSD_EINVAL, "evict: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
     const Kv4Evict e{dev_cache(c), dev_book(book), budget, recent, static_cast<int*>(workspace), evict_moves(c, budget)};
-    if (e.moves == 0) return RSD_OK;                     // no sequence can hold more than the budget
+    if (e.moves == 0) return RSD_OK;
     Launches l(hip_stream);
     const unsigned lists = (unsigned)(c->batch * c->n_kv_heads);
     const int64_t slots = (int64_t)c->max_pages * KV4_PAGE;

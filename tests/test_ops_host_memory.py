@@ -184,3 +184,25 @@ def test_sizes_beyond_32_bits_are_refused(on_host, big):
         assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, row_start=starts, max_rows=big), ops)
     if isinstance(big, int) and big < 0:
         assert refused(lambda: ops.rsd_kv4_attention(cache, q, 1.0, max_kv=big), ops)
+
+
+def test_whole_numbers_of_other_types_are_taken(on_host):
+    """A budget that holds every entry of the table leaves nothing to launch."""
+    import numpy as np
+    import torch
+    ops = on_host
+    lists, pos = torch.zeros(3, 2, 64), torch.zeros(3, 2, 64, dtype=torch.int32)
+    for budget, recent in ((64, 0), (np.int64(64), np.int32(3)), (torch.tensor(64), torch.tensor(3)), ((1 << 31) - 1, 5)):
+        ops.rsd_kv4_evict(small_cache(ops), lists, pos, budget, recent)
+
+
+@pytest.mark.parametrize("budget", [64, 65, 10 ** 6, (1 << 31) - 1])
+def test_a_budget_beyond_the_table_needs_no_workspace(lib, budget):
+    """It once grew with the budget: 1 GB for a million on 256 lists, for a call that has nothing to do."""
+    from paper_2501_19324_amd import ops
+    c, book = _cache(ops, batch=64, n_kv_heads=4, max_pages=4), ops._Book(1 << 20, 1 << 24, 256, 64, 256, 64)
+    assert lib.rsd_kv4_evict_workspace(C.byref(c), budget) == 0
+    assert lib.rsd_kv4_evict(C.byref(c), C.byref(book), budget, 0, None, 0, None) == 0
+    most = max(lib.rsd_kv4_evict_workspace(C.byref(c), b) for b in range(1, 64))
+    assert 0 < most <= 64 * 4 * (4 + 64 + 2 * 3) * 4 + 255     # an entry for each slot: those below the budget and those that move, each in whole fours
+    assert _no_workspace(lib, lambda: lib.rsd_kv4_evict(C.byref(c), C.byref(book), 63, 0, None, 0, None))
