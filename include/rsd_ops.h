@@ -97,7 +97,8 @@ int rsd_kv4_read(const rsd_kv4_cache *c, const int32_t *seq, const int32_t *slot
  * slots < n - (q - 1 - j).  q, out dev [rows][n_heads][head_dim] with row and head strides; head h reads kv head h / (n_heads /
  * n_kv_heads).  out = softmax(scale q.K) V; a row that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of
  * the sum of exp(scale q.k), -inf for such rows, which deal out no weight either.  With scores in book (NULL: none) every entry's score grows by the softmax weights it received, summed over the rows
- * and the heads of its group.  out may be q itself where no scores are given, and shares no memory with it else. */
+ * and the heads of its group.  Sizes: batch * n_kv_heads * (max_rows * n_heads / n_kv_heads in
+ * whole 64s) below 2^30, max_rows * n_heads below 2^27.  out may be q itself where no scores are given, and shares no memory with it else. */
 typedef struct rsd_kv4_attn {
     const void *q;
     void *out;

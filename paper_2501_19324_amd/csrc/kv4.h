@@ -193,7 +193,7 @@ struct Kv4Attn {
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
     float* lse2;            // kv4_weight_log of every row and head, for the kernels that add the weights afterwards (KV4_LOGS), or null
-    int max_kv, split, splits, hd;
+    int max_kv, tiles, split, splits, hd;
     bool by_length;         // the blocks of the longest sequences go first
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
@@ -631,8 +631,8 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     typedef typename u32vec<G>::type V;
     __shared__ u32x4_t lds_k[4 * G][64], lds_v[4 * G][64];              // keys [page][j], values [pair of pages][block of 16 dims]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
-    const int id = blockIdx.x + gridDim.x * blockIdx.y, head = id % a.c.hkv, col0 = id / a.c.hkv % gridDim.y * COLS;
-    const int b = kv4_by_length(a, id / a.c.hkv / gridDim.y);
+    const int id = blockIdx.x, head = id % a.c.hkv, col0 = id / a.c.hkv % a.tiles * COLS;
+    const int b = kv4_by_length(a, id / a.c.hkv / a.tiles);
     int r0, count, n;
     kv4_rows(a, b, r0, count, n);
     const int cols = count * a.group, parts = kv4_parts(a, n);

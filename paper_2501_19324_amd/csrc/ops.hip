@@ -226,15 +226,18 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
     if (a->rows < 1 || a->max_rows < 1 || a->max_kv < 0) return fail(RSD_EINVAL, "attention: rows %d, at most %d a sequence, entries %d", a->rows, a->max_rows, a->max_kv);
     if (a->n_heads < 1 || a->n_heads % c->n_kv_heads) return fail(RSD_EINVAL, "attention: %d heads over %d kv heads", a->n_heads, c->n_kv_heads);
     if (!a->row_start && a->max_rows != 1) return fail(RSD_EINVAL, "attention: max_rows %d without row_start", a->max_rows);
-    if ((int64_t)a->max_rows * a->n_heads > INT32_MAX / 16 || (int64_t)c->batch * a->max_rows * a->n_heads > kMostBlocks * 4)
+    // columns of a (sequence, kv head) are counted in 32 bits; so are the threads of a launch: blocks of 256 for 64 columns each.  (Parts are made and joined for
+    // fewer than 2048 blocks alone.)
+    if ((int64_t)a->max_rows * a->n_heads > INT32_MAX / 16 || c->batch * c->n_kv_heads * ceil_div((int64_t)a->max_rows * (a->n_heads / c->n_kv_heads), 64) >= 1 << 24)
         return fail(RSD_EINVAL, "attention: %d rows x %d heads x %d sequences", a->max_rows, a->n_heads, c->batch);
     return RSD_OK;
 }
 
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, Launches& l) {
-    const dim3 grid((unsigned)(k.c.batch * k.c.hkv), (unsigned)p.tiles, (unsigned)p.splits);
-    if (p.many && k.lse2) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS>, grid, 256, 0, k);
-    else if (p.many) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, grid, 256, 0, k);
+    const unsigned lists = (unsigned)(k.c.batch * k.c.hkv);
+    const dim3 grid(lists, (unsigned)p.tiles, (unsigned)p.splits), many(lists * (unsigned)p.tiles, 1, (unsigned)p.splits);
+    if (p.many && k.lse2) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS>, many, 256, 0, k);
+    else if (p.many) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, many, 256, 0, k);
     else if (p.fused) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_WEIGHTS>, grid, 64 * p.waves, 0, k);
     else if (k.lse2) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_LOGS>, grid, 64 * p.waves, 0, k);
     else l.run(kv4_attn_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, grid, 64 * p.waves, 0, k);
@@ -382,7 +385,7 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
     k.lse2 = p.lse_bytes ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
-    k.max_kv = a->max_kv, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.hd = c->head_dim;
+    k.max_kv = a->max_kv, k.tiles = p.tiles, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.hd = c->head_dim;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);

@@ -212,3 +212,14 @@ def test_out_may_be_q_where_no_weights_need_it_again(torch, R, heads, hkv, hd, l
     both = torch.zeros(sum(rows), 2 * heads, hd, device="cuda")         # beside each other in one buffer
     both[:, ::2] = q
     assert torch.equal(R.rsd_kv4_attention(cache, both[:, ::2], 0.2, out=both[:, 1::2], scores=sums, **kw), want) and torch.equal(both[:, ::2], q)
+
+
+def test_rows_bounded_far_above_what_there_is(torch, R):
+    """A bound that makes more than 2^16 tiles of columns of a list, and 2^24 (sequence, row, head) triples."""
+    rng = np.random.default_rng(17)
+    lens, rows, heads = [70, 0, 130, 20], [3, 0, 33, 1], 64
+    cache, pool, table = random_pages(torch, R, rng, lens, 1, 32)
+    q = dev(torch, rng.normal(size=(sum(rows), heads, 32)).astype(np.float32))
+    starts = dev(torch, starts_of(rows))
+    out, lse = R.rsd_kv4_attention(cache, q, 0.2, row_start=starts, max_rows=70_000, want_lse=True)
+    check_columns(cache, pool, table, lens, rows, q, float(np.float32(0.2)), out, lse)

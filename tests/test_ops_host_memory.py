@@ -206,3 +206,19 @@ def test_a_budget_beyond_the_table_needs_no_workspace(lib, budget):
     most = max(lib.rsd_kv4_evict_workspace(C.byref(c), b) for b in range(1, 64))
     assert 0 < most <= 64 * 4 * (4 + 64 + 2 * 3) * 4 + 255     # an entry for each slot: those below the budget and those that move, each in whole fours
     assert _no_workspace(lib, lambda: lib.rsd_kv4_evict(C.byref(c), C.byref(book), 63, 0, None, 0, None))
+
+
+# batch, heads, kv heads, most rows of a sequence: prompts of large batches, and the bounds that the header names
+SIZES = [(128, 64, 8, 4096, True), (1024, 64, 8, 1000, True), (2, 64, 1, 1 << 20, True), (16383, 16, 16, 4096, True), (16384, 16, 16, 4096, False), (1, 64, 1, (1 << 21) - 1, True),
+         (1, 64, 1, 1 << 21, False), (1 << 20, 1, 1, 64 * 15, True), (1 << 20, 1, 1, 64 * 15 + 1, False)]
+
+
+@pytest.mark.parametrize("batch,heads,hkv,most,good", SIZES)
+def test_prompts_of_large_batches_are_taken(lib, batch, heads, hkv, most, good):
+    """batch x rows x heads was once held below 2^24, for a launch that such sizes do not make."""
+    from paper_2501_19324_amd import ops
+    c = _cache(ops, batch=batch, n_kv_heads=hkv)
+    a = _attn(ops, rows=5, max_rows=most, n_heads=heads, q_row=heads * 64, out_row=heads * 64)
+    book = ops._Book(1 << 30, None, hkv * 64, 64, 0, 0)
+    assert (lib.rsd_kv4_attention_workspace(C.byref(c), C.byref(a), 1) > 0) == good
+    assert _no_workspace(lib, lambda: lib.rsd_kv4_attention(C.byref(c), C.byref(a), C.byref(book), None, 0, None)) == good
