@@ -291,14 +291,15 @@ def _attn_bytes(n_pages, kv_heads, hd, batch, max_pages, rows, max_rows, heads, 
     return (_lib or _load()).rsd_kv4_attention_workspace(C.byref(c), C.byref(a), int(scored))
 
 
-def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optional[torch.Tensor] = None, max_rows: int = 1,
+def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optional[torch.Tensor] = None, max_rows: Optional[int] = None,
                       max_kv: Optional[int] = None, scores: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                       want_lse: bool = False):
     """Attention of the rows ``q [rows, n_heads, head_dim]`` over the cache, their own entries included.
 
     Without ``row_start`` row b is sequence b's newest token; with it (``[batch + 1]`` int32) sequence b has the rows
-    ``row_start[b] .. row_start[b + 1] - 1``, at most ``max_rows``, and each sees one entry more than the row before it.  ``max_kv`` bounds
-    ``kv_len`` (default: what the table can hold); the tighter it is, the better the work is dealt.  ``scores`` ``[batch, n_kv_heads, slots]``
+    ``row_start[b] .. row_start[b + 1] - 1``, and each sees one entry more than the row before it.  ``max_rows`` bounds the rows of a sequence (default: all
+    of them could be one's): rows beyond it are not computed, and the first ``max_rows`` are taken for the sequence's newest; their places in the result, like those of rows
+    that no sequence has, are not written.  ``max_kv`` bounds ``kv_len`` (default: what the table can hold).  The tighter both are, the better the work is dealt.  ``scores`` ``[batch, n_kv_heads, slots]``
     grows by the weight each entry received.  ``out`` may be ``q`` itself, without ``scores``.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
     lib = _lib or _load()
     c, pool, st = _cache(cache)
@@ -310,10 +311,12 @@ def rsd_kv4_attention(cache, q: torch.Tensor, scale: float, *, row_start: Option
     if heads == 0 or heads % c.n_kv_heads:
         _bad(f"attention: {heads} heads over {c.n_kv_heads} kv heads")
     if row_start is None:
+        max_rows = 1 if max_rows is None else max_rows
         if rows != c.batch or max_rows != 1:
             _bad(f"attention: {rows} rows for {c.batch} sequences, max_rows {max_rows}, without row_start")
         rp = None
     else:
+        max_rows = rows if max_rows is None else max_rows
         rp = _flat("row_start", row_start, pool, _i32, (c.batch + 1,))
     if out is None:
         out = q.new_empty(rows, heads, c.head_dim)

@@ -223,3 +223,12 @@ def test_rows_bounded_far_above_what_there_is(torch, R):
     starts = dev(torch, starts_of(rows))
     out, lse = R.rsd_kv4_attention(cache, q, 0.2, row_start=starts, max_rows=70_000, want_lse=True)
     check_columns(cache, pool, table, lens, rows, q, float(np.float32(0.2)), out, lse)
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS)
+def test_rows_without_a_bound_are_all_computed(torch, R, heads, hkv, hd, lens, rows):
+    rng = np.random.default_rng(heads + 11 * hd)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    q = dev(torch, rng.normal(size=(sum(rows), heads, hd)).astype(np.float32))
+    out, lse = R.rsd_kv4_attention(cache, q, 0.2, row_start=dev(torch, starts_of(rows)), want_lse=True, out=torch.full_like(q, 1e9))
+    check_columns(cache, pool, table, lens, rows, q, float(np.float32(0.2)), out, lse)
