@@ -232,3 +232,49 @@ def test_rows_without_a_bound_are_all_computed(torch, R, heads, hkv, hd, lens, r
     q = dev(torch, rng.normal(size=(sum(rows), heads, hd)).astype(np.float32))
     out, lse = R.rsd_kv4_attention(cache, q, 0.2, row_start=dev(torch, starts_of(rows)), want_lse=True, out=torch.full_like(q, 1e9))
     check_columns(cache, pool, table, lens, rows, q, float(np.float32(0.2)), out, lse)
+
+
+# ---------------------------------------------------------------- every kernel of the attention with its rarer arguments
+
+GROUPS = [(9, 3, 64, [400, 150], [90, 60]), (3, 1, 32, [300], [100])]      # columns in two groups, the first of which ends inside a step
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS + GROUPS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.15, -0.15])
+def test_pages_outside_the_pool_and_negative_factors(torch, R, heads, hkv, hd, lens, rows, dtype, scale):
+    rng = np.random.default_rng(heads + 3 * hd)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    table[0, 1], table[0, 3], table[-1, 0] = -1, len(pool) + 3, 1 << 30
+    cache = R.Kv4Cache(cache.pool, dev(torch, table), cache.kv_len)
+    starts = starts_of(rows)
+    q = dev(torch, rng.normal(size=(int(starts[-1]), heads, hd)).astype(np.float32)).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    scores = dev(torch, rng.random((len(lens), hkv, table.shape[1] * 16)).astype(np.float32))
+    before = host(scores)
+    out, lse = R.rsd_kv4_attention(cache, q, scale, row_start=dev(torch, starts), max_rows=max(rows), scores=scores, want_lse=True)
+    check_columns(cache, pool, table, lens, rows, q, float(np.float32(scale)), out, lse, before, host(scores), dtype)
+
+
+@pytest.mark.parametrize("heads,hkv,hd,lens,rows", KINDS + GROUPS)
+@pytest.mark.parametrize("what", ["large", "infinite", "nan value", "nan key"])
+def test_weights_of_unusual_numbers(torch, R, heads, hkv, hd, lens, rows, what):
+    rng = np.random.default_rng(heads + 5 * hd)
+    cache, pool, table = random_pages(torch, R, rng, lens, hkv, hd)
+    columns_with_first_dimension_alike(pool, hd)
+    starts = starts_of(rows)
+    q = rng.normal(size=(int(starts[-1]), heads, hd)).astype(np.float32)
+    if what == "large":
+        q *= 100
+    if what == "infinite":
+        q[0, 0, 0], q[0, heads - 1, 0] = np.inf, -np.inf
+    if "nan" in what:
+        for slot in (lens[0] - 2, 5):                      # one that not every row sees where there are several, one that all see
+            pool[table[0, slot // 16], 0][ref.entry_places(hd, slot % 16)[3 if "value" in what else 2][0]] = 255
+            if "value" not in what and slot != 5:
+                break                                      # (a key that all see leaves nothing else to look at)
+    cache = R.Kv4Cache(dev(torch, pool), cache.table, cache.kv_len)
+    q = dev(torch, q)
+    scores = dev(torch, rng.random((len(lens), hkv, table.shape[1] * 16)).astype(np.float32))
+    before = host(scores)
+    out, lse = R.rsd_kv4_attention(cache, q, 0.25, row_start=dev(torch, starts), max_rows=max(rows), scores=scores, want_lse=True)
+    check_columns(cache, pool, table, lens, rows, q, 0.25, out, lse, before, host(scores))
