@@ -46,11 +46,11 @@ typedef struct rsd_w4 {
     int32_t n, k;
 } rsd_w4;
 
-/* w dev [n][k], rows ld elements apart, to codes and scales (dev, sizes as above). */
+/* w dev [n][k], rows ld >= k elements apart, to codes and scales (dev, sizes as above).  NT * KS up to 2^18. */
 int rsd_w4_pack(const void *w, int32_t dtype, int64_t ld, int32_t n, int32_t k, void *codes, void *scales, void *hip_stream);
 
 /* y[r][i] = sum_j x[r][j] W[i][j] for rows of x, any number >= 1.  x dev [rows][k] (rows ldx apart) and y dev [rows][n] (rows ldy apart)
- * are of one type and share no memory.  Products are exact and summed in fp32 (an fp32 x enters with all its 24 bits); y is rounded once.  The order of the
+ * are of one type and share no memory; rows up to 2^20, n up to 2^26, rows * n up to 2^30.  Products are exact and summed in fp32 (an fp32 x enters with all its 24 bits); y is rounded once.  The order of the
  * sum depends on the sizes only. */
 uint64_t rsd_w4_linear_workspace(int32_t rows, int32_t n, int32_t k, int32_t dtype);
 int rsd_w4_linear(const rsd_w4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, int32_t rows, int32_t dtype,
@@ -65,7 +65,9 @@ int rsd_w4_linear(const rsd_w4 *w, const void *x, int64_t ldx, void *y, int64_t 
  *   key codes    [4 quarters of the head dimension][16 t][head_dim / 8 bytes]
  *   value codes  [t / 4][dim % 16][G][t % 4]: a byte holds dims m and m + 16 of its group
  *   key scales   [G][16 t]
- *   value scales [t / 4][G][t % 4] */
+ *   value scales [t / 4][G][t % 4]
+ * Sizes: batch * n_kv_heads up to 2^20, max_pages up to 2^26 - 1; rows of a call that writes or reads entries (in whole fours) * n_kv_heads * head_dim / 32 up to
+ * 2^28. */
 typedef struct rsd_kv4_cache {
     void *pool;
     const int32_t *table;
@@ -116,7 +118,9 @@ int rsd_kv4_attention(const rsd_kv4_cache *c, const rsd_kv4_attn *a, const rsd_k
  * within `recent` of the newest, then those of the highest score (NaN: lowest), ties to the lower slot, `budget` in all.  Positions may repeat: where more than
  * `budget` entries are that new, those of the highest score among them stay.  Kept entries in slots
  * >= budget move, with score and position, into the slots freed below it: the i-th of them in slot order into the i-th
- * freed one.  kv_len becomes min(kv_len, budget); what lies behind it is left as it was.  0 <= recent <= budget, budget >= 1; book with both arrays. */
+ * freed one.  kv_len becomes min(kv_len, budget); what lies behind it is left as it was.  0 <= recent <= budget, budget >= 1; book with both
+ * arrays.  Every slot below kv_len needs its page here: entries without one are ranked like the others, but there is nothing to move, and what moves to a slot without one is
+ * lost. */
 uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache *c, int32_t budget);
 int rsd_kv4_evict(const rsd_kv4_cache *c, const rsd_kv4_book *book, int32_t budget, int32_t recent, void *workspace,
                   uint64_t workspace_bytes, void *hip_stream);

@@ -6,7 +6,8 @@
 // byte) sees one token and one group at a time.  Four tokens' pairs are transposed by byte permutes into the A operands of the products
 // V^T P^T (rows: dims), whose contraction order (tokens 4 c + i of one page, then of the next) is the layout in which the matrix instruction
 // leaves the scores: the probabilities go from one product into the other without leaving their lanes.
-// A byte belongs to one token: entries are written without reading their neighbours.
+// A byte belongs to one token: an entry is written without reading its neighbours.  (The moves of an eviction own the pages that they write to, and write the values
+// of such a page back whole.)
 #pragma once
 #include "q4.h"
 
@@ -217,7 +218,7 @@ __device__ __forceinline__ void kv4_rows(const Kv4Attn& a, int b, int& r0, int& 
 __device__ __forceinline__ int kv4_parts(const Kv4Attn& a, int n) { return a.splits == 1 ? 1 : (n - 1) / a.split + 1; }
 
 // Sequences of unlike lengths make blocks of unlike times; where the blocks do not all run at once the longest go first, so that the last to start are short
-// (16 sequences, the case at kv4_attn_many_kernel: 225 -> 150 us).  The i-th sequence in that order, among every 64 together: the same for all lanes of a
+// (16 sequences of unlike lengths and rows, 72B heads: fp32 205 -> 173 us, bf16 147 -> 126).  The i-th sequence in that order, among every 64 together: the same for all lanes of a
 // whole wave, about a microsecond at a block's start.
 __device__ __forceinline__ int kv4_by_length(const Kv4Attn& a, int i) {
     if (!a.by_length) return i;
@@ -433,7 +434,7 @@ template <int PP> __device__ __forceinline__ void kv4_weights(const f32x4_t s0, 
             w[0][i] = hi;
             w[1][i] = lo;
         } else {
-            // cut as in q4_cut3; a probability is at most 1 or NaN, whose first part is NaN
+            // cut as in q4_cut3; a probability is at most 2^8 (the maximum moves in steps) and its rounding, or NaN, whose first part is NaN
             const float x1 = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u), y1 = y - __uint_as_float(__float_as_uint(y) & 0xFFFF0000u);
             const float x2 = x1 - __uint_as_float(__float_as_uint(x1) & 0xFFFF0000u), y2 = y1 - __uint_as_float(__float_as_uint(y1) & 0xFFFF0000u);
             w[0][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
@@ -492,13 +493,14 @@ __device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
 
 // Few columns (single tokens, verification of a few): a block owns a tile of 16 columns of one (sequence, kv head) and one part of its entries, of which
 // its waves take chunks of 64 in turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's bytes are requested before
-// this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (28 columns, 64 sequences: 62 us against 78 with
-// both tiles in one wave's registers).
-// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 172 .. 181 us, 4.7 .. 5 TB/s, what a copy reaches (8 us more in the order of the sequences); 519 vector
-// and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  In that order: 190 us without the requests ahead, 198 with them dropped for a
-// third wave per SIMD.
+// this one is worked on, the table entries one chunk earlier still.  A second tile reads the entries again, from L2 (with
+// both tiles in one wave's registers 28 columns of 64 sequences took a quarter longer).
+// 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 163 .. 167 us, 5.2 TB/s, what a copy reaches (8 us more in the order of the sequences); 480 vector
+// and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  Without the requests ahead, or with them dropped for a third wave per SIMD, it
+// took 5 and 10 % longer.  At 128 dims the fp32 instances spill 4 to 6 of 256 registers.
 // KV4_WEIGHTS: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
-// once more (64 sequences of 128 .. 5120 entries: 51 us instead of 56 in two launches; 256 blocks, so the longest sequence decides).
+// once more.  Against two launches: 64 x 4 of 64 .. 512 entries 12.5 us and 16.9, of 128 .. 5120 47 and 47 (fp32 57 and 61; 256 blocks, so the longest sequence
+// decides); where the blocks go in rounds the weights' own, finer blocks are ahead (256 x 4 of 512 .. 4096: 118 and 104).
 template <typename T, int HD, int PLANES, int WEIGHTS>
 __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, WAVES = 8;
@@ -622,9 +624,10 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 
 // Many columns (steps and prompts): a block of four waves owns four tiles of columns of one (sequence, kv head) and one part of its entries.  All its waves
 // need every key and value, so a chunk is decoded once for the block, into operands in LDS, a share by each wave; the next chunk's bytes are on their way in the meantime.
-// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 137 .. 148 us, 0.9 executed PFLOP/s (three
-// bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 107 us.  (4 % more in fp32 with the sums of a tile one after the other; 225 in the
-// order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 177, bf16 115.
+// Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 131 .. 138 us, by which rows meet which
+// lengths, 0.95 executed PFLOP/s (three bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 102 .. 106 us.  (4 % more in fp32 with the sums of a
+// tile one after the other, 18 % in the order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 26 %, bf16 7 % more.
+// The fp32 instance at 128 dims spills 9 of 168 registers, reloaded in every chunk.
 template <typename T, int HD, int PLANES, int WEIGHTS>
 __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
@@ -838,8 +841,9 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
 
 // The same for more than one tile of columns: a wave keeps its chunk's keys decoded and goes over the tiles, whose q the block cuts into operands in LDS, one
 // (tile, 32 dims) by each wave, the next ones while these are worked on.  Where blocks are few or unlike the columns are dealt in groups, whose weights the next
-// kernel adds up.  16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 113 us with the sum; 145 in one group; 315 with every wave cutting q
-// for itself, chunk by chunk.  216 vector instructions a tile and chunk beside 48 matrix instructions; three waves a SIMD (two: 15 % more).
+// kernel adds up.  16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 89 .. 115 us and 5 for the sum, bf16 56 .. 69 and 5; 19 and 12 us
+// more in one group; three times as long with every wave cutting q for itself, chunk by chunk.  Some 216 vector instructions a tile and chunk beside 48 matrix
+// instructions; three waves a SIMD (two: 15 % more), for which the fp32 instance at 128 dims spills 3 registers.
 template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, TILES = 4 / G;

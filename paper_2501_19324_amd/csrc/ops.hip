@@ -177,17 +177,19 @@ struct AttnPlan {
 };
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
-//  - more than two tiles of columns share their decoded entries (28 columns, 64 sequences, bf16: 62 us without, 79 with; 56 columns: 85 with).
-//  - few columns: eight waves to a block up to 256 blocks (64 x 4 of 128 .. 5120 entries: 33 us against 37 with four), and up to 512 where lists are long
-//    (128 x 4 of 512 .. 8192: 75 us against 90; 256 x 2 of 128 .. 2048: 33 against 29); else four (150 x 4: 65 against 72).
-//    With fewer than 128 (sequence, kv head) pairs the entries are split for 512 blocks, down to two chunks a wave (one sequence, 2 x 8192 entries: 19 us, 30 with six
-//    chunks); with more, down to six (32 x 4 pairs of 8192: 38 us, 44 with four), because the parts have to be joined.
-//  - many columns: up to 2048 blocks in parts of 20 chunks at least (16 sequences x 4 kv heads, 17 .. 128 rows of 512 .. 2560 entries, bf16: 77 us whole, 68 in two
-//    parts; 64 x 4, 8 rows of 128 .. 5120: 71 in four parts, 75 in seven, 118 whole), in smaller ones, down to six, only to give every CU a block (40 rows of one
-//    sequence, 2 x 2048 entries: 57 us whole, 20 in parts of six).
-//  - more blocks than run at once: the longest sequences first (64 x 4 x 2 tiles: 43 us against 56; 256 x 4 of 4096 .. 8192: 172 against 183); below that the order decides
+//  - more than two tiles of columns share their decoded entries (64 sequences of 128 .. 5120 entries, bf16: 28 columns 42 us without, 58 with; 35 and 42 columns
+//    62 either way; 56 columns 69 without, 65 with; fp32: 53 and 70, 79 and 80, 89 and 84).
+//  - few columns: eight waves to a block up to 256 blocks (64 x 4 of 128 .. 5120 entries: 29 us against 33 with four), and up to 512 where lists are long
+//    (128 x 4 of 512 .. 8192: 61 us against 74; 256 x 2 of 128 .. 2048: 30 against 26); else four (150 x 4: 52 against 65).
+//    With fewer than 128 (sequence, kv head) pairs the entries are split for 512 blocks, down to two chunks a wave (one sequence, 2 x 8192 entries: 16 us, 26 with eight
+//    chunks, 39 whole); with more, down to six (32 x 4 pairs of 8192: 31 us in two parts, 42 in three, 41 in four, 43 whole), because the parts have to be joined.
+//  - many columns: up to 2048 blocks in parts of 20 chunks at least (64 x 4, 8 rows of 128 .. 5120: 65 us in four parts, 67 in seven, 120 whole; 16 x 4, 17 .. 128 rows of
+//    512 .. 2560, bf16, two parts or whole, by which rows the longest sequences have: 69 or 81, 64 or 67, 72 or 72, 93 or 84), in smaller ones, down to six, only to
+//    give every CU a block (40 rows of one sequence, 2 x 2048 entries: 49 us whole, 20 in parts of six).
+//  - more blocks than run at once: the longest sequences first (64 x 4 x 2 tiles: 42 us against 53; 256 x 4 of 4096 .. 8192: 163 against 171); below that the order decides
 //    nothing and costs 1 us.
-//  - attention weights of more than one tile: the columns in groups of eight tiles at least, up to 4096 blocks of four chunks.
+//  - attention weights of more than one tile: the columns in groups of eight tiles at least, up to 4096 blocks of four chunks (16 x 8, 72B heads, with the attention, fp32:
+//    295 us in two to four groups, 298 in eight, 314 in one).
 AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     AttnPlan p;
     const int64_t cols = (int64_t)a->max_rows * (a->n_heads / c->n_kv_heads);

@@ -4,8 +4,9 @@
 ``Q4Decoder`` takes one of the framework's models (a shape and its weight blob, the layout of ``rsd_inputs.blob_layout``), packs the
 projections into 4-bit tiles and feeds ragged batches of tokens: one token per sequence (decoding), several (a step to be scored or
 verified) or whole prompts.  Per layer the queries, keys and values come from one product with 4-bit weights, keys are rotated and
-written with their positions, attention reads the cache and adds up the weight every entry receives; when a sequence
-would outgrow its pages, each of its kv heads falls back to ``budget`` entries.  Norms, rotation and the activation are plain torch.
+written with their positions, attention reads the cache and adds up the weight every entry receives; when some sequence
+would outgrow its pages, every sequence with more than ``budget`` entries falls back to that many, each kv head by its own weights.  Norms, rotation and the
+activation are plain torch, and activations are fp32 whatever the model's type: the products and the attention run in their fp32 forms.
 
     python -m paper_2501_19324_amd.q4_decode --workload cfg1 --layers 4 --tokens 64
 """
@@ -22,7 +23,8 @@ from . import binding as R
 
 class Q4Decoder:
     def __init__(self, shape, blob: torch.Tensor, batch: int, capacity: int, budget: int, recent: int):
-        """``capacity`` entries of room per sequence; ``budget`` of them survive an eviction, the ``recent`` newest among them."""
+        """``capacity`` entries of room per sequence; ``budget`` of them survive an eviction, the ``recent`` newest among them.  An eviction cuts back
+        every sequence that holds more, whichever of them ran out of room."""
         from rsd_inputs import blob_layout
 
         if not 0 < budget < capacity or not 0 <= recent <= budget:
