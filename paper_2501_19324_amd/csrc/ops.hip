@@ -78,12 +78,18 @@ bool share_memory(Pieces p, Pieces q, int64_t n0, int64_t n1, size_t size) {
     if (p.s0 != q.s0) return true;
     const wide s0 = p.s0 < 0 ? -(wide)p.s0 : p.s0;         // distances in i count in both directions
     auto floor_div = [](wide a, wide b) { return a / b - (a % b < 0); };
+    if (s0 > 0 && p.s1 >= 0 && q.s1 >= 0) {                 // side by side in every row of the buffer
+        const wide from = d - floor_div(d, s0) * s0;
+        if (from >= (n1 - 1) * (wide)p.s1 + p.len && from + (n1 - 1) * (wide)q.s1 + q.len <= s0) return false;
+    }
+    // q's piece starts `c` behind p's, and a multiple of s0: somewhere between -q.len and p.len?
+    auto meet = [&](wide c) {
+        return s0 == 0 ? c > -q.len && c < p.len : std::max<wide>(-floor_div(q.len - 1 + c, s0), 1 - n0) <= std::min<wide>(floor_div(p.len - 1 - c, s0), n0 - 1);
+    };
     for (int64_t j = 0; j < n1; ++j)
         for (int64_t i = 0; i < n1; ++i) {
-            // q's piece starts `c` behind p's, and a multiple of s0: somewhere between -q.len and p.len?
-            const wide c = d + (wide)j * q.s1 - (wide)i * p.s1;
-            if (s0 == 0 ? c > -q.len && c < p.len
-                        : std::max<wide>(-floor_div(q.len - 1 + c, s0), 1 - n0) <= std::min<wide>(floor_div(p.len - 1 - c, s0), n0 - 1)) return true;
+            if (p.s1 == q.s1 && i > 0 && j > 0) break;      // (only their distance counts)
+            if (meet(d + (wide)j * q.s1 - (wide)i * p.s1)) return true;
         }
     return false;
 }

@@ -117,7 +117,9 @@ PAIRS = [(0, (512, 64), (512, 64), 3, 8), (1024, (2048, 64), (2048, 64), 3, 8), 
          (-1536, (512, 64), (512, 64), 3, 8), (-1473, (512, 64), (512, 64), 3, 8), (512, (1024, 64), (1024, 64), 3, 8), (448, (1024, 64), (1024, 64), 3, 8),
          (0, (512, 64), (64, 192), 3, 8), (1024, (2048, 64), (2048, 128), 2, 8), (1024, (2048, 64), (2048, 120), 2, 9), (960, (2048, 64), (2048, 128), 2, 8),
          (0, (0, 64), (512, 64), 3, 8), (1536, (0, 64), (512, 64), 3, 8), (64, (0, 64), (0, 128), 1, 1), (63, (7, 9), (0, 128), 1, 1), (2, (64, 192), (64, 192), 3, 2),
-         (2048, (1024, -64), (1024, 64), 2, 8), (192, (64, 300), (64, 300), 3, 2), (130, (64, 300), (64, 300), 3, 2), (172, (64, 300), (64, 300), 2, 2)]
+         (2048, (1024, -64), (1024, 64), 2, 8), (192, (64, 300), (64, 300), 3, 2), (130, (64, 300), (64, 300), 3, 2), (172, (64, 300), (64, 300), 2, 2),
+         (448, (1024, 64), (1024, 64), 3, 7), (-448, (1024, 64), (1024, 64), 3, 7), (1500, (1024, 64), (1024, 64), 4, 7), (1536, (1024, 64), (1024, 70), 4, 8),
+         (576, (1024, 64), (1024, 64), 4, 8), (512, (1024, 64), (1024, 73), 4, 8), (1984, (1024, 64), (1024, 0), 3, 9), (1023, (512, 64), (512, 64), 4, 8)]
 
 
 @pytest.mark.parametrize("d,q,out,rows,heads", PAIRS)
