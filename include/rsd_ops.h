@@ -1,7 +1,8 @@
 /*
- * rsd_ops.h - operators of a decode step whose memory is 4 bits wide, on AMD MI355X (gfx950): products with 4-bit
+ * rsd_ops.h - operators of a decode step on AMD MI355X (gfx950).  With memory 4 bits wide: products with 4-bit
  * weights, a paged 4-bit KV cache (writing, reading, attention), and eviction from that cache by accumulated attention
- * weight.
+ * weight.  With a paged cache in bf16 or fp32: norms and rotation of queries and keys, the same on the way into the cache, reading, and
+ * attention with a sliding window.
  *
  * Conventions
  *  - "dev" pointers are device addresses.  Calls enqueue their kernels on hip_stream (a hipStream_t, NULL: the default
@@ -124,6 +125,83 @@ int rsd_kv4_attention(const rsd_kv4_cache *c, const rsd_kv4_attn *a, const rsd_k
 uint64_t rsd_kv4_evict_workspace(const rsd_kv4_cache *c, int32_t budget);
 int rsd_kv4_evict(const rsd_kv4_cache *c, const rsd_kv4_book *book, int32_t budget, int32_t recent, void *workspace,
                   uint64_t workspace_bytes, void *hip_stream);
+
+/* ---- norms and rotation of queries and keys ----
+ * A head x [head_dim] becomes, in fp32 and rounded once at the end: with a weight, x[i] / sqrt(mean(x^2) + eps) * weight[i]; then with a rotation
+ * its first rot_dim dimensions turn in pairs, (i, i + rot_dim / 2), or (2 i, 2 i + 1) where they are interleaved: with
+ * angle = position * freq[i] (formed in 64 bits), c = magnitude cos(angle), s = magnitude sin(angle), (a, b) becomes (a c - b s, b c + a s).  The other dimensions are not turned. */
+typedef struct rsd_rope {
+    const double *freq;        /* dev [rot_dim / 2]: radians per position */
+    int32_t rot_dim;           /* even, 2 .. head_dim */
+    int32_t interleaved;
+    float magnitude;           /* 1: a rotation and nothing else */
+} rsd_rope;
+
+/* Frequencies theta^(-2 i / rot_dim), i < rot_dim / 2, and what makes them fit for contexts `factor` times as long as the `original` one:
+ *   RSD_ROPE_PLAIN   as they are
+ *   RSD_ROPE_LINEAR  all divided by factor
+ *   RSD_ROPE_BASE    theta becomes theta * factor^(rot_dim / (rot_dim - 2)), so that the first pair keeps its frequency and the last one's is divided by factor (rot_dim >= 4)
+ *   RSD_ROPE_PARTS   with r = original * frequency / 2 pi, the turns over the original context, and g = (r - low) / (high - low) cut to 0 .. 1:
+ *                        frequency * (g + (1 - g) / factor).  original > 0, high > low.
+ * freq: HOST [rot_dim / 2].  theta > 0, factor > 0. */
+enum { RSD_ROPE_PLAIN = 0, RSD_ROPE_LINEAR = 1, RSD_ROPE_BASE = 2, RSD_ROPE_PARTS = 3 };
+int rsd_rope_frequencies(double theta, int32_t rot_dim, int32_t kind, double factor, double original, double low, double high, double *freq);
+
+/* Heads of rows: x and out dev [rows][n_heads][head_dim] with row and head strides; weight dev [head_dim] of x's type, NULL: no norm. */
+typedef struct rsd_heads {
+    const void *x;
+    void *out;
+    const void *weight;
+    int64_t row, head, out_row, out_head;
+    int32_t n_heads;
+} rsd_heads;
+
+/* q and k (either may be NULL) to their out, in one pass.  position dev int32 [rows]; rope may be NULL (then position too).  head_dim 32, 64, 128 or 256, eps >= 0.  An out may be
+ * its x itself, and shares no memory with anything else that the call reads or writes.  rows * heads of both up to 2^26. */
+int rsd_qk_rope(const rsd_heads *q, const rsd_heads *k, const int32_t *position, const rsd_rope *rope, float eps, int32_t rows, int32_t head_dim,
+                  int32_t dtype, void *hip_stream);
+
+/* ---- a paged KV cache in bf16 or fp32 ----
+ * Pages of 16 tokens: pool dev [n_pages][n_kv_heads][2][16 * head_dim] of the cache's dtype, 16-byte aligned, the keys and the values of 16 tokens; table dev [batch][max_pages] (page of each sequence's
+ * 16 tokens, -1: none; pages may be shared by sequences that do not write to them); kv_len dev [batch], the entries of each sequence.  head_dim 32, 64 or 128.  The order
+ * of a sequence's entries is that of their slots: slot s stands in the s / 16-th page of the table.  Keys are stored as they are scored (normed and rotated).
+ * Inside a (page, kv head), E = values in 16 bytes (8 bf16, 4 fp32), token t of 16:
+ *   keys    [head_dim / 4E][4][16 t][E]             dimension 4E j + E c + i at [j][c][t][i]
+ *   values  [head_dim / 4E][4][16][E / 4][4]        dimension 4E j + 16 x + d at [j][t / 4][d][x][t % 4]
+ * Sizes: batch * n_kv_heads up to 2^20, max_pages up to 2^26 - 1; rows of a call that writes or reads entries times the heads it handles up to 2^26.
+ * Activations are of the cache's type, or fp32 over a bf16 cache. */
+typedef struct rsd_kv_cache {
+    void *pool;
+    const int32_t *table, *kv_len;
+    int32_t n_pages, n_kv_heads, head_dim, batch, max_pages, dtype;
+} rsd_kv_cache;
+
+/* Writes entries: row i (keys and values [n_kv_heads][head_dim], dev, of `dtype`) becomes slot[i] of sequence seq[i] (dev int32 [rows]; the pairs must differ), the keys as in
+ * rsd_qk_rope on their way (k->out is not used), both rounded once to the cache's type.  kv_len is neither read nor changed.  q (may be NULL) goes to q->out in
+ * the same launch, also for rows that name no entry of the cache.  q->out may be q->x and shares no memory with anything else of the call. */
+int rsd_kv_append(const rsd_kv_cache *c, const rsd_heads *k, const void *v, int64_t v_row, int64_t v_head, const rsd_heads *q, const int32_t *seq,
+                  const int32_t *slot, const int32_t *position, const rsd_rope *rope, float eps, int32_t rows, int32_t dtype, void *hip_stream);
+
+/* Reads entries back: k, v dev [rows][n_kv_heads][head_dim], contiguous, 16-byte aligned, of the cache's type; zeros for rows that name no entry of the cache. */
+int rsd_kv_read(const rsd_kv_cache *c, const int32_t *seq, const int32_t *slot, int32_t rows, void *k, void *v, void *hip_stream);
+
+/* Attention of new tokens over the cache (their own entries included).  Sequence b has the rows row_start[b] .. row_start[b + 1] - 1 (dev [batch + 1]; NULL: row b alone), at
+ * most max_rows of them (further ones are not computed), and n = min(kv_len[b], max_kv) entries.  Row j of its m rows stands at slot p = n - m + j and sees the
+ * slots s <= p that have a page and, with window > 0, lie near or at the front: s > p - window or s < sinks.  (Pages that no row sees any more are not read: the table may drop them.)
+ * q, out dev [rows][n_heads][head_dim] of `dtype` with row and head strides; head h reads kv head h / (n_heads / n_kv_heads).  out = softmax(scale q.K) V; a row
+ * that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of the sum of exp(scale q.k), -inf for such rows.  An infinity or NaN
+ * in an entry reaches the rows that see it and no others.  Sizes as for rsd_kv4_attention.  out may be q itself and shares no memory with it else. */
+typedef struct rsd_kv_attn {
+    const void *q;
+    void *out;
+    float *lse;
+    int64_t q_row, q_head, out_row, out_head;
+    const int32_t *row_start;
+    int32_t rows, max_rows, n_heads, max_kv, window, sinks, dtype;
+    float scale;
+} rsd_kv_attn;
+uint64_t rsd_kv_attention_workspace(const rsd_kv_cache *c, const rsd_kv_attn *a);
+int rsd_kv_attention(const rsd_kv_cache *c, const rsd_kv_attn *a, void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "librsd.so")
 LIB_DEBUG = os.path.join(HERE, "librsd_debug.so")
 ENGINE = os.path.join(HERE, "csrc", "rsd.hip")      # the engine (include/rsd.h)
-OPERATORS = os.path.join(HERE, "csrc", "ops.hip")   # the operators (include/rsd_ops.h)
+OPERATORS = [os.path.join(HERE, "csrc", n) for n in ("ops.hip", "ops_kv.hip")]      # the operators (include/rsd_ops.h): 4-bit memory, the bf16 / fp32 cache
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
 
@@ -33,10 +33,11 @@ def _finish(jobs: list, verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as tmp:
-        eng, dbg, ops = (os.path.join(tmp, n) for n in ("engine.o", "debug.o", "ops.o"))
+        eng, dbg = (os.path.join(tmp, n) for n in ("engine.o", "debug.o"))
+        ops = [os.path.join(tmp, os.path.basename(src) + ".o") for src in OPERATORS]
         _finish([_start(["hipcc", *FLAGS, *extra, "-c", "-o", o, src])
-                 for o, src, extra in ((eng, ENGINE, []), (dbg, ENGINE, ["-DRSD_DEBUG"]), (ops, OPERATORS, []))], verbose)
-        _finish([_start(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, o, ops])
+                 for o, src, extra in ((eng, ENGINE, []), (dbg, ENGINE, ["-DRSD_DEBUG"]), *((o, src, []) for o, src in zip(ops, OPERATORS)))], verbose)
+        _finish([_start(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, o, *ops])
                  for lib, o in ((LIB, eng), (LIB_DEBUG, dbg))], verbose)
     return LIB
 

@@ -1,4 +1,4 @@
-"""Operators of a decode step whose memory is 4 bits wide: the ctypes binding of ``include/rsd_ops.h``.
+"""Operators of a decode step, over memory 4 bits wide and over a paged cache in bf16 or fp32: the ctypes binding of ``include/rsd_ops.h``.
 
 Device buffers are torch tensors; every call goes to torch's current stream and returns without waiting.  Outputs and
 workspaces come from torch's allocator, so they follow its rules for streams and graphs.  A wrong argument raises
@@ -10,12 +10,19 @@ workspaces come from torch's allocator, so they follow its rules for streams and
 * ``rsd_kv4_append`` / ``rsd_kv4_read``: entries in and out.
 * ``rsd_kv4_attention``: attention over the cache, with the weight every entry received on request.
 * ``rsd_kv4_evict``: cuts each sequence back to a budget of entries by that weight.
+* ``rsd_rope``: a rotation by position, its frequencies scaled for long contexts if wanted.  ``rsd_qk_rope``: norms of the heads of queries and keys, and that
+  rotation, in one pass.
+* ``rsd_kv_cache``: an empty paged cache in bf16 or fp32.  A cache is any tuple ``(pool, table, kv_len)``: pages ``[n_pages, n_kv_heads, 2, 16 * head_dim]``, the rest as
+  above.
+* ``rsd_kv_append`` / ``rsd_kv_read``: entries in, keys normed and rotated on the way, and out.
+* ``rsd_kv_attention``: attention over the cache, with a sliding window and first tokens that stay visible if wanted.
 
-The format and the layouts are described in the header.
+The formats and the layouts are described in the header.
 """
 from __future__ import annotations
 
 import ctypes as C
+import math
 from functools import lru_cache
 from operator import index
 from typing import NamedTuple, Optional, Tuple
@@ -25,10 +32,11 @@ import torch
 from . import binding as _b
 
 __all__ = ["W4", "Kv4Cache", "rsd_w4_pack", "rsd_w4_linear", "rsd_kv4_cache", "rsd_kv4_append", "rsd_kv4_read", "rsd_kv4_attention",
-           "rsd_kv4_evict", "OPS_EXPORTED_SYMBOLS"]
+           "rsd_kv4_evict", "Rope", "KvCache", "rsd_rope", "rsd_qk_rope", "rsd_kv_cache", "rsd_kv_append", "rsd_kv_read", "rsd_kv_attention", "OPS_EXPORTED_SYMBOLS"]
 
 OPS_EXPORTED_SYMBOLS = ["rsd_op_last_error", "rsd_w4_pack", "rsd_w4_linear_workspace", "rsd_w4_linear", "rsd_kv4_append", "rsd_kv4_read",
-                        "rsd_kv4_attention_workspace", "rsd_kv4_attention", "rsd_kv4_evict_workspace", "rsd_kv4_evict"]
+                        "rsd_kv4_attention_workspace", "rsd_kv4_attention", "rsd_kv4_evict_workspace", "rsd_kv4_evict", "rsd_rope_frequencies",
+                        "rsd_qk_rope", "rsd_kv_append", "rsd_kv_read", "rsd_kv_attention_workspace", "rsd_kv_attention"]
 
 PAGE = 16
 _TYPE = {torch.float32: 0, torch.bfloat16: 1}
@@ -44,6 +52,19 @@ class W4(NamedTuple):
 
 
 class Kv4Cache(NamedTuple):
+    pool: torch.Tensor
+    table: torch.Tensor
+    kv_len: torch.Tensor
+
+
+class Rope(NamedTuple):
+    """A rotation: radians per position of every pair (float64 ``[rot_dim / 2]``), pairs (2 i, 2 i + 1) or (i, i + rot_dim / 2), what the result is multiplied by."""
+    freq: torch.Tensor
+    interleaved: bool
+    magnitude: float
+
+
+class KvCache(NamedTuple):
     pool: torch.Tensor
     table: torch.Tensor
     kv_len: torch.Tensor
@@ -69,6 +90,25 @@ class _Attn(C.Structure):
                 ("max_rows", C.c_int32), ("n_heads", C.c_int32), ("max_kv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
 
 
+class _Rope(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("weight", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64), ("out_row", C.c_int64),
+                ("out_head", C.c_int64), ("n_heads", C.c_int32)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [*_Cache._fields_, ("dtype", C.c_int32)]
+
+
+class _KvAttn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64),
+                ("out_row", C.c_int64), ("out_head", C.c_int64), ("row_start", C.c_void_p), ("rows", C.c_int32), ("max_rows", C.c_int32), ("n_heads", C.c_int32),
+                ("max_kv", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -87,7 +127,14 @@ def _load():
     lib.rsd_w4_linear_workspace.argtypes = [i32, i32, i32, i32]
     lib.rsd_kv4_attention_workspace.argtypes = [p, p, i32]
     lib.rsd_kv4_evict_workspace.argtypes = [p, i32]
-    for f in (lib.rsd_w4_linear_workspace, lib.rsd_kv4_attention_workspace, lib.rsd_kv4_evict_workspace):
+    f64, f32 = C.c_double, C.c_float
+    lib.rsd_rope_frequencies.argtypes = [f64, i32, i32, f64, f64, f64, f64, p]
+    lib.rsd_qk_rope.argtypes = [p, p, p, p, f32, i32, i32, i32, p]
+    lib.rsd_kv_append.argtypes = [p, p, p, i64, i64, p, p, p, p, p, f32, i32, i32, p]
+    lib.rsd_kv_read.argtypes = [p, p, p, i32, p, p, p]
+    lib.rsd_kv_attention_workspace.argtypes = [p, p]
+    lib.rsd_kv_attention.argtypes = [p, p, p, u64, p]
+    for f in (lib.rsd_w4_linear_workspace, lib.rsd_kv4_attention_workspace, lib.rsd_kv4_evict_workspace, lib.rsd_kv_attention_workspace):
         f.restype = u64
     _lib = lib
     return lib
@@ -349,3 +396,197 @@ def rsd_kv4_evict(cache, scores: torch.Tensor, entry_pos: torch.Tensor, budget: 
     nbytes = _evict_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, budget)
     ws, wp = _workspace(nbytes, pool)
     _done(lib.rsd_kv4_evict(C.byref(c), C.byref(book), budget, recent, wp, nbytes, st), lib)
+
+
+# ---- norms and rotation of queries and keys
+
+ROPE_KINDS = ("plain", "linear", "base", "parts")
+
+
+def rsd_rope(rot_dim: int, theta: float = 1e4, *, scaling: str = "plain", factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0,
+             magnitude: Optional[float] = None, interleaved: bool = False, device="cuda") -> Rope:
+    """A rotation of the first ``rot_dim`` dimensions of a head, with frequencies ``theta ** (-2 i / rot_dim)``.
+
+    ``scaling`` fits them for contexts ``factor`` times as long: "linear" divides all by ``factor``, "base" raises theta so that the last one is, "parts" divides those that turn less than ``low``
+    times over the ``original`` context, leaves those that turn more than ``high`` times, and goes over from one to the other between.  ``magnitude`` multiplies the rotated dimensions (default 1;
+    0.1 log(factor) + 1 for "parts" with a factor above 1)."""
+    lib = _lib or _load()
+    rot_dim = _int("rope: rot_dim", rot_dim, 2)
+    if scaling not in ROPE_KINDS:
+        _bad(f"rope: scaling {scaling!r}, needed one of {', '.join(ROPE_KINDS)}")
+    if rot_dim > 256:
+        _bad(f"rope: rot_dim {rot_dim}, at most 256")
+    freq = (C.c_double * (rot_dim // 2))()
+    _done(lib.rsd_rope_frequencies(theta, rot_dim, ROPE_KINDS.index(scaling), factor, original, low, high, freq), lib)
+    if magnitude is None:
+        magnitude = 0.1 * math.log(factor) + 1.0 if scaling == "parts" and factor > 1 else 1.0
+    return Rope(torch.tensor(list(freq), dtype=torch.float64, device=device), interleaved, magnitude)
+
+
+def _rope(rope, like: torch.Tensor, hd: int):
+    freq, interleaved, magnitude = rope
+    if freq.dtype is not torch.float64 or freq.device != like.device or freq.dim() != 1 or not freq.is_contiguous() or not 2 <= 2 * freq.shape[0] <= hd:
+        _bad(f"rope: the frequencies are {freq.dtype} {tuple(freq.shape)} on {freq.device}, needed float64 [1 .. {hd // 2}] on {like.device}, contiguous")
+    return _Rope(freq.data_ptr(), 2 * freq.shape[0], bool(interleaved), magnitude)
+
+
+def _heads(name: str, x: torch.Tensor, like: torch.Tensor, hd: int, weight: Optional[torch.Tensor], out: Optional[torch.Tensor], writes: bool):
+    """The heads of x, and where they go: (structure, out)."""
+    xp, xr, xh = _rows3(name, x, like, None, hd)
+    if x.dtype is not like.dtype or x.shape[0] != like.shape[0]:
+        _bad(f"{name}: {x.dtype} {tuple(x.shape)}, needed {like.dtype} and {like.shape[0]} rows")
+    wp = None if weight is None else _flat(name + "_weight", weight, like, like.dtype, (hd,))
+    if not writes:
+        return _Heads(xp, None, wp, xr, xh, 0, 0, x.shape[1]), None
+    if out is None:
+        out = x.new_empty(x.shape)
+    elif out.dtype is not x.dtype or out.shape != x.shape:
+        _bad(f"{name}_out: {out.dtype} {tuple(out.shape)}, needed {x.dtype} {tuple(x.shape)}")
+    op, orow, oh = _rows3(name + "_out", out, like, x.shape[1], hd)
+    return _Heads(xp, op, wp, xr, xh, orow, oh, x.shape[1]), out
+
+
+def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.Tensor], rope=None, *, q_weight: Optional[torch.Tensor] = None,
+                k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Heads ``q [rows, heads, head_dim]`` and ``k [rows, kv heads, head_dim]`` (may be None) normed over the head dimension, where they have a weight ``[head_dim]``, and
+    rotated by ``rope`` (may be None) at ``position`` (int32 ``[rows]``).  Returns ``(q_out, k_out)``; an out may be its input itself."""
+    lib = _lib or _load()
+    if q.dtype not in _TYPE or q.dim() != 3 or q.shape[2] not in (32, 64, 128, 256) or q.shape[1] == 0:
+        _bad(f"qk_rope: q is {q.dtype} {tuple(q.shape)}, needed fp32 or bf16 [rows, heads, 32, 64, 128 or 256]")
+    st = _stream(q)
+    rows, _, hd = q.shape
+    if k is None and (k_weight is not None or k_out is not None):
+        _bad("qk_rope: k_weight or k_out without k")
+    qs, q_out = _heads("q", q, q, hd, q_weight, q_out, True)
+    ks = None
+    if k is not None:
+        ks, k_out = _heads("k", k, q, hd, k_weight, k_out, True)
+    pp = rs = None
+    if rope is not None:
+        rs = C.byref(_rope(rope, q, hd))
+        if position is None:
+            _bad("qk_rope: a rotation without positions")
+        pp = _flat("position", position, q, _i32, (rows,))
+    if rows:
+        _done(lib.rsd_qk_rope(C.byref(qs), None if ks is None else C.byref(ks), pp, rs, eps, rows, hd, _TYPE[q.dtype], st), lib)
+    return q_out, k_out
+
+
+# ---- the cache in bf16 or fp32
+
+def rsd_kv_cache(batch: int, max_pages: int, n_pages: int, n_kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> KvCache:
+    """An empty cache: no sequence has pages or entries yet."""
+    return KvCache(torch.zeros(n_pages, n_kv_heads, 2, PAGE * head_dim, dtype=dtype, device=device),
+                   torch.full((batch, max_pages), -1, dtype=_i32, device=device), torch.zeros(batch, dtype=_i32, device=device))
+
+
+def _kv_cache(c) -> Tuple[_KvCache, torch.Tensor, int]:
+    pool, table, kv_len = c
+    st = _stream(pool)
+    shape, dev, t = pool.shape, pool.device, _TYPE.get(pool.dtype)
+    if t is None or len(shape) != 4 or shape[2] != 2 or shape[3] % PAGE or not pool.is_contiguous():
+        _bad(f"cache: the pool is {pool.dtype} {tuple(shape)}, needed fp32 or bf16 [pages, kv heads, 2, {PAGE} * head_dim], contiguous")
+    if table.dtype is not _i32 or table.device != dev or table.dim() != 2 or not table.is_contiguous():
+        _bad(f"cache: the table is {table.dtype} {tuple(table.shape)} on {table.device}, needed int32 [batch, pages] on {dev}, contiguous")
+    batch, max_pages = table.shape
+    if kv_len.dtype is not _i32 or kv_len.device != dev or kv_len.shape != (batch,) or not kv_len.is_contiguous():
+        _bad(f"cache: kv_len is {kv_len.dtype} {tuple(kv_len.shape)} on {kv_len.device}, needed int32 [{batch}] on {dev}, contiguous")
+    return _KvCache(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), shape[0], shape[1], shape[3] // PAGE, batch, max_pages, t), pool, st
+
+
+def rsd_kv_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, slot: torch.Tensor, *, position: Optional[torch.Tensor] = None, rope=None,
+                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                  q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Writes keys and values ``[rows, n_kv_heads, head_dim]`` into slot ``slot[i]`` of sequence ``seq[i]``, the keys normed (with ``k_weight``) and rotated (with ``rope``, at
+    ``position``) on their way; queries ``q [rows, heads, head_dim]`` of the same tokens go through the same in the same launch and are returned.  ``kv_len`` is left to the caller."""
+    lib = _lib or _load()
+    c, pool, st = _kv_cache(cache)
+    t = _TYPE.get(k.dtype)
+    if t is None or v.dtype is not k.dtype or v.shape != k.shape:
+        _bad(f"append: k is {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}; needed fp32 or bf16, alike")
+    hd = c.head_dim
+    if k.device != pool.device:
+        _bad(f"append: k is on {k.device}, the cache on {pool.device}")
+    ks, _ = _heads("k", k, k, hd, k_weight, None, False)
+    vp, vr, vh = _rows3("v", v, pool, c.n_kv_heads, hd)
+    rows = k.shape[0]
+    sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
+    qs = None
+    if q is not None:
+        qs, q_out = _heads("q", q, k, hd, q_weight, q_out, True)
+    elif q_weight is not None or q_out is not None:
+        _bad("append: q_weight or q_out without q")
+    pp = rs = None
+    if rope is not None:
+        rs = C.byref(_rope(rope, pool, hd))
+        if position is None:
+            _bad("append: a rotation without positions")
+        pp = _flat("position", position, pool, _i32, (rows,))
+    if rows:
+        _done(lib.rsd_kv_append(C.byref(c), C.byref(ks), vp, vr, vh, None if qs is None else C.byref(qs), sp, lp, pp, rs, eps, rows, t, st), lib)
+    return q_out
+
+
+def rsd_kv_read(cache, seq: torch.Tensor, slot: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values ``[rows, n_kv_heads, head_dim]`` of the entries (seq[i], slot[i]); zeros where there is none."""
+    lib = _lib or _load()
+    c, pool, st = _kv_cache(cache)
+    if seq.dim() != 1:
+        _bad(f"seq: shape {tuple(seq.shape)}, needed [rows]")
+    rows = seq.shape[0]
+    sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
+    k, v = pool.new_empty(2, rows, c.n_kv_heads, c.head_dim).unbind()
+    if rows:
+        _done(lib.rsd_kv_read(C.byref(c), sp, lp, rows, k.data_ptr(), v.data_ptr(), st), lib)
+    return k, v
+
+
+@lru_cache(maxsize=4096)
+def _kv_attn_bytes(n_pages, kv_heads, hd, batch, max_pages, cache_dtype, rows, max_rows, heads, max_kv, window, sinks, dtype, ragged) -> int:
+    # the sizes only; the addresses stand for "given"
+    c = _KvCache(16, 16, 16, n_pages, kv_heads, hd, batch, max_pages, cache_dtype)
+    a = _KvAttn(16, 16, None, 0, 0, 0, 0, 16 if ragged else None, rows, max_rows, heads, max_kv, window, sinks, dtype, 0.0)
+    return (_lib or _load()).rsd_kv_attention_workspace(C.byref(c), C.byref(a))
+
+
+def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, max_kv: Optional[int] = None,
+                     window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """Attention of the rows ``q [rows, n_heads, head_dim]`` over the cache, their own entries included.
+
+    Without ``row_start`` row b is sequence b's newest token; with it (``[batch + 1]`` int32) sequence b has the rows ``row_start[b] .. row_start[b + 1] - 1``, the last of which
+    stands at its last entry.  ``max_rows`` bounds the rows of a sequence (default: all of them could be one's): rows beyond it are not computed, and the first ``max_rows`` are taken for the
+    sequence's newest; their places in the result, like those of rows that no sequence has, are not written.  ``max_kv`` bounds ``kv_len`` (default: what the table can hold).  The tighter both are, the better the work is
+    dealt.  With ``window`` a row sees its own entry, the window - 1 before it, and a sequence's first ``sinks``.  ``out`` may be ``q`` itself.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
+    lib = _lib or _load()
+    c, pool, st = _kv_cache(cache)
+    t = _TYPE.get(q.dtype)
+    if t is None:
+        _bad(f"attention: q is {q.dtype}, needed fp32 or bf16")
+    qp, qr, qh = _rows3("q", q, pool, None, c.head_dim)
+    rows, heads = q.shape[0], q.shape[1]
+    if heads == 0 or heads % c.n_kv_heads:
+        _bad(f"attention: {heads} heads over {c.n_kv_heads} kv heads")
+    if row_start is None:
+        max_rows = 1 if max_rows is None else max_rows
+        if rows != c.batch or max_rows != 1:
+            _bad(f"attention: {rows} rows for {c.batch} sequences, max_rows {max_rows}, without row_start")
+        rp = None
+    else:
+        max_rows = rows if max_rows is None else max_rows
+        rp = _flat("row_start", row_start, pool, _i32, (c.batch + 1,))
+    window, sinks = _int("attention: window", window, 0), _int("attention: sinks", sinks, 0)
+    if out is None:
+        out = q.new_empty(rows, heads, c.head_dim)
+    elif out.dtype is not q.dtype or out.shape != q.shape:
+        _bad(f"attention: out is {out.dtype} {tuple(out.shape)}, needed {q.dtype} {tuple(q.shape)}")
+    op, orow, oh = _rows3("out", out, pool, heads, c.head_dim)
+    lse = q.new_empty(rows, heads, dtype=_f32) if want_lse else None
+    if rows:
+        max_rows = _int("attention: max_rows", max_rows, 1)
+        cap = c.max_pages * PAGE
+        max_kv = cap if max_kv is None else min(max(int(max_kv), -1), cap)
+        nbytes = _kv_attn_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, c.dtype, rows, max_rows, heads, max_kv, window, sinks, t, rp is not None)
+        ws, wp = _workspace(nbytes, pool)
+        a = _KvAttn(qp, op, lse.data_ptr() if want_lse else None, qr, qh, orow, oh, rp, rows, max_rows, heads, max_kv, window, sinks, t, scale)
+        _done(lib.rsd_kv_attention(C.byref(c), C.byref(a), wp, nbytes, st), lib)
+    return (out, lse) if want_lse else out
