@@ -13,6 +13,7 @@ struct KvcAttn {
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
     int total_rows, max_rows, heads, group;
     float factor2;          // |scale| * log2(e); never 0 or NaN
+    float inverse2;         // 1 / factor2
     bool negative;          // scale < 0: q changes its sign instead
     bool plain;             // scale is 0 or NaN: q is multiplied by it and factor2 is log2(e), so that -inf means "not seen" and nothing else
     float scale;
@@ -20,6 +21,7 @@ struct KvcAttn {
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
     int max_kv, window, sinks;
+    int ch;                 // slots of a chunk, or of a step of the kernel for many columns
     int lists, tiles, tile_cols;    // (sequence, kv head) pairs, tiles of columns of each
     int split, splits;      // chunks to a part, most parts
     bool by_length;         // the blocks of the longest sequences go first
@@ -36,14 +38,14 @@ __device__ __forceinline__ void kvc_rows(const KvcAttn& a, int b, int& r0, int& 
     }
     n = min(min(max(a.c.kv_len[b], 0), a.max_kv), a.c.max_pages * KVC_PAGE);
 }
-// What the columns col0 .. col1 - 1 of a sequence see, in chunks of CH slots: the first `front` chunks (sinks), then those from `from` on, `chunks` in all.
+// What the columns col0 .. col1 - 1 of a sequence see, in chunks (steps) of CH slots: the first `front` chunks (sinks), then those from `from` on, `chunks` in all.
 struct KvcSpan {
     int end;                // no column sees a slot from here on
     int safe;               // every column sees the slots below (those of the window: from `low` on)
     int near, low;          // some column's window begins at `near`, every column's has begun at `low`
     int front, from, chunks;
 };
-template <int CH> __device__ __forceinline__ KvcSpan kvc_span(const KvcAttn& a, int count, int n, int col0, int col1) {
+__device__ __forceinline__ KvcSpan kvc_span(const KvcAttn& a, int CH, int count, int n, int col0, int col1) {
     KvcSpan s;
     const int p0 = n - count + col0 / a.group, p1 = n - count + (col1 - 1) / a.group;      // slots of the first and the last row
     s.end = max(p1 + 1, 0);
@@ -58,10 +60,16 @@ template <int CH> __device__ __forceinline__ KvcSpan kvc_span(const KvcAttn& a, 
 // first slot of the i-th chunk
 template <int CH> __device__ __forceinline__ int kvc_slot(const KvcSpan& s, int i) { return (i < s.front ? i : i - s.front + s.from) * CH; }
 __device__ __forceinline__ int kvc_parts(const KvcAttn& a, const KvcSpan& s) { return a.splits == 1 ? 1 : max(1, (s.chunks + a.split - 1) / a.split); }
+// All bits where bit p of `there` is set.  (A mask that the compiler cannot look through: of branches on such a bit it has inverted one and not the other that went by the same comparison.)
+__device__ __forceinline__ int kvc_on(int there, int p) {
+    int on = -((there >> p) & 1);
+    asm("" : "+v"(on));
+    return on;
+}
 // what one column sees
 struct KvcColumn {
     int low, high, sinks;
-    __device__ __forceinline__ bool sees(int slot) const { return slot < high && (slot >= low || slot < sinks); }
+    __device__ __forceinline__ bool sees(int slot) const { return (slot < high) & ((slot >= low) | (slot < sinks)); }
 };
 __device__ __forceinline__ KvcColumn kvc_column(const KvcAttn& a, int count, int n, int col, int cols) {
     const int p = n - count + col / a.group;
@@ -108,7 +116,16 @@ template <typename T, typename C, int HD> struct KvcMath {
     static constexpr bool F32 = sizeof(C) == 4;
     static constexpr int N = L::N, PAGES = F32 ? 1 : 2, CH = PAGES * KVC_PAGE, PLANES = !F32 && sizeof(T) == 4 ? 3 : 1;
     struct Q { u32x4_t w[N][PLANES]; };
-    struct Entries { u32x4_t w[PAGES][N]; };        // keys, or values, of a chunk
+    struct Entries { u32x4_t w[PAGES][N]; };        // keys, or values, of a chunk as pages hold them
+    struct Values { u32x4_t w[HD / 16]; };          // values as operands: block d of 16 dims, rows (dims) lane % 16, tokens 4 (lane / 16) + i of the first page, then of the second
+    static __device__ __forceinline__ Values operands(const Entries& e) {
+        Values v;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+            if constexpr (F32) v.w[d] = e.w[0][d];
+            else v.w[d] = u32x4_t{e.w[0][d / 2][2 * (d & 1)], e.w[0][d / 2][2 * (d & 1) + 1], e.w[PAGES - 1][d / 2][2 * (d & 1)], e.w[PAGES - 1][d / 2][2 * (d & 1) + 1]};
+        return v;
+    }
 
     // operands of a tile of 16 columns: column lane % 16, dims 4E j + E (lane / 16) ..
     static __device__ __forceinline__ void load_q(const KvcAttn& a, int r0, int head, int col, int cols, int lane, Q& q) {
@@ -151,19 +168,24 @@ template <typename T, typename C, int HD> struct KvcMath {
     static __device__ __forceinline__ f32x4_t mfma4(uint32_t x, uint32_t y, f32x4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), __uint_as_float(y), c, 0, 0, 0);
     }
-    // scores of a page: rows (tokens) 4 (lane / 16) + i, column lane % 16
-    static __device__ __forceinline__ f32x4_t scores(const u32x4_t k[N], const Q& q) {
-        f32x4_t s = {};
+    // Scores of a chunk, rows (tokens) 4 (lane / 16) + i of each page, column lane % 16 of each tile.  The sums go side by side: a matrix instruction that waits for the one
+    // before it leaves the unit idle.
+    template <int NT> static __device__ __forceinline__ void scores(const Entries& k, const Q q[NT], f32x4_t s[NT][PAGES]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = 0; p < PAGES; ++p) s[t][p] = f32x4_t{};
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            if constexpr (F32) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s = mfma4(k[j][i], q.w[j][0][i], s);
-            } else {
+            for (int x = 0; x < (F32 ? 4 : PLANES); ++x)
 #pragma unroll
-                for (int x = 0; x < PLANES; ++x) s = q4_mfma(k[j], q.w[j][x], s);
-            }
-        return s;
+                for (int p = 0; p < PAGES; ++p)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if constexpr (F32) s[t][p] = mfma4(k.w[p][j][x], q[t].w[j][0][x], s[t][p]);
+                        else s[t][p] = q4_mfma(k.w[p][j], q[t].w[j][x], s[t][p]);
+                    }
     }
     // probabilities of a chunk as operands
     struct P { u32x4_t w[PLANES]; };
@@ -185,72 +207,99 @@ template <typename T, typename C, int HD> struct KvcMath {
             }
         return p;
     }
-    // o += V^T P^T, block d of 16 dims
-    static __device__ __forceinline__ void gather(const Entries& v, const P& p, f32x4_t o[HD / 16]) {
+    // o += V^T P^T, block d of 16 dims, for every tile; sums side by side
+    template <int NT> static __device__ __forceinline__ void gather(const Values& v, const P p[NT], f32x4_t o[NT][HD / 16]) {
+        constexpr int SIDE = HD / 16 < 4 ? HD / 16 : 4;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if constexpr (F32) {
+        for (int d0 = 0; d0 < HD / 16; d0 += SIDE)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[j] = mfma4(v.w[0][j][i], p.w[0][i], o[j]);
-            } else {
-                const u32x4_t x = v.w[0][j], y = v.w[1][j], lo = {x[0], x[1], y[0], y[1]}, hi = {x[2], x[3], y[2], y[3]};
+            for (int e = 0; e < (F32 ? 4 : PLANES); ++e)
 #pragma unroll
-                for (int e = 0; e < PLANES; ++e) {
-                    o[2 * j] = q4_mfma(lo, p.w[e], o[2 * j]);
-                    o[2 * j + 1] = q4_mfma(hi, p.w[e], o[2 * j + 1]);
-                }
-            }
+                for (int d = d0; d < d0 + SIDE; ++d)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if constexpr (F32) o[t][d] = mfma4(v.w[d][e], p[t].w[0][e], o[t][d]);
+                        else o[t][d] = q4_mfma(v.w[d], p[t].w[e], o[t][d]);
+                    }
     }
     // Whether a value among the entries is an infinity or a NaN: 0 times it is not 0.
-    static __device__ __forceinline__ bool unbounded(const Entries& v) {
+    static __device__ __forceinline__ bool unbounded(const Values& v) {
         f32x4_t z = {};
-        P zero;
 #pragma unroll
-        for (int e = 0; e < PLANES; ++e) zero.w[e] = u32x4_t{};
-        f32x4_t all[HD / 16];
+        for (int d = 0; d < HD / 16; ++d)
+            if constexpr (F32) {
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) all[d] = z;
-        gather(v, zero, all);
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) z += all[d];
+                for (int i = 0; i < 4; ++i) z = mfma4(v.w[d][i], 0u, z);
+            } else z = q4_mfma(v.w[d], u32x4_t{}, z);
         return __any(!(z[0] + z[1] + z[2] + z[3] == 0.f));
     }
-    // Values of the entries that no column of the tile sees, cleared: what lies there may be NaN, and 0 * NaN is NaN.  `seen(slot)`: some column does.
-    template <typename F> static __device__ __forceinline__ void clear(Entries& v, int slot0, int there, F seen) {
+    // slot of the tokens that dword i of an operand holds (the first of two in bf16)
+    static __device__ __forceinline__ int slot_of(int slot0, int i) {
         const int quad = (threadIdx.x & 63) >> 4;
-#pragma unroll
-        for (int p = 0; p < PAGES; ++p) {
-            const int at = slot0 + p * KVC_PAGE + quad * 4;
-            uint32_t m[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m[i] = ((there >> p) & 1) && seen(at + i) ? 0xFFFFFFFFu : 0u;
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if constexpr (F32) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v.w[p][j][i] &= m[i];
-                } else {
-                    const uint32_t a = (m[0] & 0xFFFFu) | (m[1] & 0xFFFF0000u), b = (m[2] & 0xFFFFu) | (m[3] & 0xFFFF0000u);
-                    v.w[p][j] &= u32x4_t{a, b, a, b};
-                }
-        }
+        return F32 ? slot0 + quad * 4 + i : slot0 + i / 2 * KVC_PAGE + quad * 4 + 2 * (i & 1);
     }
-    // The second product value by value, for a chunk that holds an infinity or a NaN which some columns must not meet
-    static __device__ void gather_one_by_one(const C* const page[PAGES], int there, int slot0, const f32x4_t s[PAGES], const KvcColumn& see, f32x4_t o[HD / 16]) {
-        const int lane = threadIdx.x & 63, quad = lane >> 4;
+    // Values of the entries that no column of the tile sees, cleared: what lies there may be NaN, and 0 * NaN is NaN.
+    static __device__ __forceinline__ void clear(Values& v, int slot0, int there, const KvcSpan& span, int sinks) {
+        u32x4_t m;
 #pragma unroll
-        for (int p = 0; p < PAGES; ++p)
+        for (int i = 0; i < 4; ++i) {
+            const int slot = slot_of(slot0, i), end = span.end & kvc_on(there, F32 ? 0 : i / 2);
+            auto seen = [&](int at) { return (at < end) & ((at >= span.near) | (at < sinks)); };
+            m[i] = F32 ? -(uint32_t)seen(slot) : (-(uint32_t)seen(slot) & 0xFFFFu) | (-(uint32_t)seen(slot + 1) & 0xFFFF0000u);
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll 1
-                for (int from = 0; from < 4; ++from) {
-                    const float w = __shfl(s[p][i], from * 16 + (lane & 15), 64);
-                    if (!((there >> p) & 1) || !see.sees(slot0 + p * KVC_PAGE + from * 4 + i)) continue;
+        for (int d = 0; d < HD / 16; ++d) v.w[d] &= m;
+    }
+    // Infinities and NaN among the values reach the columns that see them and no others: products of marks (rows: dims) and of what is seen, shaped like the one of values and
+    // probabilities, count them; `strip` takes them out of the values.
+    static __device__ __forceinline__ uint32_t strip1(uint32_t w) {
+        if constexpr (F32) return (w & 0x7F800000u) == 0x7F800000u ? 0u : w;
+        return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void strip(Values& v) {
 #pragma unroll
-                    for (int d = 0; d < HD / 16; ++d)
+        for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[d][e] = __builtin_fmaf(w, ld1(page[p] + L::value(from * 4 + i, d * 16 + quad * 4 + e)), o[d][e]);
+            for (int i = 0; i < 4; ++i) v.w[d][i] = strip1(v.w[d][i]);
+    }
+    // 1 where a value is `what` (bits of its type), or NaN where what is 0
+    static __device__ __forceinline__ uint32_t mark1(uint32_t w, uint32_t what) {
+        if constexpr (F32) return (what ? w == what : (w & 0x7FFFFFFFu) > 0x7F800000u) ? 0x3F800000u : 0u;
+        const uint32_t lo = w & 0xFFFFu, hi = w >> 16;
+        return ((what ? lo == what : (lo & 0x7FFFu) > 0x7F80u) ? 0x3F80u : 0u) | ((what ? hi == what : (hi & 0x7FFFu) > 0x7F80u) ? 0x3F800000u : 0u);
+    }
+    template <int NT> static __device__ __forceinline__ void add_unbounded(const Values& v, const KvcColumn see[NT], int slot0, f32x4_t o[NT][HD / 16]) {
+        u32x4_t sees[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int slot = slot_of(slot0, i);
+                if constexpr (F32) sees[t][i] = see[t].sees(slot) ? 0x3F800000u : 0u;
+                else sees[t][i] = (see[t].sees(slot) ? 0x3F80u : 0u) | (see[t].sees(slot + 1) ? 0x3F800000u : 0u);
+            }
+        constexpr uint32_t PLUS = F32 ? 0x7F800000u : 0x7F80u, MINUS = F32 ? 0xFF800000u : 0xFF80u;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+            for (int kind = 0; kind < 3; ++kind) {
+                const uint32_t what = kind == 0 ? PLUS : kind == 1 ? MINUS : 0u;
+                const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __uint_as_float(0x7FC00000u);
+                u32x4_t mark;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mark[i] = mark1(v.w[d][i], what);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    f32x4_t many = {};
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) many = mfma4(mark[i], sees[t][i], many);
+                    } else many = q4_mfma(mark, sees[t], many);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][d][e] += many[e] > 0.f ? add : 0.f;
                 }
+                __builtin_amdgcn_sched_barrier(0);          // (marks of one block and kind at a time: registers)
+            }
     }
 };
 
@@ -267,31 +316,33 @@ template <typename C, int HD, int PAGES> __device__ __forceinline__ void kvc_pag
     }
 }
 
-// Scores of a chunk -> probabilities in their place; the maximum moves where it has to, and what was gathered is scaled.  factor2 > 0; top is in units of the exponent.
+// The running state of a lane's column.  `top`, in units of the exponent (base 2), is the same in its four lanes, `sum` each lane's own.
+struct KvcRun {
+    float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;      // base: top, or 0 where that is -inf; limit: of scores that need no new maximum
+};
+// Scores of a chunk -> probabilities in their place; the maximum moves, and what was gathered is scaled, only where a score passes it by 2^8 (probabilities up to 2^8 lose nothing
+// in 32 bits, nor in bf16): seldom after the first chunks, so the lanes of a column exchange their maxima there and nowhere else.  factor2 > 0.
 template <int PAGES, int NB>
-__device__ __forceinline__ void kvc_softmax(f32x4_t s[PAGES], float factor2, float& top, float& sum, f32x4_t o[NB]) {
-    float best = -INFINITY;
+__device__ __forceinline__ void kvc_softmax(f32x4_t s[PAGES], const KvcAttn& a, KvcRun& r, f32x4_t o[NB]) {
+    float best = s[0][0];
 #pragma unroll
-    for (int p = 0; p < PAGES; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) best = fmaxf(best, s[p][i]);
-    best = rows4_max(best);
-    best = fmaxf(top, best * factor2);
-    // (probabilities up to 2^8 lose nothing in 32 bits, nor in bf16)
-    if (__any(best > top + 8.f)) {
-        const float scale = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.f : best));
-        sum *= scale;
+    for (int i = 1; i < 4 * PAGES; ++i) best = fmaxf(best, s[i / 4][i % 4]);
+    if (__any(best > r.limit)) {
+        const float top = fmaxf(r.top, rows4_max(best) * a.factor2), base = top == -INFINITY ? 0.f : top;
+        const float scale = __builtin_amdgcn_exp2f(r.top - base);
+        r.sum *= scale;
 #pragma unroll
         for (int d = 0; d < NB; ++d) o[d] *= scale;
-        top = best;
+        r.top = top;
+        r.base = base;
+        r.limit = (top + 8.f) * a.inverse2;
     }
-    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int p = 0; p < PAGES; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[p][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], factor2, -base));
-            sum += s[p][i];
+            s[p][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], a.factor2, -r.base));
+            r.sum += s[p][i];
         }
 }
 // what a column has gathered, rows (dims) dim .. + 3, to its place or to the join
@@ -309,35 +360,36 @@ __device__ __forceinline__ void kvc_finish(const KvcAttn& a, int64_t row, int qh
     else *reinterpret_cast<f32x4_any_t*>(dst) = acc * inv;
     if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
 }
-// One chunk against one tile of columns, keys and values as operands: the scores, then `border` decides what has to be masked
-template <typename M, int HD, typename C>
-__device__ __forceinline__ void kvc_chunk(const KvcAttn& a, const typename M::Q& q, const typename M::Entries& k, typename M::Entries& v, const C* const page[M::PAGES], int there,
-                                          int slot0, const KvcSpan& span, const KvcColumn& see, float& top, float& sum, f32x4_t o[HD / 16]) {
+// Scores that a column must not see, where a chunk is not seen whole by all of them
+template <typename M, int NT> __device__ __forceinline__ void kvc_mask_scores(const KvcColumn see[NT], int slot0, int there, f32x4_t s[NT][M::PAGES]) {
     const int quad = (threadIdx.x & 63) >> 4;
-    f32x4_t s[M::PAGES];
 #pragma unroll
-    for (int p = 0; p < M::PAGES; ++p) s[p] = M::scores(k.w[p], q);
-    // every column sees all of it: it ends before the first row's slot, and begins in every window or ends among the sinks
-    const bool whole = there == (1 << M::PAGES) - 1 && slot0 + M::CH <= span.safe && (slot0 >= span.low || slot0 + M::CH <= a.sinks);
-    if (whole) {
-        kvc_softmax<M::PAGES, HD / 16>(s, a.factor2, top, sum, o);
-        M::gather(v, M::weights(s), o);
-        return;
-    }
-    M::clear(v, slot0, there, [&](int slot) { return slot < span.end && (slot >= span.near || slot < a.sinks); });
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int p = 0; p < M::PAGES; ++p)
+        for (int p = 0; p < M::PAGES; ++p) {
+            const KvcColumn c{see[t].low, see[t].high & kvc_on(there, p), see[t].sinks};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[p][i] = ((there >> p) & 1) && see.sees(slot0 + p * KVC_PAGE + quad * 4 + i) ? s[p][i] : -INFINITY;
-    kvc_softmax<M::PAGES, HD / 16>(s, a.factor2, top, sum, o);
-    if (M::unbounded(v)) M::gather_one_by_one(page, there, slot0, s, see, o);
-    else M::gather(v, M::weights(s), o);
+            for (int e = 0; e < 4; ++e) s[t][p][e] = c.sees(slot0 + p * KVC_PAGE + quad * 4 + e) ? s[t][p][e] : -INFINITY;
+        }
+}
+// every column sees all of the chunk: it ends before the first row's slot, and begins in every window or ends among the sinks
+template <typename M> __device__ __forceinline__ bool kvc_whole(const KvcAttn& a, const KvcSpan& span, int slot0, int there) {
+    return there == (1 << M::PAGES) - 1 && slot0 + M::CH <= span.safe && (slot0 >= span.low || slot0 + M::CH <= a.sinks);
+}
+// The values of such a chunk: what no column sees is cleared, and an infinity or a NaN must not reach the columns that do not see it, as 0 times it
+template <typename M, int HD, int NT>
+__device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan& span, const KvcColumn see[NT], int slot0, int there, typename M::Values& v, f32x4_t o[NT][HD / 16]) {
+    M::clear(v, slot0, there, span, a.sinks);
+    if (!M::unbounded(v)) return;
+    M::template add_unbounded<NT>(v, see, slot0, o);
+    M::strip(v);
 }
 
-// A block owns a tile of 16 columns of one (sequence, kv head) and one part of its chunks, which its waves take in turn, each with its own running
-// maximum and sum; they are joined in LDS.  The next chunk is requested before this one is worked on, the table entries one chunk earlier still.
+// Few columns (single tokens): a block owns a tile of 16 columns of one (sequence, kv head) and one part of its chunks, which its waves take in
+// turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's keys are requested as soon as this one's are used up, the values likewise, the table entries
+// one chunk earlier still.
 template <typename T, typename C, int HD>
-__global__ __launch_bounds__(512, 2) void kvc_attn_kernel(KvcAttn a) {
+__global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;
     constexpr int NB = HD / 16, WAVES = 8;
     __shared__ __align__(16) float lds_o[WAVES][NB][64][4];
@@ -350,52 +402,58 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_kernel(KvcAttn a) {
     kvc_rows(a, b, r0, count, n);
     const int cols = count * a.group;
     if (col0 >= cols) return;
-    const KvcSpan span = kvc_span<M::CH>(a, count, n, col0, min(cols, col0 + 16));
+    const KvcSpan span = kvc_span(a, M::CH, count, n, col0, min(cols, col0 + 16));
     const int parts = kvc_parts(a, span);
     if ((int)blockIdx.y >= parts) return;
-    const KvcColumn see = kvc_column(a, count, n, col, cols);
     const int end = min((int)(blockIdx.y + 1) * a.split, span.chunks);
 
-    typename M::Entries k[2], v[2];
-    const C* page[3][M::PAGES];                             // of the chunk worked on, the next one, the one after it
-    int there[3];
-    typename M::Q q;
-    f32x4_t o[NB] = {};
-    float top = -INFINITY, sum = 0.f;
-    auto load = [&](const C* const pg[M::PAGES], typename M::Entries& k_, typename M::Entries& v_) {
+    typename M::Entries k, v;
+    typename M::Q q[1];
+    const KvcColumn see[1] = {kvc_column(a, count, n, col, cols)};
+    f32x4_t o[1][NB] = {};
+    KvcRun run;
+    int i = blockIdx.y * a.split + wave;
+    // (past the end the wave's last chunk is requested again)
+    auto table = [&](int i, const C* pg[M::PAGES], int& there_) { kvc_pages<C, HD, M::PAGES>(a.c, b, head, kvc_slot<M::CH>(span, i < end ? i : end - 1 - (end - 1 - wave + waves * 4096) % waves), pg, there_); };
+    auto load = [&](const C* const pg[M::PAGES], int offset, typename M::Entries& e) {
 #pragma unroll
         for (int p = 0; p < M::PAGES; ++p)
 #pragma unroll
-            for (int j = 0; j < M::N; ++j) {
-                k_.w[p][j] = reinterpret_cast<const u32x4_t*>(pg[p])[j * 64 + lane];
-                v_.w[p][j] = reinterpret_cast<const u32x4_t*>(pg[p] + KVC_PAGE * HD)[j * 64 + lane];
-            }
+            for (int j = 0; j < M::N; ++j) e.w[p][j] = reinterpret_cast<const u32x4_t*>(pg[p] + offset)[j * 64 + lane];
     };
-    auto table = [&](int i, const C* pg[M::PAGES], int& there_) { kvc_pages<C, HD, M::PAGES>(a.c, b, head, kvc_slot<M::CH>(span, min(i, max(span.chunks - 1, 0))), pg, there_); };
-    int i = blockIdx.y * a.split + wave;
-    M::load_q(a, r0, head, col, cols, lane, q);
+    const C* page[M::PAGES];                                // of the chunk whose entries are requested next
+    int there = 0, there_next = 0;
     if (i < end) {
-        table(i, page[0], there[0]);
-        load(page[0], k[0], v[0]);
-        table(i + waves, page[1], there[1]);
+        table(i, page, there);
+        load(page, 0, k);
+        load(page, KVC_PAGE * HD, v);
+        table(i + waves, page, there_next);
     }
-    while (i < end) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (i + waves < end) load(page[1], k[1 - u], v[1 - u]);
-            table(i + 2 * waves, page[2], there[2]);
-            kvc_chunk<M, HD, C>(a, q, k[u], v[u], page[0], there[0], kvc_slot<M::CH>(span, i), span, see, top, sum, o);
-#pragma unroll
-            for (int p = 0; p < M::PAGES; ++p) page[0][p] = page[1][p], page[1][p] = page[2][p];
-            there[0] = there[1], there[1] = there[2];
-            i += waves;
-            if (i >= end) break;
-        }
+    M::load_q(a, r0, head, col, cols, lane, q[0]);
+    for (; i < end; i += waves) {
+        const int slot0 = kvc_slot<M::CH>(span, i);
+        f32x4_t s[1][M::PAGES];
+        M::template scores<1>(k, q, s);
+        __builtin_amdgcn_sched_barrier(0);
+        load(page, 0, k);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool whole = kvc_whole<M>(a, span, slot0, there);
+        if (!whole) kvc_mask_scores<M, 1>(see, slot0, there, s);
+        kvc_softmax<M::PAGES, NB>(s[0], a, run, o[0]);
+        typename M::Values vo = M::operands(v);
+        if (!whole) kvc_bound_values<M, HD, 1>(a, span, see, slot0, there, vo, o);
+        const typename M::P w[1] = {M::weights(s[0])};
+        M::template gather<1>(vo, w, o);
+        __builtin_amdgcn_sched_barrier(0);
+        load(page, KVC_PAGE * HD, v);
+        there = there_next;
+        table(i + 2 * waves, page, there_next);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    sum = rows4_sum(sum);
-    if (quad == 0) lds_ml[wave][0][lane] = top, lds_ml[wave][1][lane] = sum;
+    const float sum = rows4_sum(run.sum);
+    if (quad == 0) lds_ml[wave][0][lane] = run.top, lds_ml[wave][1][lane] = sum;
 #pragma unroll
-    for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(lds_o[wave][d][lane]) = o[d];
+    for (int d = 0; d < NB; ++d) *reinterpret_cast<f32x4_t*>(lds_o[wave][d][lane]) = o[0][d];
     __syncthreads();
     for (int d = wave; d < NB; d += waves) {
         const int c = lane & 15;
@@ -412,8 +470,157 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_kernel(KvcAttn a) {
     }
 }
 
-// Joins the parts of the entries: 16 lanes per (row, head), HD / 16 dims each, 16 parts' maxima and sums at once.  CH: slots to a chunk.
-template <typename T, int HD, int CH>
+// COUNT KB straight into LDS, 16 bytes to a lane and instruction (the instruction's offset goes into both addresses)
+template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint32_t lane16, const char* base) {
+    if constexpr (COUNT > 4) {
+        kvc_copy<4>(lds, lane16, base);
+        kvc_copy<COUNT - 4>(lds + 4096, lane16, base + 4096);
+    } else if constexpr (COUNT == 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+    else if constexpr (COUNT == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+}
+
+// Many columns (chunks of prompts, steps, scoring): a block of four waves owns 64 * NT columns, NT tiles to a wave, and one part of their steps of U chunks.  The steps go through a ring of
+// R stages in LDS, straight from memory (pages are operands as they are), a quarter of each by every wave.  The one barrier of a step stands in the middle of its last chunk,
+// when all of the step's operands are in registers: behind it the next step's keys are read and this one's stage is requested anew.
+template <typename T, typename C, int HD, int NT> struct KvcMany {
+    static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);
+    static constexpr int U = SMALL ? 1 : 2, R = SMALL ? 3 : 2, WAVES = SMALL ? 3 : 2, CH = U * KvcMath<T, C, HD>::CH;       // WAVES: to a SIMD; CH: slots of a step
+};
+template <typename T, typename C, int HD, int NT>
+__global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_many_kernel(KvcAttn a) {
+    typedef KvcMath<T, C, HD> M;
+    typedef KvcLayout<C, HD> L;
+    typedef KvcMany<T, C, HD, NT> K;
+    constexpr int NB = HD / 16, N = M::N, U = K::U, R = K::R, CH = K::CH, PAGES = U * M::PAGES, OWN = PAGES * 2 * N / 4, COLS = 64 * NT;      // a wave requests OWN of a stage's KB
+    constexpr int SPAN = 64 / PAGES;                        // steps whose table entries a wave holds, one to a lane
+    static_assert(2 * N % OWN == 0, "a wave's share lies in one page");
+    __shared__ u32x4_t ring[R][PAGES][2 * N][64];           // keys, then values of each page
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+    int list, tile;
+    if (!kvc_work(a, blockIdx.x, list, tile)) return;
+    const int b = kvc_by_length(a, list / a.c.hkv), head = list % a.c.hkv, col0 = tile * COLS;
+    int r0, count, n;
+    kvc_rows(a, b, r0, count, n);
+    const int cols = count * a.group;
+    if (col0 >= cols) return;
+    const KvcSpan span = kvc_span(a, CH, count, n, col0, min(cols, col0 + COLS));
+    const int parts = kvc_parts(a, span);
+    if ((int)blockIdx.y >= parts) return;
+    const int begin = blockIdx.y * a.split, end = min(begin + a.split, span.chunks);
+    // this wave's columns, what they see, and the steps that all of them see whole (but for missing pages)
+    const int colw = col0 + wave * 16 * NT;
+    const bool mine = colw < cols;
+    const KvcSpan own = kvc_span(a, CH, count, n, min(colw, cols - 1), min(cols, colw + 16 * NT));
+    const int whole0 = max(span.front, span.front + (own.low + CH - 1) / CH - span.from), whole1 = mine ? span.front + own.safe / CH - span.from : 0;
+    KvcColumn see[NT];
+    typename M::Q q[NT];
+    f32x4_t o[NT][NB];
+    KvcRun run[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int col = colw + 16 * t + (lane & 15);
+        see[t] = kvc_column(a, count, n, col, cols);
+        M::load_q(a, r0, head, col, cols, lane, q[t]);
+#pragma unroll
+        for (int d = 0; d < NB; ++d) o[t][d] = f32x4_t{};
+    }
+    int ids = 0, ids_from = begin - SPAN;                   // of the step ids_from + lane / PAGES, its page lane % PAGES
+    uint64_t ids_there = 0;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring + wave * OWN * 1024;
+    auto request = [&](int i, int stage) {                  // returns which of the step's pages are there
+        i = min(i, end - 1);
+        if (i - ids_from >= SPAN) {
+            ids_from = i;
+            const int at = kvc_slot<CH>(span, min(i + lane / PAGES, span.chunks - 1)) / KVC_PAGE + lane % PAGES;
+            ids = at < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + at] : -1;
+            if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
+            asm volatile("" : "+v"(ids));                   // (waited for here, not at every use)
+            ids_there = __ballot(ids >= 0);
+        }
+        const int at = (i - ids_from) * PAGES;
+        const int id = max(__builtin_amdgcn_readlane(ids, at + wave * OWN / (2 * N)), 0);
+        const char* src = a.c.pool + ((int64_t)id * a.c.hkv + head) * (L::BLOCK * (int64_t)sizeof(C)) + wave * OWN % (2 * N) * 1024;
+        kvc_copy<OWN>(lds0 + stage * (PAGES * 2 * N * 1024), lane * 16, src);
+        return (int)(ids_there >> at) & ((1 << PAGES) - 1);
+    };
+    typename M::Entries k, v;
+    auto read_k = [&](int stage, int u) {
+#pragma unroll
+        for (int x = 0; x < M::PAGES * N; ++x) k.w[x / N][x % N] = ring[stage][u * M::PAGES + x / N][x % N][lane];
+    };
+    auto read_v = [&](int stage, int u) {
+#pragma unroll
+        for (int x = 0; x < M::PAGES * N; ++x) v.w[x / N][x % N] = ring[stage][u * M::PAGES + x / N][N + x % N][lane];
+    };
+    if (begin < end) {
+        int there[R];                                       // of this step, the next one, ...
+#pragma unroll
+        for (int i = 0; i < R; ++i) there[i] = request(begin + i, i);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((R - 1) * OWN) : "memory");
+        read_k(0, 0);
+        int stage = 0;
+        auto turn = [&](int i) {                            // the next step's entries have landed, this one's are in registers
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((R - 2) * OWN) : "memory");
+            const int last = request(i + R, stage);
+#pragma unroll
+            for (int x = 0; x + 1 < R; ++x) there[x] = there[x + 1];
+            there[R - 1] = last;
+            stage = stage == R - 1 ? 0 : stage + 1;
+            read_k(stage, 0);
+        };
+        auto step = [&](auto border, int i) {
+            const int there_i = there[0], slot = border.value ? kvc_slot<CH>(span, i) : 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int slot0 = slot + u * M::CH, there0 = there_i >> (u * M::PAGES);
+                read_v(stage, u);
+                f32x4_t s[NT][M::PAGES];
+                M::template scores<NT>(k, q, s);
+                if constexpr (border.value) kvc_mask_scores<M, NT>(see, slot0, there0, s);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) kvc_softmax<M::PAGES, NB>(s[t], a, run[t], o[t]);
+                typename M::Values vo;
+                if constexpr (border.value) {
+                    vo = M::operands(v);
+                    kvc_bound_values<M, HD, NT>(a, own, see, slot0, there0, vo, o);
+                }
+                if (u == U - 1) turn(i);
+                else read_k(stage, u + 1);
+                if constexpr (!border.value) vo = M::operands(v);
+                typename M::P w[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) w[t] = M::weights(s[t]);
+                M::template gather<NT>(vo, w, o);
+            }
+        };
+        for (int i = begin; i < end; ++i) {
+            // (a loop of its own for what needs no mask: where the two kinds of steps met in one, the rare one cost the other copies of its operands)
+            for (; i >= whole0 && i < min(end, whole1) && there[0] == (1 << PAGES) - 1; ++i) step(std::false_type{}, i);
+            if (i >= end) break;
+            const int slot0 = kvc_slot<CH>(span, i);
+            if (!mine || slot0 >= own.end || (slot0 + CH <= own.near && slot0 >= a.sinks)) turn(i);      // (the other waves need this one's copies)
+            else step(std::true_type{}, i);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // nothing is in flight into LDS when the block ends
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int col = colw + 16 * t + (lane & 15);
+        const float total = rows4_sum(run[t].sum);
+        if (col < cols)
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+                kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[t][d], run[t].top, total, blockIdx.y, parts);
+    }
+}
+
+// Joins the parts of the entries: 16 lanes per (row, head), HD / 16 dims each, 16 parts' maxima and sums at once.
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvc_join_kernel(KvcAttn a) {
     constexpr int N = HD / 16;
     const int l = threadIdx.x & 15;
@@ -424,7 +631,7 @@ __global__ __launch_bounds__(256) void kvc_join_kernel(KvcAttn a) {
     kvc_rows(a, b, r0, count, n);
     if (r >= count) return;
     const int cols = count * a.group, col0 = (r * a.group + qh % a.group) / a.tile_cols * a.tile_cols;
-    const KvcSpan span = kvc_span<CH>(a, count, n, col0, min(cols, col0 + a.tile_cols));
+    const KvcSpan span = kvc_span(a, a.ch, count, n, col0, min(cols, col0 + a.tile_cols));
     const int parts = kvc_parts(a, span);
     if (parts == 1) return;                                 // a single part went to its place
     const int64_t row = r0 + r, at = (row * a.heads + qh) * a.splits;

@@ -140,33 +140,43 @@ template <typename T, typename C> void append_run(const RowArgs& a, const KvcRow
 // ---- attention
 
 struct AttnPlan {
-    int lists, tiles, tile_cols, waves, split, splits;
-    bool by_length;
+    int lists, tiles, tile_cols, ch, waves, split, splits;
+    bool many, by_length;
     uint64_t o_bytes, ml_bytes;
     uint64_t bytes() const { return o_bytes + ml_bytes; }
 };
-int chunk_slots(const rsd_kv_cache* c) { return c->dtype == RSD_F32 ? KVC_PAGE : 2 * KVC_PAGE; }
 // a window that no row reaches past is none
 int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >= std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KVC_PAGE) ? 0 : a->window; }
 
 AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     AttnPlan p{};
-    const int group = a->n_heads / c->n_kv_heads, ch = chunk_slots(c), window = window_of(c, a);
+    const int group = a->n_heads / c->n_kv_heads, window = window_of(c, a);
     const int64_t cols = (int64_t)a->max_rows * group, max_kv = std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KVC_PAGE);
     p.lists = c->batch * c->n_kv_heads;
-    p.tile_cols = 16;
+    const bool parts3 = c->dtype == RSD_BF16 && a->dtype == RSD_F32;
+    p.many = cols > 16;
+    p.tile_cols = !p.many ? 16 : parts3 || c->dtype == RSD_F32 || cols <= 64 ? 64 : 128;
     p.tiles = (int)ceil_div(cols, p.tile_cols);
+    // slots of a chunk, or of a step of the kernel for many columns
+    p.ch = (c->dtype == RSD_F32 ? 1 : 2) * KVC_PAGE * (p.many && (parts3 || p.tile_cols == 128) ? 2 : 1);
+    const int ch = p.ch;
     int64_t chunks = std::max<int64_t>(1, ceil_div(max_kv, ch));
     if (window) {
         const int64_t rows = std::min<int64_t>(a->max_rows, (p.tile_cols + group - 2) / group + 1);      // that share a tile
         chunks = std::min(chunks, ceil_div(std::min<int64_t>(a->sinks, max_kv), ch) + ceil_div((int64_t)window + rows - 1, ch) + 1);
     }
     const int64_t base = (int64_t)p.lists * p.tiles;
-    p.waves = (int)std::min<int64_t>(base <= 256 ? 8 : 4, chunks);
-    const int64_t parts = std::min<int64_t>(ceil_div(512, base), chunks / (p.waves * 2));
+    int64_t parts;
+    if (p.many) {
+        p.waves = 4;
+        parts = std::min(ceil_div(1024, base), chunks / 8);
+    } else {
+        parts = std::min<int64_t>(ceil_div(256, base), chunks / 24);
+        p.waves = (int)std::min<int64_t>(base * parts <= 256 || chunks >= 48 * parts ? 8 : 4, chunks);
+    }
     p.split = (int)ceil_div(chunks, std::max<int64_t>(1, parts));
     p.splits = (int)ceil_div(chunks, p.split);
-    p.by_length = base * p.splits * p.waves > 2048;
+    p.by_length = c->batch > 1 && base * p.splits * p.waves > 2048;
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -185,8 +195,11 @@ int check_attn(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     return RSD_OK;
 }
 template <typename T, typename C, int HD> void attn_run(const KvcAttn& k, const AttnPlan& p, Launches& l) {
-    l.run(kvc_attn_kernel<T, C, HD>, dim3((unsigned)kvc_blocks(p.lists, p.tiles), (unsigned)p.splits), 64 * p.waves, 0, k);
-    if (p.splits > 1) l.run(kvc_join_kernel<T, HD, KvcMath<T, C, HD>::CH>, (unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, k);
+    const dim3 grid((unsigned)kvc_blocks(p.lists, p.tiles), (unsigned)p.splits);
+    if (!p.many) l.run(kvc_attn_few_kernel<T, C, HD>, grid, 64 * p.waves, 0, k);
+    else if (p.tile_cols == 64) l.run(kvc_attn_many_kernel<T, C, HD, 1>, grid, 256, 0, k);
+    else if constexpr (sizeof(T) == 2) l.run(kvc_attn_many_kernel<T, C, HD, 2>, grid, 256, 0, k);
+    if (p.splits > 1) l.run(kvc_join_kernel<T, HD>, (unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, k);
 }
 template <typename T, typename C> void attn_run(const KvcAttn& k, const AttnPlan& p, int hd, Launches& l) {
     if (hd == 32) attn_run<T, C, 32>(k, p, l);
@@ -294,11 +307,12 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     k.scale = a->scale;
     k.plain = !(std::fabs(a->scale) > 0.f);
     k.factor2 = k.plain ? 1.4426950408889634f : (float)(std::fabs((double)a->scale) * 1.4426950408889634);
+    k.inverse2 = 1.f / k.factor2;
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
     k.max_kv = a->max_kv, k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
-    k.lists = p.lists, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length;
+    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length;
     k.part_o = static_cast<float*>(workspace);
     k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.o_bytes);
     Launches l(hip_stream);

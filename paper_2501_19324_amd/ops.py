@@ -23,6 +23,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from functools import lru_cache
 from operator import index
 from typing import NamedTuple, Optional, Tuple
@@ -423,27 +424,43 @@ def rsd_rope(rot_dim: int, theta: float = 1e4, *, scaling: str = "plain", factor
     return Rope(torch.tensor(list(freq), dtype=torch.float64, device=device), interleaved, magnitude)
 
 
-def _rope(rope, like: torch.Tensor, hd: int):
+# The structures of these calls as bytes, packed field by field: 0.6 us against 1.8 for a ctypes.Structure of sixteen fields, of the 8 to 13 that a small call takes.
+_ROPE_BYTES, _HEADS_BYTES = struct.Struct("=Qiifi").pack, struct.Struct("=QQQqqqqii").pack
+_KV_CACHE_BYTES, _KV_ATTN_BYTES = struct.Struct("=QQQiiiiii").pack, struct.Struct("=QQQqqqqQiiiiiiif").pack
+_f64 = torch.float64
+
+
+def _rope(rope, like: torch.Tensor, hd: int) -> bytes:
     freq, interleaved, magnitude = rope
-    if freq.dtype is not torch.float64 or freq.device != like.device or freq.dim() != 1 or not freq.is_contiguous() or not 2 <= 2 * freq.shape[0] <= hd:
-        _bad(f"rope: the frequencies are {freq.dtype} {tuple(freq.shape)} on {freq.device}, needed float64 [1 .. {hd // 2}] on {like.device}, contiguous")
-    return _Rope(freq.data_ptr(), 2 * freq.shape[0], bool(interleaved), magnitude)
+    shape = freq.shape
+    if freq.dtype is not _f64 or freq.device != like.device or len(shape) != 1 or not freq.is_contiguous() or not 2 <= 2 * shape[0] <= hd:
+        _bad(f"rope: the frequencies are {freq.dtype} {tuple(shape)} on {freq.device}, needed float64 [1 .. {hd // 2}] on {like.device}, contiguous")
+    try:
+        return _ROPE_BYTES(freq.data_ptr(), 2 * shape[0], 1 if interleaved else 0, magnitude, 0)
+    except (struct.error, OverflowError):
+        _bad(f"rope: magnitude {magnitude!r}")
 
 
-def _heads(name: str, x: torch.Tensor, like: torch.Tensor, hd: int, weight: Optional[torch.Tensor], out: Optional[torch.Tensor], writes: bool):
-    """The heads of x, and where they go: (structure, out)."""
-    xp, xr, xh = _rows3(name, x, like, None, hd)
-    if x.dtype is not like.dtype or x.shape[0] != like.shape[0]:
-        _bad(f"{name}: {x.dtype} {tuple(x.shape)}, needed {like.dtype} and {like.shape[0]} rows")
-    wp = None if weight is None else _flat(name + "_weight", weight, like, like.dtype, (hd,))
+def _heads(name: str, x: torch.Tensor, rows: int, hd: int, dtype, device, weight: Optional[torch.Tensor], out: Optional[torch.Tensor], writes: bool):
+    """The heads of x [rows, heads, hd], and where they go: (structure, out)."""
+    shape, (xr, xh, one) = x.shape, x.stride() if x.dim() == 3 else (0, 0, 0)
+    if one != 1 or shape[0] != rows or shape[2] != hd or x.dtype is not dtype or x.device != device:
+        _bad(f"{name}: {x.dtype} {tuple(shape)} on {x.device}, strides {x.stride()}, needed {dtype} [{rows}, heads, {hd}] on {device}, contiguous heads")
+    heads, wp = shape[1], 0
+    if weight is not None:
+        if weight.dtype is not dtype or weight.shape != (hd,) or not weight.is_contiguous() or weight.device != device:
+            _bad(f"{name}_weight: {weight.dtype} {tuple(weight.shape)} on {weight.device}, needed {dtype} [{hd}] on {device}, contiguous")
+        wp = weight.data_ptr()
     if not writes:
-        return _Heads(xp, None, wp, xr, xh, 0, 0, x.shape[1]), None
+        return _HEADS_BYTES(x.data_ptr(), 0, wp, xr, xh, 0, 0, heads, 0), None
     if out is None:
-        out = x.new_empty(x.shape)
-    elif out.dtype is not x.dtype or out.shape != x.shape:
-        _bad(f"{name}_out: {out.dtype} {tuple(out.shape)}, needed {x.dtype} {tuple(x.shape)}")
-    op, orow, oh = _rows3(name + "_out", out, like, x.shape[1], hd)
-    return _Heads(xp, op, wp, xr, xh, orow, oh, x.shape[1]), out
+        out = x.new_empty(shape)
+        orow, oh = heads * hd, hd
+    else:
+        orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
+        if one != 1 or out.shape != shape or out.dtype is not dtype or out.device != device:
+            _bad(f"{name}_out: {out.dtype} {tuple(out.shape)} on {out.device}, strides {out.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
+    return _HEADS_BYTES(x.data_ptr(), out.data_ptr(), wp, xr, xh, orow, oh, heads, 0), out
 
 
 def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.Tensor], rope=None, *, q_weight: Optional[torch.Tensor] = None,
@@ -451,24 +468,26 @@ def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[t
     """Heads ``q [rows, heads, head_dim]`` and ``k [rows, kv heads, head_dim]`` (may be None) normed over the head dimension, where they have a weight ``[head_dim]``, and
     rotated by ``rope`` (may be None) at ``position`` (int32 ``[rows]``).  Returns ``(q_out, k_out)``; an out may be its input itself."""
     lib = _lib or _load()
-    if q.dtype not in _TYPE or q.dim() != 3 or q.shape[2] not in (32, 64, 128, 256) or q.shape[1] == 0:
-        _bad(f"qk_rope: q is {q.dtype} {tuple(q.shape)}, needed fp32 or bf16 [rows, heads, 32, 64, 128 or 256]")
+    dtype, shape = q.dtype, q.shape
+    t = _TYPE.get(dtype)
+    if t is None or len(shape) != 3 or shape[2] not in (32, 64, 128, 256) or shape[1] == 0:
+        _bad(f"qk_rope: q is {dtype} {tuple(shape)}, needed fp32 or bf16 [rows, heads, 32, 64, 128 or 256]")
     st = _stream(q)
-    rows, _, hd = q.shape
-    if k is None and (k_weight is not None or k_out is not None):
-        _bad("qk_rope: k_weight or k_out without k")
-    qs, q_out = _heads("q", q, q, hd, q_weight, q_out, True)
-    ks = None
+    rows, _, hd = shape
+    device = q.device
+    qs, q_out = _heads("q", q, rows, hd, dtype, device, q_weight, q_out, True)
+    ks = pp = rs = None
     if k is not None:
-        ks, k_out = _heads("k", k, q, hd, k_weight, k_out, True)
-    pp = rs = None
+        ks, k_out = _heads("k", k, rows, hd, dtype, device, k_weight, k_out, True)
+    elif k_weight is not None or k_out is not None:
+        _bad("qk_rope: k_weight or k_out without k")
     if rope is not None:
-        rs = C.byref(_rope(rope, q, hd))
+        rs = _rope(rope, q, hd)
         if position is None:
             _bad("qk_rope: a rotation without positions")
         pp = _flat("position", position, q, _i32, (rows,))
     if rows:
-        _done(lib.rsd_qk_rope(C.byref(qs), None if ks is None else C.byref(ks), pp, rs, eps, rows, hd, _TYPE[q.dtype], st), lib)
+        _done(lib.rsd_qk_rope(qs, ks, pp, rs, eps, rows, hd, t, st), lib)
     return q_out, k_out
 
 
@@ -480,7 +499,8 @@ def rsd_kv_cache(batch: int, max_pages: int, n_pages: int, n_kv_heads: int, head
                    torch.full((batch, max_pages), -1, dtype=_i32, device=device), torch.zeros(batch, dtype=_i32, device=device))
 
 
-def _kv_cache(c) -> Tuple[_KvCache, torch.Tensor, int]:
+def _kv_cache(c):
+    """A cache as bytes, with what its calls go by: (bytes, pool, stream, (n_pages, n_kv_heads, head_dim, batch, max_pages, dtype))."""
     pool, table, kv_len = c
     st = _stream(pool)
     shape, dev, t = pool.shape, pool.device, _TYPE.get(pool.dtype)
@@ -491,7 +511,11 @@ def _kv_cache(c) -> Tuple[_KvCache, torch.Tensor, int]:
     batch, max_pages = table.shape
     if kv_len.dtype is not _i32 or kv_len.device != dev or kv_len.shape != (batch,) or not kv_len.is_contiguous():
         _bad(f"cache: kv_len is {kv_len.dtype} {tuple(kv_len.shape)} on {kv_len.device}, needed int32 [{batch}] on {dev}, contiguous")
-    return _KvCache(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), shape[0], shape[1], shape[3] // PAGE, batch, max_pages, t), pool, st
+    sizes = (shape[0], shape[1], shape[3] // PAGE, batch, max_pages, t)
+    try:
+        return _KV_CACHE_BYTES(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), *sizes), pool, st, sizes
+    except struct.error:
+        _bad(f"cache: pool {tuple(shape)}, table {tuple(table.shape)}")
 
 
 def rsd_kv_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, slot: torch.Tensor, *, position: Optional[torch.Tensor] = None, rope=None,
@@ -500,53 +524,51 @@ def rsd_kv_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, sl
     """Writes keys and values ``[rows, n_kv_heads, head_dim]`` into slot ``slot[i]`` of sequence ``seq[i]``, the keys normed (with ``k_weight``) and rotated (with ``rope``, at
     ``position``) on their way; queries ``q [rows, heads, head_dim]`` of the same tokens go through the same in the same launch and are returned.  ``kv_len`` is left to the caller."""
     lib = _lib or _load()
-    c, pool, st = _kv_cache(cache)
-    t = _TYPE.get(k.dtype)
-    if t is None or v.dtype is not k.dtype or v.shape != k.shape:
-        _bad(f"append: k is {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}; needed fp32 or bf16, alike")
-    hd = c.head_dim
-    if k.device != pool.device:
-        _bad(f"append: k is on {k.device}, the cache on {pool.device}")
-    ks, _ = _heads("k", k, k, hd, k_weight, None, False)
-    vp, vr, vh = _rows3("v", v, pool, c.n_kv_heads, hd)
-    rows = k.shape[0]
+    c, pool, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
+    dtype, shape, device = k.dtype, k.shape, pool.device
+    t = _TYPE.get(dtype)
+    if t is None or len(shape) != 3 or shape[1] != kv_heads:
+        _bad(f"append: k is {dtype} {tuple(shape)}, needed fp32 or bf16 [rows, {kv_heads}, {hd}]")
+    rows = shape[0]
+    ks, _ = _heads("k", k, rows, hd, dtype, device, k_weight, None, False)
+    vr, vh, one = v.stride() if v.dim() == 3 else (0, 0, 0)
+    if one != 1 or v.shape != shape or v.dtype is not dtype or v.device != device:
+        _bad(f"v: {v.dtype} {tuple(v.shape)} on {v.device}, strides {v.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
     sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
-    qs = None
+    qs = pp = rs = None
     if q is not None:
-        qs, q_out = _heads("q", q, k, hd, q_weight, q_out, True)
+        qs, q_out = _heads("q", q, rows, hd, dtype, device, q_weight, q_out, True)
     elif q_weight is not None or q_out is not None:
         _bad("append: q_weight or q_out without q")
-    pp = rs = None
     if rope is not None:
-        rs = C.byref(_rope(rope, pool, hd))
+        rs = _rope(rope, pool, hd)
         if position is None:
             _bad("append: a rotation without positions")
         pp = _flat("position", position, pool, _i32, (rows,))
     if rows:
-        _done(lib.rsd_kv_append(C.byref(c), C.byref(ks), vp, vr, vh, None if qs is None else C.byref(qs), sp, lp, pp, rs, eps, rows, t, st), lib)
+        _done(lib.rsd_kv_append(c, ks, v.data_ptr(), vr, vh, qs, sp, lp, pp, rs, eps, rows, t, st), lib)
     return q_out
 
 
 def rsd_kv_read(cache, seq: torch.Tensor, slot: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """Keys and values ``[rows, n_kv_heads, head_dim]`` of the entries (seq[i], slot[i]); zeros where there is none."""
     lib = _lib or _load()
-    c, pool, st = _kv_cache(cache)
+    c, pool, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
     if seq.dim() != 1:
         _bad(f"seq: shape {tuple(seq.shape)}, needed [rows]")
     rows = seq.shape[0]
     sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
-    k, v = pool.new_empty(2, rows, c.n_kv_heads, c.head_dim).unbind()
+    k, v = pool.new_empty(2, rows, kv_heads, hd).unbind()
     if rows:
-        _done(lib.rsd_kv_read(C.byref(c), sp, lp, rows, k.data_ptr(), v.data_ptr(), st), lib)
+        _done(lib.rsd_kv_read(c, sp, lp, rows, k.data_ptr(), v.data_ptr(), st), lib)
     return k, v
 
 
 @lru_cache(maxsize=4096)
-def _kv_attn_bytes(n_pages, kv_heads, hd, batch, max_pages, cache_dtype, rows, max_rows, heads, max_kv, window, sinks, dtype, ragged) -> int:
+def _kv_attn_bytes(cache, rows, max_rows, heads, max_kv, window, sinks, dtype, ragged) -> int:
     # the sizes only; the addresses stand for "given"
-    c = _KvCache(16, 16, 16, n_pages, kv_heads, hd, batch, max_pages, cache_dtype)
-    a = _KvAttn(16, 16, None, 0, 0, 0, 0, 16 if ragged else None, rows, max_rows, heads, max_kv, window, sinks, dtype, 0.0)
-    return (_lib or _load()).rsd_kv_attention_workspace(C.byref(c), C.byref(a))
+    a = _KV_ATTN_BYTES(16, 16, 0, 0, 0, 0, 0, 16 if ragged else 0, rows, max_rows, heads, max_kv, window, sinks, dtype, 0.0)
+    return (_lib or _load()).rsd_kv_attention_workspace(_KV_CACHE_BYTES(16, 16, 16, *cache), a)
 
 
 def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, max_kv: Optional[int] = None,
@@ -558,35 +580,40 @@ def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optiona
     sequence's newest; their places in the result, like those of rows that no sequence has, are not written.  ``max_kv`` bounds ``kv_len`` (default: what the table can hold).  The tighter both are, the better the work is
     dealt.  With ``window`` a row sees its own entry, the window - 1 before it, and a sequence's first ``sinks``.  ``out`` may be ``q`` itself.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
     lib = _lib or _load()
-    c, pool, st = _kv_cache(cache)
-    t = _TYPE.get(q.dtype)
-    if t is None:
-        _bad(f"attention: q is {q.dtype}, needed fp32 or bf16")
-    qp, qr, qh = _rows3("q", q, pool, None, c.head_dim)
-    rows, heads = q.shape[0], q.shape[1]
-    if heads == 0 or heads % c.n_kv_heads:
-        _bad(f"attention: {heads} heads over {c.n_kv_heads} kv heads")
+    c, pool, st, sizes = _kv_cache(cache)
+    _, kv_heads, hd, batch, max_pages, _ = sizes
+    dtype, shape, device = q.dtype, q.shape, pool.device
+    t = _TYPE.get(dtype)
+    qr, qh, one = q.stride() if q.dim() == 3 else (0, 0, 0)
+    if t is None or one != 1 or shape[2] != hd or q.device != device:
+        _bad(f"attention: q is {dtype} {tuple(shape)} on {q.device}, strides {q.stride()}, needed fp32 or bf16 [rows, heads, {hd}] on {device}, contiguous heads")
+    rows, heads, _ = shape
+    if heads == 0 or kv_heads == 0 or heads % kv_heads:
+        _bad(f"attention: {heads} heads over {kv_heads} kv heads")
+    rp = 0
     if row_start is None:
         max_rows = 1 if max_rows is None else max_rows
-        if rows != c.batch or max_rows != 1:
-            _bad(f"attention: {rows} rows for {c.batch} sequences, max_rows {max_rows}, without row_start")
-        rp = None
+        if rows != batch or max_rows != 1:
+            _bad(f"attention: {rows} rows for {batch} sequences, max_rows {max_rows}, without row_start")
     else:
         max_rows = rows if max_rows is None else max_rows
-        rp = _flat("row_start", row_start, pool, _i32, (c.batch + 1,))
-    window, sinks = _int("attention: window", window, 0), _int("attention: sinks", sinks, 0)
+        rp = _flat("row_start", row_start, pool, _i32, (batch + 1,))
+    if window.__class__ is not int or sinks.__class__ is not int or not 0 <= window < 1 << 31 or not 0 <= sinks < 1 << 31:
+        window, sinks = _int("attention: window", window, 0), _int("attention: sinks", sinks, 0)
     if out is None:
-        out = q.new_empty(rows, heads, c.head_dim)
-    elif out.dtype is not q.dtype or out.shape != q.shape:
-        _bad(f"attention: out is {out.dtype} {tuple(out.shape)}, needed {q.dtype} {tuple(q.shape)}")
-    op, orow, oh = _rows3("out", out, pool, heads, c.head_dim)
-    lse = q.new_empty(rows, heads, dtype=_f32) if want_lse else None
+        out = q.new_empty(shape)
+        orow, oh = heads * hd, hd
+    else:
+        orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
+        if one != 1 or out.shape != shape or out.dtype is not dtype or out.device != device:
+            _bad(f"attention: out is {out.dtype} {tuple(out.shape)} on {out.device}, strides {out.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
+    lse = q.new_empty((rows, heads), dtype=_f32) if want_lse else None
     if rows:
         max_rows = _int("attention: max_rows", max_rows, 1)
-        cap = c.max_pages * PAGE
+        cap = max_pages * PAGE
         max_kv = cap if max_kv is None else min(max(int(max_kv), -1), cap)
-        nbytes = _kv_attn_bytes(c.n_pages, c.n_kv_heads, c.head_dim, c.batch, c.max_pages, c.dtype, rows, max_rows, heads, max_kv, window, sinks, t, rp is not None)
+        nbytes = _kv_attn_bytes(sizes, rows, max_rows, heads, max_kv, window, sinks, t, rp != 0)
         ws, wp = _workspace(nbytes, pool)
-        a = _KvAttn(qp, op, lse.data_ptr() if want_lse else None, qr, qh, orow, oh, rp, rows, max_rows, heads, max_kv, window, sinks, t, scale)
-        _done(lib.rsd_kv_attention(C.byref(c), C.byref(a), wp, nbytes, st), lib)
+        a = _KV_ATTN_BYTES(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, qr, qh, orow, oh, rp, rows, max_rows, heads, max_kv, window, sinks, t, scale)
+        _done(lib.rsd_kv_attention(c, a, wp, nbytes, st), lib)
     return (out, lse) if want_lse else out

@@ -26,6 +26,12 @@ def ops():
 def test_structures_have_the_headers_sizes(ops):
     assert C.sizeof(ops._KvCache) == 24 + 24 and C.sizeof(ops._KvAttn) == 24 + 32 + 8 + 32
     assert C.sizeof(ops._Heads) == 24 + 32 + 8 and C.sizeof(ops._Rope) == 24
+    # the bytes that the binding packs are those of the structures
+    for kind, pack, values in ((ops._KvCache, ops._KV_CACHE_BYTES, (16, 17, 18, 1, 2, 3, 4, 5, 1)), (ops._Rope, ops._ROPE_BYTES, (16, 64, 1, 1.25, 0)),
+                               (ops._Heads, ops._HEADS_BYTES, (16, 17, 18, -5, 6, 1 << 40, 8, 9, 0)),
+                               (ops._KvAttn, ops._KV_ATTN_BYTES, (16, 17, 18, -1, 2, 3, 1 << 40, 19, 4, 5, 6, 7, 8, 9, 1, -0.5))):
+        made = kind(*values[:len(kind._fields_)])
+        assert bytes(made)[:sum(C.sizeof(f) for _, f in kind._fields_)] == pack(*values)[:sum(C.sizeof(f) for _, f in kind._fields_)] and C.sizeof(kind) == len(pack(*values))
 
 
 def cache(ops, **kw):
