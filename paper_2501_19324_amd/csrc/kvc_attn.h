@@ -25,6 +25,7 @@ struct KvcAttn {
     int lists, tiles, tile_cols;    // (sequence, kv head) pairs, tiles of columns of each
     int split, splits;      // chunks to a part, most parts
     bool by_length;         // the blocks of the longest sequences go first
+    bool turns;             // blocks are dealt forwards and backwards in turn
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
 };
@@ -89,11 +90,19 @@ __device__ __forceinline__ int kvc_by_length(const KvcAttn& a, int i) {
     return first + __builtin_ctzll(__ballot(before == (i & 63)));
 }
 
-// The work of block `id`: a list, that is a (sequence, kv head), and a tile of its columns; the last tile first, which sees most.  Blocks go to the eight XCDs in turn: the
-// tiles of a list, which read the same entries, are neighbours on one XCD and its L2.  Fewer than eight lists that divide eight share them out evenly.
-__host__ __device__ __forceinline__ int kvc_blocks(int lists, int tiles) { return lists < 8 && 8 % lists == 0 ? (tiles + 8 / lists - 1) / (8 / lists) * 8 : (lists + 7) / 8 * 8 * tiles; }
-__device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, int& tile) {
-    const int xcd = id & 7, at = id >> 3;
+// The work of block `id`: a list, that is a (sequence, kv head), a tile of its columns, and a part of their chunks; the last tile first, which sees most.  Blocks go to the eight XCDs in
+// turn: the tiles of a list, which read the same entries, are neighbours on one XCD and its L2.  Fewer than eight lists that divide eight share the XCDs out evenly.
+// An XCD deals its blocks to 32 CUs in turn; where all run at once (`turns`) every second round goes backwards, so that a CU whose first block is among the longest does not get the longest of every round
+// (16 sequences x 16 heads of 17 .. 128 rows and 300 .. 1025 entries, fp32: the second tile of most is empty, and the CUs that got first tiles in every round were busy twice as long).
+__host__ __device__ __forceinline__ int kvc_blocks(int lists, int tiles, int splits) {
+    return (lists < 8 && 8 % lists == 0 ? (tiles + 8 / lists - 1) / (8 / lists) * 8 : (lists + 7) / 8 * 8 * tiles) * splits;
+}
+__device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, int& tile, int& part) {
+    const int xcd = id & 7, all = gridDim.x >> 3;
+    int at = id >> 3;
+    if (a.turns && (at & 32) && (at | 31) < all) at ^= 31;
+    part = at / (all / a.splits);
+    at -= part * (all / a.splits);
     if (a.lists < 8 && 8 % a.lists == 0) {
         list = xcd % a.lists;
         tile = at * (8 / a.lists) + xcd / a.lists;
@@ -395,8 +404,8 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     __shared__ __align__(16) float lds_o[WAVES][NB][64][4];
     __shared__ float lds_ml[WAVES][2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, quad = lane >> 4;
-    int list, tile;
-    if (!kvc_work(a, blockIdx.x, list, tile)) return;
+    int list, tile, part;
+    if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
     const int b = kvc_by_length(a, list / a.c.hkv), head = list % a.c.hkv, col0 = tile * 16, col = col0 + (lane & 15);
     int r0, count, n;
     kvc_rows(a, b, r0, count, n);
@@ -404,15 +413,15 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, M::CH, count, n, col0, min(cols, col0 + 16));
     const int parts = kvc_parts(a, span);
-    if ((int)blockIdx.y >= parts) return;
-    const int end = min((int)(blockIdx.y + 1) * a.split, span.chunks);
+    if (part >= parts) return;
+    const int end = min((part + 1) * a.split, span.chunks);
 
     typename M::Entries k, v;
     typename M::Q q[1];
     const KvcColumn see[1] = {kvc_column(a, count, n, col, cols)};
     f32x4_t o[1][NB] = {};
     KvcRun run;
-    int i = blockIdx.y * a.split + wave;
+    int i = part * a.split + wave;
     // (past the end the wave's last chunk is requested again)
     auto table = [&](int i, const C* pg[M::PAGES], int& there_) { kvc_pages<C, HD, M::PAGES>(a.c, b, head, kvc_slot<M::CH>(span, i < end ? i : end - 1 - (end - 1 - wave + waves * 4096) % waves), pg, there_); };
     auto load = [&](const C* const pg[M::PAGES], int offset, typename M::Entries& e) {
@@ -466,7 +475,7 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
-        if (col < cols) kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, blockIdx.y, parts);
+        if (col < cols) kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, part, parts);
     }
 }
 
@@ -500,8 +509,8 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     static_assert(2 * N % OWN == 0, "a wave's share lies in one page");
     __shared__ u32x4_t ring[R][PAGES][2 * N][64];           // keys, then values of each page
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
-    int list, tile;
-    if (!kvc_work(a, blockIdx.x, list, tile)) return;
+    int list, tile, part;
+    if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
     const int b = kvc_by_length(a, list / a.c.hkv), head = list % a.c.hkv, col0 = tile * COLS;
     int r0, count, n;
     kvc_rows(a, b, r0, count, n);
@@ -509,8 +518,8 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, CH, count, n, col0, min(cols, col0 + COLS));
     const int parts = kvc_parts(a, span);
-    if ((int)blockIdx.y >= parts) return;
-    const int begin = blockIdx.y * a.split, end = min(begin + a.split, span.chunks);
+    if (part >= parts) return;
+    const int begin = part * a.split, end = min(begin + a.split, span.chunks);
     // this wave's columns, what they see, and the steps that all of them see whole (but for missing pages)
     const int colw = col0 + wave * 16 * NT;
     const bool mine = colw < cols;
@@ -615,7 +624,7 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
         if (col < cols)
 #pragma unroll
             for (int d = 0; d < NB; ++d)
-                kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[t][d], run[t].top, total, blockIdx.y, parts);
+                kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[t][d], run[t].top, total, part, parts);
     }
 }
 

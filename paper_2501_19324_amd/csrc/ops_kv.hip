@@ -114,16 +114,16 @@ int check_rows(const RowArgs& a, bool cached, const char* what) {
 }
 KvcHeads dev_heads(const rsd_heads* h) { return h ? KvcHeads{h->x, h->out, h->weight, h->row, h->head, h->out_row, h->out_head, h->n_heads} : KvcHeads{}; }
 KvcRows dev_rows(const RowArgs& a, const KvcCache& c) {
-    KvcRows r{dev_heads(a.q), dev_heads(a.k), a.v, a.v_row, a.v_head, a.position, a.seq, a.slot, nullptr, 0, 1.f, a.eps, a.rows, c};
+    KvcRows r{dev_heads(a.q), dev_heads(a.k), a.v, a.v_row, a.v_head, a.position, a.seq, a.slot, nullptr, 0, 1.f, a.eps, a.rows, 0, c};
     if (a.rope) r.freq = a.rope->freq, r.rot_dim = a.rope->rot_dim, r.magnitude = a.rope->magnitude;
     return r;
 }
-template <typename T, typename C, int HD, bool CACHE> void rows_run(const RowArgs& a, const KvcRows& r, Launches& l) {
-    const int64_t items = (int64_t)a.rows * (r.q.n + r.k.n * (CACHE ? 2 : 1));
-    const unsigned grid = (unsigned)ceil_div(items, 256 / (HD / 16));
-    if (a.rope && a.rope->interleaved) l.run(kvc_rows_kernel<T, C, HD, true, true, CACHE>, grid, 256, 0, r);
-    else if (r.rot_dim % 16 == 0) l.run(kvc_rows_kernel<T, C, HD, false, true, CACHE>, grid, 256, 0, r);
-    else l.run(kvc_rows_kernel<T, C, HD, false, false, CACHE>, grid, 256, 0, r);
+template <typename T, typename C, int HD, bool CACHE> void rows_run(const RowArgs& a, KvcRows r, Launches& l) {
+    r.value_blocks = CACHE ? (int)(ceil_div(a.rows, KvcValueBlock<C, HD>::ROWS) * ceil_div(r.k.n, KvcValueBlock<C, HD>::HEADS)) : 0;
+    const unsigned grid = (unsigned)(r.value_blocks + ceil_div((int64_t)a.rows * (r.q.n + r.k.n), 256 / (HD / 16)));
+    if (a.rope && a.rope->interleaved) l.run(kvc_rows_kernel<T, C, HD, true, false, CACHE>, grid, 256, 0, r);
+    else if (r.rot_dim % 16 == 0) l.run(kvc_rows_kernel<T, C, HD, false, false, CACHE>, grid, 256, 0, r);
+    else l.run(kvc_rows_kernel<T, C, HD, false, true, CACHE>, grid, 256, 0, r);
 }
 template <typename T> void rope_run(const RowArgs& a, const KvcRows& r, Launches& l) {
     if (a.head_dim == 32) rows_run<T, T, 32, false>(a, r, l);
@@ -141,7 +141,7 @@ template <typename T, typename C> void append_run(const RowArgs& a, const KvcRow
 
 struct AttnPlan {
     int lists, tiles, tile_cols, ch, waves, split, splits;
-    bool many, by_length;
+    bool many, by_length, turns;
     uint64_t o_bytes, ml_bytes;
     uint64_t bytes() const { return o_bytes + ml_bytes; }
 };
@@ -177,6 +177,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     p.split = (int)ceil_div(chunks, std::max<int64_t>(1, parts));
     p.splits = (int)ceil_div(chunks, p.split);
     p.by_length = c->batch > 1 && base * p.splits * p.waves > 2048;
+    p.turns = p.many && base * p.splits * p.waves <= (c->head_dim == 128 ? 2048 : 4096);
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -195,7 +196,7 @@ int check_attn(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     return RSD_OK;
 }
 template <typename T, typename C, int HD> void attn_run(const KvcAttn& k, const AttnPlan& p, Launches& l) {
-    const dim3 grid((unsigned)kvc_blocks(p.lists, p.tiles), (unsigned)p.splits);
+    const unsigned grid = (unsigned)kvc_blocks(p.lists, p.tiles, p.splits);
     if (!p.many) l.run(kvc_attn_few_kernel<T, C, HD>, grid, 64 * p.waves, 0, k);
     else if (p.tile_cols == 64) l.run(kvc_attn_many_kernel<T, C, HD, 1>, grid, 256, 0, k);
     else if constexpr (sizeof(T) == 2) l.run(kvc_attn_many_kernel<T, C, HD, 2>, grid, 256, 0, k);
@@ -312,7 +313,7 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
     k.max_kv = a->max_kv, k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
-    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length;
+    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.turns = p.turns;
     k.part_o = static_cast<float*>(workspace);
     k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.o_bytes);
     Launches l(hip_stream);

@@ -428,6 +428,7 @@ def rsd_rope(rot_dim: int, theta: float = 1e4, *, scaling: str = "plain", factor
 _ROPE_BYTES, _HEADS_BYTES = struct.Struct("=Qiifi").pack, struct.Struct("=QQQqqqqii").pack
 _KV_CACHE_BYTES, _KV_ATTN_BYTES = struct.Struct("=QQQiiiiii").pack, struct.Struct("=QQQqqqqQiiiiiiif").pack
 _f64 = torch.float64
+_empty_like, _contiguous = torch.empty_like, torch.contiguous_format
 
 
 def _rope(rope, like: torch.Tensor, hd: int) -> bytes:
@@ -454,7 +455,7 @@ def _heads(name: str, x: torch.Tensor, rows: int, hd: int, dtype, device, weight
     if not writes:
         return _HEADS_BYTES(x.data_ptr(), 0, wp, xr, xh, 0, 0, heads, 0), None
     if out is None:
-        out = x.new_empty(shape)
+        out = _empty_like(x, memory_format=_contiguous)
         orow, oh = heads * hd, hd
     else:
         orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
@@ -601,7 +602,7 @@ def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optiona
     if window.__class__ is not int or sinks.__class__ is not int or not 0 <= window < 1 << 31 or not 0 <= sinks < 1 << 31:
         window, sinks = _int("attention: window", window, 0), _int("attention: sinks", sinks, 0)
     if out is None:
-        out = q.new_empty(shape)
+        out = _empty_like(q, memory_format=_contiguous)
         orow, oh = heads * hd, hd
     else:
         orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
