@@ -6,12 +6,22 @@
 #pragma once
 #include "kvc.h"
 
+// Division of 0 <= n < 2^30 by a number that the host knows: inverse = 2^32 / d + 1 gives at most one too much; for d = 1 it is 2^32 - 1, one too little
+struct KvcDivisor {
+    uint32_t d, inverse;
+    __device__ __forceinline__ int operator()(int n) const {
+        const int q = (int)__umulhi((uint32_t)n, inverse);
+        const int rest = n - q * (int)d;
+        return q + (rest >= (int)d) - (rest < 0);
+    }
+};
 struct KvcAttn {
     KvcCache c;
     const void* q;
     int64_t q_row, q_head;
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
-    int total_rows, max_rows, heads, group;
+    int total_rows, max_rows, heads;
+    KvcDivisor group, by_heads, by_tiles;    // heads of a kv head; by the kv heads and by the tiles
     float factor2;          // |scale| * log2(e); never 0 or NaN
     float inverse2;         // 1 / factor2
     bool negative;          // scale < 0: q changes its sign instead
@@ -48,7 +58,7 @@ struct KvcSpan {
 };
 __device__ __forceinline__ KvcSpan kvc_span(const KvcAttn& a, int CH, int count, int n, int col0, int col1) {
     KvcSpan s;
-    const int p0 = n - count + col0 / a.group, p1 = n - count + (col1 - 1) / a.group;      // slots of the first and the last row
+    const int p0 = n - count + a.group(col0), p1 = n - count + a.group(col1 - 1);      // slots of the first and the last row
     s.end = max(p1 + 1, 0);
     s.safe = max(p0 + 1, 0);
     s.near = a.window ? max(p0 - a.window + 1, 0) : 0;
@@ -73,21 +83,27 @@ struct KvcColumn {
     __device__ __forceinline__ bool sees(int slot) const { return (slot < high) & ((slot >= low) | (slot < sinks)); }
 };
 __device__ __forceinline__ KvcColumn kvc_column(const KvcAttn& a, int count, int n, int col, int cols) {
-    const int p = n - count + col / a.group;
+    const int p = n - count + a.group(col);
     return KvcColumn{a.window ? p - a.window + 1 : 0, col < cols ? p + 1 : 0, a.sinks};
 }
 
 // Sequences of unlike lengths make blocks of unlike times: the longest go first where the blocks do not all run at once.  The i-th sequence in that order, among
-// every 64 together; the same for all lanes of a whole wave.
+// every 64 together, by the first eight bits of their lengths (of max_kv's): bit by bit, those that have it go before those that do not.  The same for all lanes of a whole wave.
 __device__ __forceinline__ int kvc_by_length(const KvcAttn& a, int i) {
     if (!a.by_length) return i;
     const int lane = threadIdx.x & 63, first = i & ~63;
-    const int len = first + lane < a.c.batch ? min(max(a.c.kv_len[first + lane], 0), 1 << 24) : -1;
-    const int key = len * 64 + 63 - lane;                   // no two alike
-    int before = 0;
-#pragma unroll 8
-    for (int u = 0; u < 64; ++u) before += __builtin_amdgcn_readlane(key, u) > key;
-    return first + __builtin_ctzll(__ballot(before == (i & 63)));
+    const int key = first + lane < a.c.batch ? min(max(a.c.kv_len[first + lane], 0), a.max_kv) >> max(24 - __clz(a.max_kv), 0) : -1;
+    uint64_t among = __ballot(key >= 0);
+    int rank = i & 63;
+#pragma unroll
+    for (int bit = 7; bit >= 0; --bit) {
+        const uint64_t have = __ballot((key >> bit) & 1) & among;
+        const int n = __popcll(have);
+        among = rank < n ? have : among & ~have;
+        rank -= rank < n ? 0 : n;
+    }
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(among >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)among, 0));
+    return first + __builtin_ctzll(__ballot(((among >> lane) & 1) && before == rank));
 }
 
 // The work of block `id`: a list, that is a (sequence, kv head), a tile of its columns, and a part of their chunks; the last tile first, which sees most.  Blocks go to the eight XCDs in
@@ -101,14 +117,18 @@ __device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, in
     const int xcd = id & 7, all = gridDim.x >> 3;
     int at = id >> 3;
     if (a.turns && (at & 32) && (at | 31) < all) at ^= 31;
-    part = at / (all / a.splits);
-    at -= part * (all / a.splits);
+    part = 0;
+    if (a.splits > 1) {
+        part = at / (all / a.splits);
+        at -= part * (all / a.splits);
+    }
     if (a.lists < 8 && 8 % a.lists == 0) {
         list = xcd % a.lists;
         tile = at * (8 / a.lists) + xcd / a.lists;
     } else {
-        list = at / a.tiles * 8 + xcd;
-        tile = at % a.tiles;
+        const int eight = a.by_tiles(at);
+        list = eight * 8 + xcd;
+        tile = at - eight * a.tiles;
     }
     tile = a.tiles - 1 - tile;
     return list < a.lists && tile >= 0;
@@ -138,8 +158,18 @@ template <typename T, typename C, int HD> struct KvcMath {
 
     // operands of a tile of 16 columns: column lane % 16, dims 4E j + E (lane / 16) ..
     static __device__ __forceinline__ void load_q(const KvcAttn& a, int r0, int head, int col, int cols, int lane, Q& q) {
-        const int use = min(col, cols - 1);
-        const T* src = static_cast<const T*>(a.q) + (int64_t)(r0 + use / a.group) * a.q_row + (int64_t)(head * a.group + use % a.group) * a.q_head + (lane >> 4) * L::E;
+        const int use = min(col, cols - 1), row = a.group(use), group = (int)a.group.d;
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(r0 + row) * a.q_row + (int64_t)(head * group + use - row * group) * a.q_head + (lane >> 4) * L::E;
+        if constexpr (PLANES == 1)
+            if (!a.plain) {                                 // (the bits as they are)
+                const uint32_t sign = !a.negative ? 0u : F32 ? 0x80000000u : 0x80008000u, keep = col < cols ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    u32x4_t v = *reinterpret_cast<const u32x4_any_t*>(src + j * 4 * L::E);
+                    q.w[j][0] = (v ^ sign) & keep;
+                }
+                return;
+            }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float x[8];
@@ -354,20 +384,28 @@ __device__ __forceinline__ void kvc_softmax(f32x4_t s[PAGES], const KvcAttn& a, 
             r.sum += s[p][i];
         }
 }
-// what a column has gathered, rows (dims) dim .. + 3, to its place or to the join
-template <typename T, int HD>
-__device__ __forceinline__ void kvc_finish(const KvcAttn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total, int part, int parts) {
+// What a column has gathered, blocks of 16 dims from d on (dims 16 d + 4 (lane / 16) + i each), to its place or to the join
+template <typename T, int HD, int COUNT>
+__device__ __forceinline__ void kvc_finish(const KvcAttn& a, int r0, int head, int col, int d, const f32x4_t acc[COUNT], float top, float total, int part, int parts) {
+    const int quad = (threadIdx.x & 63) >> 4, row = a.group(col), qh = head * (int)a.group.d + col - row * (int)a.group.d;
+    const int64_t line = (int64_t)(r0 + row) * a.heads + qh;
     if (parts > 1) {
-        const int64_t at = (row * a.heads + qh) * a.splits + part;
-        *reinterpret_cast<f32x4_t*>(a.part_o + at * HD + dim) = acc;
-        if (first) a.part_ml[at] = make_float2(top, total);
+        const int64_t at = line * a.splits + part;
+        float* dst = a.part_o + at * HD + d * 16 + quad * 4;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) *reinterpret_cast<f32x4_t*>(dst + i * 16) = acc[i];
+        if (d == 0 && quad == 0) a.part_ml[at] = make_float2(top, total);
         return;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst) = u32x2_t{f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv)};
-    else *reinterpret_cast<f32x4_any_t*>(dst) = acc * inv;
-    if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
+    T* dst = static_cast<T*>(a.out) + (int64_t)(r0 + row) * a.o_row + qh * a.o_head + d * 16 + quad * 4;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const f32x4_t x = acc[i] * inv;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst + i * 16) = u32x2_t{f2bf2(x[0], x[1]), f2bf2(x[2], x[3])};
+        else *reinterpret_cast<f32x4_any_t*>(dst + i * 16) = x;
+    }
+    if (d == 0 && quad == 0 && a.lse) a.lse[line] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
 }
 // Scores that a column must not see, where a chunk is not seen whole by all of them
 template <typename M, int NT> __device__ __forceinline__ void kvc_mask_scores(const KvcColumn see[NT], int slot0, int there, f32x4_t s[NT][M::PAGES]) {
@@ -406,10 +444,10 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, quad = lane >> 4;
     int list, tile, part;
     if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
-    const int b = kvc_by_length(a, list / a.c.hkv), head = list % a.c.hkv, col0 = tile * 16, col = col0 + (lane & 15);
+    const int at = a.by_heads(list), head = list - at * a.c.hkv, b = kvc_by_length(a, at), col0 = tile * 16, col = col0 + (lane & 15);
     int r0, count, n;
     kvc_rows(a, b, r0, count, n);
-    const int cols = count * a.group;
+    const int cols = count * (int)a.group.d;
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, M::CH, count, n, col0, min(cols, col0 + 16));
     const int parts = kvc_parts(a, span);
@@ -475,7 +513,7 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
-        if (col < cols) kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, acc, best, total, part, parts);
+        if (col < cols) kvc_finish<T, HD, 1>(a, r0, head, col, d, &acc, best, total, part, parts);
     }
 }
 
@@ -511,10 +549,10 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
     int list, tile, part;
     if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
-    const int b = kvc_by_length(a, list / a.c.hkv), head = list % a.c.hkv, col0 = tile * COLS;
+    const int at = a.by_heads(list), head = list - at * a.c.hkv, b = kvc_by_length(a, at), col0 = tile * COLS;
     int r0, count, n;
     kvc_rows(a, b, r0, count, n);
-    const int cols = count * a.group;
+    const int cols = count * (int)a.group.d;
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, CH, count, n, col0, min(cols, col0 + COLS));
     const int parts = kvc_parts(a, span);
@@ -541,7 +579,6 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     uint64_t ids_there = 0;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring + wave * OWN * 1024;
     auto request = [&](int i, int stage) {                  // returns which of the step's pages are there
-        i = min(i, end - 1);
         if (i - ids_from >= SPAN) {
             ids_from = i;
             const int at = kvc_slot<CH>(span, min(i + lane / PAGES, span.chunks - 1)) / KVC_PAGE + lane % PAGES;
@@ -568,13 +605,16 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     if (begin < end) {
         int there[R];                                       // of this step, the next one, ...
 #pragma unroll
-        for (int i = 0; i < R; ++i) there[i] = request(begin + i, i);
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((R - 1) * OWN) : "memory");
+        for (int i = 0; i < R; ++i) there[i] = begin + i < end ? request(begin + i, i) : 0;
+        if (begin + R <= end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((R - 1) * OWN) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         read_k(0, 0);
         int stage = 0;
         auto turn = [&](int i) {                            // the next step's entries have landed, this one's are in registers
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((R - 2) * OWN) : "memory");
-            const int last = request(i + R, stage);
+            // (of the steps i + 1 .. i + R - 1, requested in turn, all but the first may still be on their way; near the end there are fewer)
+            if (i + R <= end) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((R - 2) * OWN) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const int last = i + R < end ? request(i + R, stage) : 0;
 #pragma unroll
             for (int x = 0; x + 1 < R; ++x) there[x] = there[x + 1];
             there[R - 1] = last;
@@ -621,10 +661,7 @@ __global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_
     for (int t = 0; t < NT; ++t) {
         const int col = colw + 16 * t + (lane & 15);
         const float total = rows4_sum(run[t].sum);
-        if (col < cols)
-#pragma unroll
-            for (int d = 0; d < NB; ++d)
-                kvc_finish<T, HD>(a, r0 + col / a.group, head * a.group + col % a.group, d * 16 + quad * 4, d == 0 && quad == 0, o[t][d], run[t].top, total, part, parts);
+        if (col < cols) kvc_finish<T, HD, NB>(a, r0, head, col, 0, o[t], run[t].top, total, part, parts);
     }
 }
 
@@ -639,7 +676,7 @@ __global__ __launch_bounds__(256) void kvc_join_kernel(KvcAttn a) {
     int r0, count, n;
     kvc_rows(a, b, r0, count, n);
     if (r >= count) return;
-    const int cols = count * a.group, col0 = (r * a.group + qh % a.group) / a.tile_cols * a.tile_cols;
+    const int group = (int)a.group.d, cols = count * group, col0 = (r * group + qh % group) / a.tile_cols * a.tile_cols;
     const KvcSpan span = kvc_span(a, a.ch, count, n, col0, min(cols, col0 + a.tile_cols));
     const int parts = kvc_parts(a, span);
     if (parts == 1) return;                                 // a single part went to its place

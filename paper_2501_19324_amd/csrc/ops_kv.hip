@@ -155,7 +155,12 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     p.lists = c->batch * c->n_kv_heads;
     const bool parts3 = c->dtype == RSD_BF16 && a->dtype == RSD_F32;
     p.many = cols > 16;
-    p.tile_cols = !p.many ? 16 : parts3 || c->dtype == RSD_F32 || cols <= 64 ? 64 : 128;
+    p.tile_cols = 16;
+    if (p.many) {
+        p.tile_cols = 64;
+        const int64_t base = (int64_t)p.lists * ceil_div(cols, 128), parts = std::max<int64_t>(1, std::min(512 / base, max_kv / 1024));
+        if (a->dtype == RSD_BF16 && cols > 64 && max_kv - a->max_rows >= 768 && base * parts >= 384) p.tile_cols = 128;
+    }
     p.tiles = (int)ceil_div(cols, p.tile_cols);
     // slots of a chunk, or of a step of the kernel for many columns
     p.ch = (c->dtype == RSD_F32 ? 1 : 2) * KVC_PAGE * (p.many && (parts3 || p.tile_cols == 128) ? 2 : 1);
@@ -169,7 +174,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     int64_t parts;
     if (p.many) {
         p.waves = 4;
-        parts = std::min(ceil_div(1024, base), chunks / 8);
+        parts = p.tile_cols == 128 ? std::min(512 / base, max_kv / 1024) : std::min((c->dtype == RSD_F32 || cols <= 48 ? 1024 : 512) / base, max_kv / 256);
     } else {
         parts = std::min<int64_t>(ceil_div(256, base), chunks / 24);
         p.waves = (int)std::min<int64_t>(base * parts <= 256 || chunks >= 48 * parts ? 8 : 4, chunks);
@@ -304,7 +309,9 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     KvcAttn k{};
     k.c = dev_cache(c);
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
-    k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads, k.group = a->n_heads / c->n_kv_heads;
+    k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads;
+    auto divisor = [](int d) { return KvcDivisor{(uint32_t)d, d == 1 ? 0xFFFFFFFFu : (uint32_t)((1ull << 32) / (uint64_t)d + 1)}; };
+    k.group = divisor(a->n_heads / c->n_kv_heads), k.by_heads = divisor(c->n_kv_heads), k.by_tiles = divisor(p.tiles);
     k.scale = a->scale;
     k.plain = !(std::fabs(a->scale) > 0.f);
     k.factor2 = k.plain ? 1.4426950408889634f : (float)(std::fabs((double)a->scale) * 1.4426950408889634);
@@ -312,7 +319,7 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
-    k.max_kv = a->max_kv, k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
+    k.max_kv = std::min(a->max_kv, c->max_pages * KVC_PAGE), k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
     k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.turns = p.turns;
     k.part_o = static_cast<float*>(workspace);
     k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.o_bytes);
