@@ -535,10 +535,10 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
 // when all of the step's operands are in registers: behind it the next step's keys are read and this one's stage is requested anew.
 template <typename T, typename C, int HD, int NT> struct KvcMany {
     static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);
-    static constexpr int U = SMALL ? 1 : 2, R = SMALL ? 3 : 2, WAVES = SMALL ? 3 : 2, CH = U * KvcMath<T, C, HD>::CH;       // WAVES: to a SIMD; CH: slots of a step
+    static constexpr int U = SMALL ? 1 : 2, R = SMALL ? 3 : 2, CH = U * KvcMath<T, C, HD>::CH;      // CH: slots of a step
 };
 template <typename T, typename C, int HD, int NT>
-__global__ __launch_bounds__(256, (KvcMany<T, C, HD, NT>::WAVES)) void kvc_attn_many_kernel(KvcAttn a) {
+__global__ __launch_bounds__(256, 2) void kvc_attn_many_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;
     typedef KvcLayout<C, HD> L;
     typedef KvcMany<T, C, HD, NT> K;

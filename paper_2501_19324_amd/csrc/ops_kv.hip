@@ -174,7 +174,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     int64_t parts;
     if (p.many) {
         p.waves = 4;
-        parts = p.tile_cols == 128 ? std::min(512 / base, max_kv / 1024) : std::min((c->dtype == RSD_F32 || cols <= 48 ? 1024 : 512) / base, max_kv / 256);
+        parts = p.tile_cols == 128 ? std::min(512 / base, chunks * ch / 1024) : std::min((c->dtype == RSD_F32 ? 1024 : cols <= 48 ? 768 : 512) / base, chunks * ch / 512);
     } else {
         parts = std::min<int64_t>(ceil_div(256, base), chunks / 24);
         p.waves = (int)std::min<int64_t>(base * parts <= 256 || chunks >= 48 * parts ? 8 : 4, chunks);
