@@ -153,8 +153,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     const int group = a->n_heads / c->n_kv_heads, window = window_of(c, a);
     const int64_t cols = (int64_t)a->max_rows * group, max_kv = std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KVC_PAGE);
     p.lists = c->batch * c->n_kv_heads;
-    const bool parts3 = c->dtype == RSD_BF16 && a->dtype == RSD_F32;
-    p.many = cols > 16;
+    p.many = c->dtype == RSD_BF16 && (cols > 32 || (cols > 16 && p.lists >= 512));
     p.tile_cols = 16;
     if (p.many) {
         p.tile_cols = 64;
@@ -163,7 +162,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     }
     p.tiles = (int)ceil_div(cols, p.tile_cols);
     // slots of a chunk, or of a step of the kernel for many columns
-    p.ch = (c->dtype == RSD_F32 ? 1 : 2) * KVC_PAGE * (p.many && (parts3 || p.tile_cols == 128) ? 2 : 1);
+    p.ch = (c->dtype == RSD_F32 ? 1 : 2) * KVC_PAGE * (p.many && (a->dtype == RSD_F32 || p.tile_cols == 128) ? 2 : 1);
     const int ch = p.ch;
     int64_t chunks = std::max<int64_t>(1, ceil_div(max_kv, ch));
     if (window) {
@@ -174,10 +173,10 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     int64_t parts;
     if (p.many) {
         p.waves = 4;
-        parts = p.tile_cols == 128 ? std::min(512 / base, chunks * ch / 1024) : std::min((c->dtype == RSD_F32 ? 1024 : cols <= 48 ? 768 : 512) / base, chunks * ch / 512);
+        parts = p.tile_cols == 128 ? std::min(512 / base, chunks * ch / 1024) : std::min((cols <= 48 ? 768 : 512) / base, chunks * ch / 512);
     } else {
-        parts = std::min<int64_t>(ceil_div(256, base), chunks / 24);
-        p.waves = (int)std::min<int64_t>(base * parts <= 256 || chunks >= 48 * parts ? 8 : 4, chunks);
+        parts = std::max<int64_t>(1, std::min(256 / base, chunks * ch / 768));
+        p.waves = (int)std::min<int64_t>(base * parts <= 256 || (chunks * ch >= 1536 * parts && base < 1 << 21) ? 8 : 4, chunks);
     }
     p.split = (int)ceil_div(chunks, std::max<int64_t>(1, parts));
     p.splits = (int)ceil_div(chunks, p.split);
@@ -196,15 +195,17 @@ int check_attn(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     if (a->n_heads < 1 || a->n_heads % c->n_kv_heads) return fail(RSD_EINVAL, "attention: %d heads over %d kv heads", a->n_heads, c->n_kv_heads);
     if (a->window < 0 || a->sinks < 0) return fail(RSD_EINVAL, "attention: window %d, sinks %d", a->window, a->sinks);
     if (!a->row_start && a->max_rows != 1) return fail(RSD_EINVAL, "attention: max_rows %d without row_start", a->max_rows);
-    if ((int64_t)a->max_rows * a->n_heads > INT32_MAX / 16 || c->batch * (int64_t)c->n_kv_heads * ceil_div((int64_t)a->max_rows * (a->n_heads / c->n_kv_heads), 64) > kMostBlocks / 2)
+    if ((int64_t)a->max_rows * a->n_heads > INT32_MAX / 16 || c->batch * (int64_t)c->n_kv_heads * ceil_div((int64_t)a->max_rows * (a->n_heads / c->n_kv_heads), 64) > 1 << 20)
         return fail(RSD_EINVAL, "attention: %d rows x %d heads x %d sequences", a->max_rows, a->n_heads, c->batch);
     return RSD_OK;
 }
 template <typename T, typename C, int HD> void attn_run(const KvcAttn& k, const AttnPlan& p, Launches& l) {
     const unsigned grid = (unsigned)kvc_blocks(p.lists, p.tiles, p.splits);
     if (!p.many) l.run(kvc_attn_few_kernel<T, C, HD>, grid, 64 * p.waves, 0, k);
-    else if (p.tile_cols == 64) l.run(kvc_attn_many_kernel<T, C, HD, 1>, grid, 256, 0, k);
-    else if constexpr (sizeof(T) == 2) l.run(kvc_attn_many_kernel<T, C, HD, 2>, grid, 256, 0, k);
+    else if constexpr (sizeof(C) == 2) {
+        if (p.tile_cols == 64) l.run(kvc_attn_many_kernel<T, C, HD, 1>, grid, 256, 0, k);
+        else if constexpr (sizeof(T) == 2) l.run(kvc_attn_many_kernel<T, C, HD, 2>, grid, 256, 0, k);
+    }
     if (p.splits > 1) l.run(kvc_join_kernel<T, HD>, (unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, k);
 }
 template <typename T, typename C> void attn_run(const KvcAttn& k, const AttnPlan& p, int hd, Launches& l) {
