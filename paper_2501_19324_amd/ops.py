@@ -150,15 +150,16 @@ def _done(rc: int, lib):
         raise _b.RsdError(rc, lib.rsd_op_last_error().decode())
 
 
-_current_device = torch.cuda.current_device
+# the current device as a number, without the checks that a tensor on some GPU has passed already (0.1 instead of 0.4 us)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 # torch.cuda.current_stream(d).cuda_stream without the stream object (0.1 instead of 1.9 us, of the 6 to 10 that a small call takes)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
 
 def _stream(t: torch.Tensor) -> int:
     """The current stream of the device that `t` lies on, which has to be the current device."""
-    d = t.device.index
-    if d is None or d != _current_device():
+    d = t.get_device()
+    if d < 0 or d != _current_device():
         _bad(f"tensors have to be on the current device: got {t.device}")
     return _raw_stream(d)
 
@@ -428,40 +429,46 @@ def rsd_rope(rot_dim: int, theta: float = 1e4, *, scaling: str = "plain", factor
 _ROPE_BYTES, _HEADS_BYTES = struct.Struct("=Qiifi").pack, struct.Struct("=QQQqqqqii").pack
 _KV_CACHE_BYTES, _KV_ATTN_BYTES = struct.Struct("=QQQiiiiii").pack, struct.Struct("=QQQqqqqQiiiiiiif").pack
 _f64 = torch.float64
-_empty_like, _contiguous = torch.empty_like, torch.contiguous_format
 
 
-def _rope(rope, like: torch.Tensor, hd: int) -> bytes:
+def _rope(rope, device: int, hd: int) -> bytes:
     freq, interleaved, magnitude = rope
     shape = freq.shape
-    if freq.dtype is not _f64 or freq.device != like.device or len(shape) != 1 or not freq.is_contiguous() or not 2 <= 2 * shape[0] <= hd:
-        _bad(f"rope: the frequencies are {freq.dtype} {tuple(shape)} on {freq.device}, needed float64 [1 .. {hd // 2}] on {like.device}, contiguous")
+    if freq.dtype is not _f64 or freq.get_device() != device or len(shape) != 1 or not freq.is_contiguous() or not 2 <= 2 * shape[0] <= hd:
+        _bad(f"rope: the frequencies are {freq.dtype} {tuple(shape)} on {freq.device}, needed float64 [1 .. {hd // 2}] on cuda:{device}, contiguous")
     try:
         return _ROPE_BYTES(freq.data_ptr(), 2 * shape[0], 1 if interleaved else 0, magnitude, 0)
     except (struct.error, OverflowError):
         _bad(f"rope: magnitude {magnitude!r}")
 
 
-def _heads(name: str, x: torch.Tensor, rows: int, hd: int, dtype, device, weight: Optional[torch.Tensor], out: Optional[torch.Tensor], writes: bool):
+def _ints(name: str, t: torch.Tensor, device: int, rows: int) -> int:
+    """Address of a contiguous int32 [rows]."""
+    if t.dtype is not _i32 or t.shape != (rows,) or t.get_device() != device or not t.is_contiguous():
+        _bad(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, needed {_i32} [{rows}] on cuda:{device}, contiguous")
+    return t.data_ptr()
+
+
+def _heads(name: str, x: torch.Tensor, rows: int, hd: int, dtype, device: int, weight: Optional[torch.Tensor], out: Optional[torch.Tensor], writes: bool):
     """The heads of x [rows, heads, hd], and where they go: (structure, out)."""
-    shape, (xr, xh, one) = x.shape, x.stride() if x.dim() == 3 else (0, 0, 0)
-    if one != 1 or shape[0] != rows or shape[2] != hd or x.dtype is not dtype or x.device != device:
-        _bad(f"{name}: {x.dtype} {tuple(shape)} on {x.device}, strides {x.stride()}, needed {dtype} [{rows}, heads, {hd}] on {device}, contiguous heads")
-    heads, wp = shape[1], 0
+    shape, stride = x.shape, x.stride()
+    if len(stride) != 3 or stride[2] != 1 or shape[0] != rows or shape[2] != hd or x.dtype is not dtype or x.get_device() != device:
+        _bad(f"{name}: {x.dtype} {tuple(shape)} on {x.device}, strides {stride}, needed {dtype} [{rows}, heads, {hd}] on cuda:{device}, contiguous heads")
+    wp = 0
     if weight is not None:
-        if weight.dtype is not dtype or weight.shape != (hd,) or not weight.is_contiguous() or weight.device != device:
-            _bad(f"{name}_weight: {weight.dtype} {tuple(weight.shape)} on {weight.device}, needed {dtype} [{hd}] on {device}, contiguous")
+        if weight.dtype is not dtype or weight.shape != (hd,) or not weight.is_contiguous() or weight.get_device() != device:
+            _bad(f"{name}_weight: {weight.dtype} {tuple(weight.shape)} on {weight.device}, needed {dtype} [{hd}] on cuda:{device}, contiguous")
         wp = weight.data_ptr()
     if not writes:
-        return _HEADS_BYTES(x.data_ptr(), 0, wp, xr, xh, 0, 0, heads, 0), None
+        return _HEADS_BYTES(x.data_ptr(), 0, wp, stride[0], stride[1], 0, 0, shape[1], 0), None
     if out is None:
-        out = _empty_like(x, memory_format=_contiguous)
-        orow, oh = heads * hd, hd
-    else:
-        orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
-        if one != 1 or out.shape != shape or out.dtype is not dtype or out.device != device:
-            _bad(f"{name}_out: {out.dtype} {tuple(out.shape)} on {out.device}, strides {out.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
-    return _HEADS_BYTES(x.data_ptr(), out.data_ptr(), wp, xr, xh, orow, oh, heads, 0), out
+        heads = shape[1]
+        out = x.new_empty(rows, heads, hd)
+        return _HEADS_BYTES(x.data_ptr(), out.data_ptr(), wp, stride[0], stride[1], heads * hd, hd, heads, 0), out
+    to = out.stride()
+    if out.shape != shape or to[2] != 1 or out.dtype is not dtype or out.get_device() != device:
+        _bad(f"{name}_out: {out.dtype} {tuple(out.shape)} on {out.device}, strides {to}, needed {dtype} {tuple(shape)} on cuda:{device}, contiguous heads")
+    return _HEADS_BYTES(x.data_ptr(), out.data_ptr(), wp, stride[0], stride[1], to[0], to[1], shape[1], 0), out
 
 
 def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.Tensor], rope=None, *, q_weight: Optional[torch.Tensor] = None,
@@ -475,7 +482,7 @@ def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[t
         _bad(f"qk_rope: q is {dtype} {tuple(shape)}, needed fp32 or bf16 [rows, heads, 32, 64, 128 or 256]")
     st = _stream(q)
     rows, _, hd = shape
-    device = q.device
+    device = q.get_device()
     qs, q_out = _heads("q", q, rows, hd, dtype, device, q_weight, q_out, True)
     ks = pp = rs = None
     if k is not None:
@@ -483,12 +490,14 @@ def rsd_qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[t
     elif k_weight is not None or k_out is not None:
         _bad("qk_rope: k_weight or k_out without k")
     if rope is not None:
-        rs = _rope(rope, q, hd)
+        rs = _rope(rope, device, hd)
         if position is None:
             _bad("qk_rope: a rotation without positions")
-        pp = _flat("position", position, q, _i32, (rows,))
+        pp = _ints("position", position, device, rows)
     if rows:
-        _done(lib.rsd_qk_rope(qs, ks, pp, rs, eps, rows, hd, t, st), lib)
+        rc = lib.rsd_qk_rope(qs, ks, pp, rs, eps, rows, hd, t, st)
+        if rc:
+            _done(rc, lib)
     return q_out, k_out
 
 
@@ -501,22 +510,23 @@ def rsd_kv_cache(batch: int, max_pages: int, n_pages: int, n_kv_heads: int, head
 
 
 def _kv_cache(c):
-    """A cache as bytes, with what its calls go by: (bytes, pool, stream, (n_pages, n_kv_heads, head_dim, batch, max_pages, dtype))."""
+    """A cache as bytes, with what its calls go by: (bytes, pool, device, stream, (n_pages, n_kv_heads, head_dim, batch, max_pages, dtype))."""
     pool, table, kv_len = c
     st = _stream(pool)
-    shape, dev, t = pool.shape, pool.device, _TYPE.get(pool.dtype)
+    device = pool.get_device()
+    shape, entries, t = pool.shape, table.shape, _TYPE.get(pool.dtype)
     if t is None or len(shape) != 4 or shape[2] != 2 or shape[3] % PAGE or not pool.is_contiguous():
         _bad(f"cache: the pool is {pool.dtype} {tuple(shape)}, needed fp32 or bf16 [pages, kv heads, 2, {PAGE} * head_dim], contiguous")
-    if table.dtype is not _i32 or table.device != dev or table.dim() != 2 or not table.is_contiguous():
-        _bad(f"cache: the table is {table.dtype} {tuple(table.shape)} on {table.device}, needed int32 [batch, pages] on {dev}, contiguous")
-    batch, max_pages = table.shape
-    if kv_len.dtype is not _i32 or kv_len.device != dev or kv_len.shape != (batch,) or not kv_len.is_contiguous():
-        _bad(f"cache: kv_len is {kv_len.dtype} {tuple(kv_len.shape)} on {kv_len.device}, needed int32 [{batch}] on {dev}, contiguous")
+    if table.dtype is not _i32 or table.get_device() != device or len(entries) != 2 or not table.is_contiguous():
+        _bad(f"cache: the table is {table.dtype} {tuple(entries)} on {table.device}, needed int32 [batch, pages] on {pool.device}, contiguous")
+    batch, max_pages = entries
     sizes = (shape[0], shape[1], shape[3] // PAGE, batch, max_pages, t)
+    if kv_len.dtype is not _i32 or kv_len.get_device() != device or kv_len.shape != (batch,) or not kv_len.is_contiguous():
+        _bad(f"cache: kv_len is {kv_len.dtype} {tuple(kv_len.shape)} on {kv_len.device}, needed int32 [{batch}] on {pool.device}, contiguous")
     try:
-        return _KV_CACHE_BYTES(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), *sizes), pool, st, sizes
+        return _KV_CACHE_BYTES(pool.data_ptr(), table.data_ptr(), kv_len.data_ptr(), *sizes), pool, device, st, sizes
     except struct.error:
-        _bad(f"cache: pool {tuple(shape)}, table {tuple(table.shape)}")
+        _bad(f"cache: pool {tuple(shape)}, table {tuple(entries)}")
 
 
 def rsd_kv_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, slot: torch.Tensor, *, position: Optional[torch.Tensor] = None, rope=None,
@@ -525,40 +535,42 @@ def rsd_kv_append(cache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, sl
     """Writes keys and values ``[rows, n_kv_heads, head_dim]`` into slot ``slot[i]`` of sequence ``seq[i]``, the keys normed (with ``k_weight``) and rotated (with ``rope``, at
     ``position``) on their way; queries ``q [rows, heads, head_dim]`` of the same tokens go through the same in the same launch and are returned.  ``kv_len`` is left to the caller."""
     lib = _lib or _load()
-    c, pool, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
-    dtype, shape, device = k.dtype, k.shape, pool.device
+    c, pool, device, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
+    dtype, shape = k.dtype, k.shape
     t = _TYPE.get(dtype)
     if t is None or len(shape) != 3 or shape[1] != kv_heads:
         _bad(f"append: k is {dtype} {tuple(shape)}, needed fp32 or bf16 [rows, {kv_heads}, {hd}]")
     rows = shape[0]
     ks, _ = _heads("k", k, rows, hd, dtype, device, k_weight, None, False)
-    vr, vh, one = v.stride() if v.dim() == 3 else (0, 0, 0)
-    if one != 1 or v.shape != shape or v.dtype is not dtype or v.device != device:
-        _bad(f"v: {v.dtype} {tuple(v.shape)} on {v.device}, strides {v.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
-    sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
+    stride = v.stride()
+    if v.shape != shape or stride[2] != 1 or v.dtype is not dtype or v.get_device() != device:
+        _bad(f"v: {v.dtype} {tuple(v.shape)} on {v.device}, strides {stride}, needed {dtype} {tuple(shape)} on cuda:{device}, contiguous heads")
+    sp, lp = _ints("seq", seq, device, rows), _ints("slot", slot, device, rows)
     qs = pp = rs = None
     if q is not None:
         qs, q_out = _heads("q", q, rows, hd, dtype, device, q_weight, q_out, True)
     elif q_weight is not None or q_out is not None:
         _bad("append: q_weight or q_out without q")
     if rope is not None:
-        rs = _rope(rope, pool, hd)
+        rs = _rope(rope, device, hd)
         if position is None:
             _bad("append: a rotation without positions")
-        pp = _flat("position", position, pool, _i32, (rows,))
+        pp = _ints("position", position, device, rows)
     if rows:
-        _done(lib.rsd_kv_append(c, ks, v.data_ptr(), vr, vh, qs, sp, lp, pp, rs, eps, rows, t, st), lib)
+        rc = lib.rsd_kv_append(c, ks, v.data_ptr(), stride[0], stride[1], qs, sp, lp, pp, rs, eps, rows, t, st)
+        if rc:
+            _done(rc, lib)
     return q_out
 
 
 def rsd_kv_read(cache, seq: torch.Tensor, slot: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """Keys and values ``[rows, n_kv_heads, head_dim]`` of the entries (seq[i], slot[i]); zeros where there is none."""
     lib = _lib or _load()
-    c, pool, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
+    c, pool, device, st, (_, kv_heads, hd, _, _, _) = _kv_cache(cache)
     if seq.dim() != 1:
         _bad(f"seq: shape {tuple(seq.shape)}, needed [rows]")
     rows = seq.shape[0]
-    sp, lp = _flat("seq", seq, pool, _i32, (rows,)), _flat("slot", slot, pool, _i32, (rows,))
+    sp, lp = _ints("seq", seq, device, rows), _ints("slot", slot, device, rows)
     k, v = pool.new_empty(2, rows, kv_heads, hd).unbind()
     if rows:
         _done(lib.rsd_kv_read(c, sp, lp, rows, k.data_ptr(), v.data_ptr(), st), lib)
@@ -581,13 +593,12 @@ def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optiona
     sequence's newest; their places in the result, like those of rows that no sequence has, are not written.  ``max_kv`` bounds ``kv_len`` (default: what the table can hold).  The tighter both are, the better the work is
     dealt.  With ``window`` a row sees its own entry, the window - 1 before it, and a sequence's first ``sinks``.  ``out`` may be ``q`` itself.  Returns ``out``, or ``(out, lse)`` with ``want_lse``."""
     lib = _lib or _load()
-    c, pool, st, sizes = _kv_cache(cache)
+    c, pool, device, st, sizes = _kv_cache(cache)
     _, kv_heads, hd, batch, max_pages, _ = sizes
-    dtype, shape, device = q.dtype, q.shape, pool.device
+    dtype, shape, stride = q.dtype, q.shape, q.stride()
     t = _TYPE.get(dtype)
-    qr, qh, one = q.stride() if q.dim() == 3 else (0, 0, 0)
-    if t is None or one != 1 or shape[2] != hd or q.device != device:
-        _bad(f"attention: q is {dtype} {tuple(shape)} on {q.device}, strides {q.stride()}, needed fp32 or bf16 [rows, heads, {hd}] on {device}, contiguous heads")
+    if t is None or len(shape) != 3 or stride[2] != 1 or shape[2] != hd or q.get_device() != device:
+        _bad(f"attention: q is {dtype} {tuple(shape)} on {q.device}, strides {stride}, needed fp32 or bf16 [rows, heads, {hd}] on {pool.device}, contiguous heads")
     rows, heads, _ = shape
     if heads == 0 or kv_heads == 0 or heads % kv_heads:
         _bad(f"attention: {heads} heads over {kv_heads} kv heads")
@@ -598,23 +609,30 @@ def rsd_kv_attention(cache, q: torch.Tensor, scale: float, *, row_start: Optiona
             _bad(f"attention: {rows} rows for {batch} sequences, max_rows {max_rows}, without row_start")
     else:
         max_rows = rows if max_rows is None else max_rows
-        rp = _flat("row_start", row_start, pool, _i32, (batch + 1,))
+        rp = _ints("row_start", row_start, device, batch + 1)
     if window.__class__ is not int or sinks.__class__ is not int or not 0 <= window < 1 << 31 or not 0 <= sinks < 1 << 31:
         window, sinks = _int("attention: window", window, 0), _int("attention: sinks", sinks, 0)
     if out is None:
-        out = _empty_like(q, memory_format=_contiguous)
+        out = q.new_empty(rows, heads, hd)
         orow, oh = heads * hd, hd
     else:
-        orow, oh, one = out.stride() if out.dim() == 3 else (0, 0, 0)
-        if one != 1 or out.shape != shape or out.dtype is not dtype or out.device != device:
-            _bad(f"attention: out is {out.dtype} {tuple(out.shape)} on {out.device}, strides {out.stride()}, needed {dtype} {tuple(shape)} on {device}, contiguous heads")
+        to = out.stride()
+        if out.shape != shape or to[2] != 1 or out.dtype is not dtype or out.get_device() != device:
+            _bad(f"attention: out is {out.dtype} {tuple(out.shape)} on {out.device}, strides {to}, needed {dtype} {tuple(shape)} on {pool.device}, contiguous heads")
+        orow, oh, _ = to
     lse = q.new_empty((rows, heads), dtype=_f32) if want_lse else None
     if rows:
-        max_rows = _int("attention: max_rows", max_rows, 1)
+        if max_rows.__class__ is not int or not 1 <= max_rows < 1 << 31:
+            max_rows = _int("attention: max_rows", max_rows, 1)
         cap = max_pages * PAGE
         max_kv = cap if max_kv is None else min(max(int(max_kv), -1), cap)
+        try:
+            a = _KV_ATTN_BYTES(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, stride[0], stride[1], orow, oh, rp, rows, max_rows, heads, max_kv, window, sinks, t, scale)
+        except (struct.error, OverflowError):
+            _bad(f"attention: {rows} rows of {heads} heads, scale {scale!r}")
         nbytes = _kv_attn_bytes(sizes, rows, max_rows, heads, max_kv, window, sinks, t, rp != 0)
-        ws, wp = _workspace(nbytes, pool)
-        a = _KV_ATTN_BYTES(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, qr, qh, orow, oh, rp, rows, max_rows, heads, max_kv, window, sinks, t, scale)
-        _done(lib.rsd_kv_attention(c, a, wp, nbytes, st), lib)
+        ws = pool.new_empty(nbytes, dtype=_u8) if nbytes else None
+        rc = lib.rsd_kv_attention(c, a, ws.data_ptr() if nbytes else None, nbytes, st)
+        if rc:
+            _done(rc, lib)
     return (out, lse) if want_lse else out
