@@ -178,11 +178,12 @@ typedef struct rsd_kv_cache {
 
 /* Writes entries: row i (keys and values [n_kv_heads][head_dim], dev, of `dtype`) becomes slot[i] of sequence seq[i] (dev int32 [rows]; the pairs must differ), the keys as in
  * rsd_qk_rope on their way (k->out is not used), both rounded once to the cache's type.  kv_len is neither read nor changed.  q (may be NULL) goes to q->out in
- * the same launch, also for rows that name no entry of the cache.  q->out may be q->x and shares no memory with anything else of the call. */
+ * the same launch, also for rows that name no entry of the cache.  q->out may be q->x and shares no memory with anything else of the call; k, v and q->x lie outside the pool. */
 int rsd_kv_append(const rsd_kv_cache *c, const rsd_heads *k, const void *v, int64_t v_row, int64_t v_head, const rsd_heads *q, const int32_t *seq,
                   const int32_t *slot, const int32_t *position, const rsd_rope *rope, float eps, int32_t rows, int32_t dtype, void *hip_stream);
 
-/* Reads entries back: k, v dev [rows][n_kv_heads][head_dim], contiguous, 16-byte aligned, of the cache's type; zeros for rows that name no entry of the cache. */
+/* Reads entries back: k, v dev [rows][n_kv_heads][head_dim], contiguous, 16-byte aligned, of the cache's type; zeros for rows that name no entry of the cache.
+ * They share no memory with each other or with what the call reads. */
 int rsd_kv_read(const rsd_kv_cache *c, const int32_t *seq, const int32_t *slot, int32_t rows, void *k, void *v, void *hip_stream);
 
 /* Attention of new tokens over the cache (their own entries included).  Sequence b has the rows row_start[b] .. row_start[b + 1] - 1 (dev [batch + 1]; NULL: row b alone), at
@@ -191,7 +192,8 @@ int rsd_kv_read(const rsd_kv_cache *c, const int32_t *seq, const int32_t *slot, 
  * q, out dev [rows][n_heads][head_dim] of `dtype` with row and head strides; head h reads kv head h / (n_heads / n_kv_heads).  out = softmax(scale q.K) V; a row
  * that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of the sum of exp(scale q.k), -inf for such rows.  An infinity or NaN
  * in an entry reaches the rows that see it and no others.  Sizes: batch * n_kv_heads * (max_rows * n_heads / n_kv_heads in whole 64s) up to
- * 2^26, max_rows * n_heads below 2^27.  out may be q itself and shares no memory with it else. */
+ * 2^26, max_rows * n_heads below 2^27.  out may be q itself; but for that, out, lse and the workspace share no memory with each other or with
+ * what the call reads (an array that lies between the ends of another counts as sharing). */
 typedef struct rsd_kv_attn {
     const void *q;
     void *out;

@@ -100,7 +100,7 @@ template <int K> __device__ __forceinline__ uint32_t kvc_take(const uint32_t x[4
 // Values into their pages: a block takes 16 rows of a head (of several, where they are short), a quad of lanes G dims of four rows.  The four tokens whose values lie together in a page are mostly four
 // rows that follow each other, at any place among the rows: the quad that has the first of them loads all four, one to a lane, exchanges, and stores a dim's four tokens at once.  Rows
 // that are not among four such go value by value.
-// 7937 rows of 16 heads of 64, bf16, with queries and keys (98 MB): TIMEV
+// Bound by bytes: 7937 rows of 28 heads of 128 and 4, bf16 (146 MB with queries and keys), 31 us, 36 with every value loaded and stored by itself; of 16 heads of 64 (98 MB) 24.
 template <typename C, int HD> struct KvcValueBlock {
     static constexpr int ROWS = 16, G = sizeof(C) == 2 ? 8 : 4, QUADS = HD / G, HEADS = QUADS >= 16 ? 1 : 16 / QUADS;      // quads of a row's values; heads of a block
 };
@@ -174,9 +174,11 @@ template <typename T, typename C, int HD> __device__ __forceinline__ void kvc_wr
 
 // HD / 16 lanes take a head, 16 of its dims each: eight pairs where they are interleaved, (2 i, 2 i + 1), or in halves, (i, i + rot / 2) and, behind the rotation, (rot + j, rot + rest / 2 + j),
 // as two runs of eight neighbours, read and written 16 bytes at a time.  Halves of a rotation of which 16 is no divisor (SPLIT) take 16 neighbours and exchange
-// with the lanes that have their partners through LDS (8192 rows of 32 heads, bf16: TIMES us, 85 with pairs read one by one).
+// with the lanes that have their partners through LDS (8192 rows of 32 heads, bf16: 35 us, 85 with pairs read one by one).
 // A block takes 16 * 256 / HD neighbouring (row, head) and forms the angles of its rows once, one to a thread, for all their heads.  The turns position * freq / 2 pi are
-// formed and reduced in 64 bits: in 32 an angle at position 10^5 is off by some 2^-8.
+// formed and reduced in 64 bits: in 32 an angle at position 10^5 is off by some 2^-8.  Norm and rotation are computed in fp32 and rounded once.
+// Bound by bytes: 8192 rows of 32 heads, bf16 (134 MB), 23.8 us, 5.6 TB/s; 7937 rows of 72 heads, fp32 (585 MB), 116 us, 5.0 TB/s; 16 prompts of 480 .. 512 tokens, 72B heads, fp32 into a bf16 cache (618 MB),
+// 127 us, 4.9 TB/s.  Single tokens of 64 sequences: 4.6 us, a chain of latencies (row numbers, table, stores).
 template <typename T, typename C, int HD, bool INTERLEAVED, bool SPLIT, bool CACHE>
 __global__ __launch_bounds__(256) void kvc_rows_kernel(KvcRows a) {
     constexpr int LANES = HD / 16, ITEMS = 256 / LANES, P = HD / 2, LINE = HD + LANES;
@@ -184,7 +186,6 @@ __global__ __launch_bounds__(256) void kvc_rows_kernel(KvcRows a) {
     __shared__ float2 turn[ITEMS * P];
     __shared__ float lines[SPLIT ? ITEMS * LINE : 1];       // 17 words to a lane's 16 dims: lanes on different banks
     const int heads = a.q.n + a.k.n, total = a.rows * heads;
-    // the first blocks write values
     // Blocks that write values are spread evenly among the others, so that a row's pieces are read at about one time.
     int block = blockIdx.x;
     if (CACHE) {

@@ -138,7 +138,7 @@ __device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, in
 //   bf16 over bf16: operands as they are.  A probability enters the second product rounded to bf16, off by at most 2^-8 of itself like a
 //     result that is rounded to bf16 itself; the sum it is divided by has all of its bits.
 //   fp32 over bf16: q and probabilities in three bf16 parts, which hold all 24 bits; three matrix instructions each.  They are cut, not rounded, so that all have the sign of the whole, and
-//     none is 0 where the whole is not (2^-30 of it stands in): an infinite key or value meets no 0 that would make a NaN of it.
+//     none is 0 where the whole is not (2^-30 of it stands in, or is added): an infinite key or value meets no 0 that would make a NaN of it.
 //   fp32 over fp32: matrix instructions in fp32.
 template <typename T, typename C, int HD> struct KvcMath {
     typedef KvcLayout<C, HD> L;
@@ -237,11 +237,11 @@ template <typename T, typename C, int HD> struct KvcMath {
                 const float x = s[i / 2][2 * (i & 1)], y = s[i / 2][2 * (i & 1) + 1];
                 if constexpr (PLANES == 1) p.w[0][i] = f2bf2(x, y);
                 else {                                      // (a probability is not negative)
-                    const float xl = x * 0x1p-30f, yl = y * 0x1p-30f;
-                    const float x1 = fmaxf(x - first_part(x), xl), y1 = fmaxf(y - first_part(y), yl);
+                    const float x1 = __builtin_fmaf(x, 0x1p-30f, x - first_part(x)), y1 = __builtin_fmaf(y, 0x1p-30f, y - first_part(y));
+                    const float x2 = __builtin_fmaf(x, 0x1p-30f, x1 - first_part(x1)), y2 = __builtin_fmaf(y, 0x1p-30f, y1 - first_part(y1));
                     p.w[0][i] = first_parts(x, y);
                     p.w[1][i] = first_parts(x1, y1);
-                    p.w[2][i] = first_parts(fmaxf(x1 - first_part(x1), xl), fmaxf(y1 - first_part(y1), yl));
+                    p.w[2][i] = first_parts(x2, y2);
                 }
             }
         return p;
@@ -432,9 +432,12 @@ __device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan
     M::strip(v);
 }
 
-// Few columns (single tokens): a block owns a tile of 16 columns of one (sequence, kv head) and one part of its chunks, which its waves take in
+// Few columns (single tokens), and everything over an fp32 cache: a block owns a tile of 16 columns of one (sequence, kv head) and one part of its chunks, which its waves take in
 // turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's keys are requested as soon as this one's are used up, the values likewise, the table entries
-// one chunk earlier still.
+// one chunk earlier still: one set of registers for each instead of two, and eight waves on a CU.
+// Bound by bytes: 256 sequences of 4096 .. 8192 entries, 7B heads, bf16 (3.24 GB): 537 us, 6.0 TB/s, what a read alone reaches (572 with two whole chunks of registers, 558 with four waves to a
+// block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 7 .. 9 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
+// rows: 49 us, matrix instructions in fp32 busy 40 % of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
 template <typename T, typename C, int HD>
 __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;
@@ -530,9 +533,15 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
 }
 
-// Many columns (chunks of prompts, steps, scoring): a block of four waves owns 64 * NT columns, NT tiles to a wave, and one part of their steps of U chunks.  The steps go through a ring of
+// Many columns over a bf16 cache (chunks of prompts, steps, scoring): a block of four waves owns 64 * NT columns, NT tiles to a wave, and one part of their steps of U chunks.  The steps go through a ring of
 // R stages in LDS, straight from memory (pages are operands as they are), a quarter of each by every wave.  The one barrier of a step stands in the middle of its last chunk,
 // when all of the step's operands are in registers: behind it the next step's keys are read and this one's stage is requested anew.
+// 2048 rows of a 7B prompt's 8192 entries: 218 us, 963 TFLOP/s of the 1396 that a plain product of 8192^3 reaches (281 with NT = 1; 423 with a tile of 16 to a block and no ring).  Matrix instructions
+// are busy 42 % of the time, vector instructions about as long (per 32 entries and 16 columns 16 of the one and 50 of the other, 8 of them exponentials); two waves on a SIMD, of different blocks,
+// overlap them in part.  Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  Neither priorities of waves nor eight-byte reads of the values
+// (no moves, twice the reads) changed the time.
+// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 112 us, 0.83 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
+// 256 of 2048 entries, 8 rows: 198 us, 5.6 TB/s.
 template <typename T, typename C, int HD, int NT> struct KvcMany {
     static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);
     static constexpr int U = SMALL ? 1 : 2, R = SMALL ? 3 : 2, CH = U * KvcMath<T, C, HD>::CH;      // CH: slots of a step

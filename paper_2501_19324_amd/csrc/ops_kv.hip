@@ -39,6 +39,12 @@ Bytes bytes_of(const void* p, int64_t n0, int64_t s0, int64_t n1, int64_t s1, in
 }
 Bytes bytes_of(const void* p, int64_t bytes) { return bytes_of(p, 1, 0, 1, 0, bytes, 1); }
 bool meet(Bytes a, Bytes b) { return a.from < b.to && b.from < a.to; }
+// whether an array meets the pool, the table or (where it is used) kv_len
+bool meets_cache(Bytes a, const rsd_kv_cache* c, bool lengths) {
+    const int64_t page = 2ll * KVC_PAGE * c->head_dim * c->n_kv_heads;
+    return meet(a, bytes_of(c->pool, c->n_pages, page, 1, 0, page, size_of(c->dtype))) || meet(a, bytes_of(c->table, 4ll * c->batch * c->max_pages)) ||
+           (lengths && meet(a, bytes_of(c->kv_len, 4ll * c->batch)));
+}
 
 struct RowArgs {
     const rsd_heads *q, *k;
@@ -148,6 +154,16 @@ struct AttnPlan {
 // a window that no row reaches past is none
 int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >= std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KVC_PAGE) ? 0 : a->window; }
 
+// Which kernel, which tiles, how the entries are split: by the sizes that the host knows.  Measured with 28 heads over 4 of 128, bf16, where nothing else is said, in us:
+//  - the kernel of few columns takes up to two tiles of 16 (21 columns, 4 sequences of 2048 entries: 13.2, the other 15.8; 64 of 128 .. 2048, fp32 activations: 32 and 39; 64 of 128 .. 5120: 71 and 70),
+//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 49 and 63).
+//  - 128 columns to a block instead of 64 where rows see 768 entries and more before their own (2048 rows of 8192: 223 and 280, 16 x 128 of 1024: 48 and 54; against that 2048 of 2048: 58 and 50,
+//    64 x 128 of 300: 87 and 74) and there are 384 such blocks with their parts (512 rows of 8192: 84 and 92; against that 4 x 128 of 2048: 42 and 36, 256 of 8192: 56 and 54).
+//  - a part's sums are 4 bytes an element written and read, beside the join's launch.  Many columns are split up to 512 blocks (16 x 128 of 1024: 50 whole, 71 in two; 256 x 8 of 2048: 197 whole, 244 in two;
+//    256 of 8192: 166 whole, 57 in eight), up to 48 columns for 768 (64 x 5 of 128 .. 5120: 89 whole, 74 in three, 85 in four; where all have 5120 the three cost: 116 whole, 140), no part under 512 or 1024 entries.
+//    Few columns for 256 blocks, no part under 768 (one sequence of 1279: 9.9 whole, 10.8 in two; of 2500: 14.4 whole, 11.9 in three; of 8000: 39 whole, 15.7 in ten; 16 of 8000: 67 whole, 46 .. 49 in two to four).
+//  - few columns: eight waves up to 256 blocks (one sequence of 896 .. 1279: 9.8, 11.1 with four) and for long lists (256 of 4096 .. 8192: 535 and 558), else four (window 1024: 101, 105 with eight; heads of 64: 49 and 54).
+//  - the longest lists first, from the point where the blocks are more than the card holds at once (64 x 5 of 128 .. 5120: 75 and 84; 256 of 4096 .. 8192: 534 and 555).
 AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     AttnPlan p{};
     const int group = a->n_heads / c->n_kv_heads, window = window_of(c, a);
@@ -259,9 +275,7 @@ extern "C" int rsd_kv_append(const rsd_kv_cache* c, const rsd_heads* k, const vo
     if (!aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: v is not aligned to its type");
     const RowArgs a{q, k, v, v_row, v_head, position, seq, slot, rope, eps, rows, c->head_dim, dtype};
     if (int rc = check_rows(a, true, "append")) return rc;
-    if (q && (meet(bytes_of(q->out, rows, q->out_row, q->n_heads, q->out_head, c->head_dim, size_of(dtype)),
-                   bytes_of(c->pool, c->n_pages, 2ll * KVC_PAGE * c->head_dim * c->n_kv_heads, 1, 0, 2ll * KVC_PAGE * c->head_dim * c->n_kv_heads, size_of(c->dtype))) ||
-              meet(bytes_of(q->out, rows, q->out_row, q->n_heads, q->out_head, c->head_dim, size_of(dtype)), bytes_of(c->table, 4ll * c->batch * c->max_pages))))
+    if (q && meets_cache(bytes_of(q->out, rows, q->out_row, q->n_heads, q->out_head, c->head_dim, size_of(dtype)), c, false))
         return fail(RSD_EINVAL, "append: the out of q shares memory with the cache");
     Launches l(hip_stream);
     const KvcRows r = dev_rows(a, dev_cache(c));
@@ -277,6 +291,12 @@ extern "C" int rsd_kv_read(const rsd_kv_cache* c, const int32_t* seq, const int3
     if (rows < 1) return fail(RSD_EINVAL, "read: %d rows", rows);
     if (!aligned(k, 16) || !aligned(v, 16)) return fail(RSD_EINVAL, "read: k or v is not 16-byte aligned");
     if (2ll * rows * c->n_kv_heads > 1 << 26) return fail(RSD_EINVAL, "read: %d rows are too many", rows);
+    const int64_t bytes = (int64_t)rows * c->n_kv_heads * c->head_dim * (int64_t)size_of(c->dtype);
+    for (const void* p : {k, v}) {
+        const Bytes out = bytes_of(p, bytes);
+        if (meets_cache(out, c, false) || meet(out, bytes_of(seq, 4ll * rows)) || meet(out, bytes_of(slot, 4ll * rows)) || meet(bytes_of(k, bytes), bytes_of(v, bytes)))
+            return fail(RSD_EINVAL, "read: k or v shares memory with another array");
+    }
     const unsigned grid = (unsigned)ceil_div(2ll * rows * c->n_kv_heads * (c->head_dim / 8), 256);
     Launches l(hip_stream);
     auto run = [&](auto zero) {
@@ -296,7 +316,7 @@ extern "C" uint64_t rsd_kv_attention_workspace(const rsd_kv_cache* c, const rsd_
 extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
     if (int rc = check_attn(c, a)) return rc;
     if (!a->q || !a->out) return fail(RSD_EINVAL, "attention: null array");
-    if (!aligned(a->q, size_of(a->dtype)) || !aligned(a->out, size_of(a->dtype))) return fail(RSD_EINVAL, "attention: q or out is not aligned to its type");
+    if (!aligned(a->q, size_of(a->dtype)) || !aligned(a->out, size_of(a->dtype)) || !aligned(a->lse, 4)) return fail(RSD_EINVAL, "attention: q, out or lse is not aligned to its type");
     if (pieces_overlap(a->rows, a->out_row, a->n_heads, a->out_head, c->head_dim))
         return fail(RSD_EINVAL, "attention: rows of out overlap (strides %lld, %lld)", (long long)a->out_row, (long long)a->out_head);
     // a block has read its columns of q before it writes them, and no other block reads them
@@ -307,6 +327,13 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     const uint64_t need = p.bytes();
     if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
         return fail(RSD_EINVAL, "attention: the workspace holds %llu of %llu bytes, or is not 256-byte aligned", (unsigned long long)workspace_bytes, (unsigned long long)need);
+    const size_t size = size_of(a->dtype);
+    const Bytes q = bytes_of(a->q, a->rows, a->q_row, a->n_heads, a->q_head, c->head_dim, size), out = bytes_of(a->out, a->rows, a->out_row, a->n_heads, a->out_head, c->head_dim, size),
+                lse = bytes_of(a->lse, a->lse ? 4ll * a->rows * a->n_heads : 0), ws = bytes_of(need ? workspace : nullptr, need);
+    if (meet(out, lse) || meet(out, ws) || meet(lse, ws) || meet(q, lse) || meet(q, ws))
+        return fail(RSD_EINVAL, "attention: two of q, out, lse and the workspace share memory");
+    for (const Bytes& x : {out, lse, ws})
+        if (meets_cache(x, c, true) || (a->row_start && meet(x, bytes_of(a->row_start, 4ll * (c->batch + 1))))) return fail(RSD_EINVAL, "attention: out, lse or the workspace shares memory with the cache or row_start");
     KvcAttn k{};
     k.c = dev_cache(c);
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;

@@ -196,3 +196,33 @@ def test_binding_refuses_what_it_can_see(ops):
             ops.rsd_rope(rot, device="cpu")
     r = ops.rsd_rope(64, 1e4, scaling="parts", factor=4.0, original=64, device="cpu")
     assert r.freq.shape == (32,) and abs(r.magnitude - (0.1 * np.log(4.0) + 1)) < 1e-12
+
+
+def test_arrays_that_share_memory_are_refused(lib, ops):
+    big = dict(batch=1, max_pages=512, pool=1 << 30)
+    c, a = cache(ops, **big), dict(rows=1, max_kv=8192)
+    need = lib.rsd_kv_attention_workspace(C.byref(c), C.byref(attn(ops, **a)))
+    line = 8 * 64 * 2                                       # bytes of q, and of out
+    for kw, ws in ((dict(out=(1 << 30) + 2), WS), (dict(lse=(1 << 30) + 4), WS), (dict(lse=(1 << 21) + line - 4), WS), (dict(lse=(1 << 20) - 28), WS), (dict(out=4096), WS), (dict(lse=8192 - 28), WS),
+                   (dict(row_start=(1 << 21) - 4), WS), (dict(lse=(1 << 21) + 4096, row_start=(1 << 21) + 4096 + 28), WS), (dict(out=WS + need - 2), WS), (dict(q=WS + need - 2), WS), (dict(lse=WS), WS),
+                   (dict(), (1 << 30) - 256), (dict(), (1 << 21) - 256), (dict(lse=1 << 22 | 2), WS)):
+        assert lib.rsd_kv_attention(C.byref(c), C.byref(attn(ops, **a, **kw)), ws, 1 << 30, None) == -1, (kw, ws)
+        assert b"share" in lib.rsd_op_last_error() or b"aligned" in lib.rsd_op_last_error(), lib.rsd_op_last_error()
+    rows = 3 * 2 * 64 * 2                                   # bytes of k, and of v
+    for k, v, seq in ((1 << 20, (1 << 20) + rows - 16, 1 << 16), ((1 << 30) + 16, 1 << 20, 1 << 16), (1 << 20, 4096, 1 << 16), (1 << 20, 1 << 21, (1 << 20) + rows - 4)):
+        assert lib.rsd_kv_read(C.byref(c), seq, 1 << 17, 3, k, v, None) == -1 and b"shares" in lib.rsd_op_last_error()
+    k, q = heads(ops, n_heads=2, out=None), heads(ops, x=1 << 23, out=1 << 30)
+    assert lib.rsd_kv_append(C.byref(c), C.byref(k), 1 << 22, 128, 64, C.byref(q), 1 << 16, 1 << 17, None, None, 1e-6, 3, 1, None) == -1 and b"cache" in lib.rsd_op_last_error()
+
+
+@pytest.mark.parametrize("rows,batch,kv,heads_", [(1, 1, 1279, 12), (64, 64, 5120, 28), (2048, 1, 8192, 28), (1, 1, 1, 1), (130, 3, 4096, 16), (7, 2, 1 << 20, 64), (512, 512, 70, 8)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (1000, 4), (5, 1 << 20)])
+def test_workspaces_hold_the_parts(lib, ops, rows, batch, kv, heads_, window, sinks):
+    """A part of a row's head is head_dim sums and two numbers, and there are no more parts than the entries have chunks."""
+    for hd in (32, 64, 128):
+        for held, act in ((1, 1), (1, 0), (0, 0)):
+            c = cache(ops, batch=batch, max_pages=-(-kv // 16), n_kv_heads=1, head_dim=hd, dtype=held)
+            a = attn(ops, rows=rows, max_rows=max(rows // batch, 1), row_start=1 << 16, n_heads=heads_, max_kv=kv, window=window, sinks=sinks, dtype=act)
+            need = lib.rsd_kv_attention_workspace(C.byref(c), C.byref(a))
+            most = -(-kv // 16) * rows * heads_ * (4 * hd + 8) + 512
+            assert need % 256 == 0 and need <= most and (need == 0 or need >= 2 * rows * heads_ * (4 * hd + 8))
