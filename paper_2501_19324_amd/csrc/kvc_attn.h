@@ -35,7 +35,6 @@ struct KvcAttn {
     int lists, tiles, tile_cols;    // (sequence, kv head) pairs, tiles of columns of each
     int split, splits;      // chunks to a part, most parts
     bool by_length;         // the blocks of the longest sequences go first
-    bool turns;             // blocks are dealt forwards and backwards in turn
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
 };
@@ -108,15 +107,16 @@ __device__ __forceinline__ int kvc_by_length(const KvcAttn& a, int i) {
 
 // The work of block `id`: a list, that is a (sequence, kv head), a tile of its columns, and a part of their chunks; the last tile first, which sees most.  Blocks go to the eight XCDs in
 // turn: the tiles of a list, which read the same entries, are neighbours on one XCD and its L2.  Fewer than eight lists that divide eight share the XCDs out evenly.
-// An XCD deals its blocks to 32 CUs in turn; where all run at once (`turns`) every second round goes backwards, so that a CU whose first block is among the longest does not get the longest of every round
-// (16 sequences x 16 heads of 17 .. 128 rows and 300 .. 1025 entries, fp32: the second tile of most is empty, and the CUs that got first tiles in every round were busy twice as long).
+// An XCD deals its blocks to 32 CUs in turn; where lists have several tiles every second round goes backwards, so that a CU whose first block is among the longest does not get the longest of every
+// round: the last tiles of many lists are empty, and some CUs would get a first tile in every round (17 .. 128 rows, 16 sequences x 16 heads of 64, fp32: 45 us against 48 .. 51; 72B heads, 1024 .. 8192 entries:
+// 204 against 209).  With one tile the longest first alone does better (256 single tokens of 4096 .. 8192: 534 against 549).
 __host__ __device__ __forceinline__ int kvc_blocks(int lists, int tiles, int splits) {
     return (lists < 8 && 8 % lists == 0 ? (tiles + 8 / lists - 1) / (8 / lists) * 8 : (lists + 7) / 8 * 8 * tiles) * splits;
 }
 __device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, int& tile, int& part) {
     const int xcd = id & 7, all = gridDim.x >> 3;
     int at = id >> 3;
-    if (a.turns && (at & 32) && (at | 31) < all) at ^= 31;
+    if (a.tiles > 1 && (at & 32) && (at | 31) < all) at ^= 31;
     part = 0;
     if (a.splits > 1) {
         part = at / (all / a.splits);
@@ -437,7 +437,7 @@ __device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan
 // one chunk earlier still: one set of registers for each instead of two, and eight waves on a CU.
 // Bound by bytes: 256 sequences of 4096 .. 8192 entries, 7B heads, bf16 (3.24 GB): 537 us, 6.0 TB/s, what a read alone reaches (572 with two whole chunks of registers, 558 with four waves to a
 // block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 7 .. 9 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
-// rows: 49 us, matrix instructions in fp32 busy 40 % of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
+// rows: 45 us, matrix instructions in fp32 busy 45 % of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
 template <typename T, typename C, int HD>
 __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;

@@ -147,7 +147,7 @@ template <typename T, typename C> void append_run(const RowArgs& a, const KvcRow
 
 struct AttnPlan {
     int lists, tiles, tile_cols, ch, waves, split, splits;
-    bool many, by_length, turns;
+    bool many, by_length;
     uint64_t o_bytes, ml_bytes;
     uint64_t bytes() const { return o_bytes + ml_bytes; }
 };
@@ -156,7 +156,7 @@ int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >=
 
 // Which kernel, which tiles, how the entries are split: by the sizes that the host knows.  Measured with 28 heads over 4 of 128, bf16, where nothing else is said, in us:
 //  - the kernel of few columns takes up to two tiles of 16 (21 columns, 4 sequences of 2048 entries: 13.2, the other 15.8; 64 of 128 .. 2048, fp32 activations: 32 and 39; 64 of 128 .. 5120: 71 and 70),
-//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 49 and 63).
+//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 46 and 63).
 //  - 128 columns to a block instead of 64 where rows see 768 entries and more before their own (2048 rows of 8192: 223 and 280, 16 x 128 of 1024: 48 and 54; against that 2048 of 2048: 58 and 50,
 //    64 x 128 of 300: 87 and 74) and there are 384 such blocks with their parts (512 rows of 8192: 84 and 92; against that 4 x 128 of 2048: 42 and 36, 256 of 8192: 56 and 54).
 //  - a part's sums are 4 bytes an element written and read, beside the join's launch.  Many columns are split up to 512 blocks (16 x 128 of 1024: 50 whole, 71 in two; 256 x 8 of 2048: 197 whole, 244 in two;
@@ -197,7 +197,6 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     p.split = (int)ceil_div(chunks, std::max<int64_t>(1, parts));
     p.splits = (int)ceil_div(chunks, p.split);
     p.by_length = c->batch > 1 && base * p.splits * p.waves > 2048;
-    p.turns = p.many && base * p.splits * p.waves <= (c->head_dim == 128 ? 2048 : 4096);
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -348,7 +347,7 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
     k.max_kv = std::min(a->max_kv, c->max_pages * KVC_PAGE), k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
-    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.turns = p.turns;
+    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length;
     k.part_o = static_cast<float*>(workspace);
     k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.o_bytes);
     Launches l(hip_stream);
