@@ -35,6 +35,7 @@ struct KvcAttn {
     int lists, tiles, tile_cols;    // (sequence, kv head) pairs, tiles of columns of each
     int split, splits;      // chunks to a part, most parts
     bool by_length;         // the blocks of the longest sequences go first
+    bool packed;            // blocks without columns lie behind the others
     float* part_o;          // [rows][heads][splits][hd], unnormalised
     float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
 };
@@ -105,33 +106,86 @@ __device__ __forceinline__ int kvc_by_length(const KvcAttn& a, int i) {
     return first + __builtin_ctzll(__ballot(((among >> lane) & 1) && before == rank));
 }
 
+// The place of a lane's sequence in the same order, among the up to 64 sequences of a wave's lanes that are `there` (the others keep their lanes, behind)
+__device__ __forceinline__ int kvc_rank(bool there, int n, int max_kv) {
+    const int lane = threadIdx.x & 63, key = n >> max(24 - __clz(max_kv), 0);
+    const uint64_t all = __ballot(there);
+    uint64_t among = all;
+    int rank = 0;
+#pragma unroll
+    for (int bit = 7; bit >= 0; --bit) {
+        const bool mine = (key >> bit) & 1;
+        const uint64_t have = __ballot(mine) & all;
+        rank += mine ? 0 : __popcll(among & have);
+        among &= mine ? have : ~have;
+    }
+    return there ? rank + __popcll(among & ((1ull << lane) - 1)) : lane;
+}
+
 // The work of block `id`: a list, that is a (sequence, kv head), a tile of its columns, and a part of their chunks; the last tile first, which sees most.  Blocks go to the eight XCDs in
 // turn: the tiles of a list, which read the same entries, are neighbours on one XCD and its L2.  Fewer than eight lists that divide eight share the XCDs out evenly.
 // An XCD deals its blocks to 32 CUs in turn; where lists have several tiles every second round goes backwards, so that a CU whose first block is among the longest does not get the longest of every
-// round: the last tiles of many lists are empty, and some CUs would get a first tile in every round (17 .. 128 rows, 16 sequences x 16 heads of 64, fp32: 45 us against 48 .. 51; 72B heads, 1024 .. 8192 entries:
-// 204 against 209).  With one tile the longest first alone does better (256 single tokens of 4096 .. 8192: 534 against 549).
+// round (17 .. 128 rows, 16 sequences x 16 heads of 64, fp32: 45 us against 48 .. 51; 72B heads, 1024 .. 8192 entries: 204 against 209).  With one tile the longest first alone does better (256 single tokens of
+// 4096 .. 8192: 534 against 549).  Blocks without columns, of sequences with fewer rows than others, would upset the rounds: `packed` counts the tiles that there are, sequence by sequence in the order of their lengths.
 __host__ __device__ __forceinline__ int kvc_blocks(int lists, int tiles, int splits) {
     return (lists < 8 && 8 % lists == 0 ? (tiles + 8 / lists - 1) / (8 / lists) * 8 : (lists + 7) / 8 * 8 * tiles) * splits;
 }
-__device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, int& list, int& tile, int& part) {
+struct KvcWork {
+    int b, head, tile, part;
+    int r0, count, n;       // of the sequence: first row, rows, entries
+};
+__device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, KvcWork& w) {
     const int xcd = id & 7, all = gridDim.x >> 3;
     int at = id >> 3;
     if (a.tiles > 1 && (at & 32) && (at | 31) < all) at ^= 31;
-    part = 0;
+    w.part = 0;
     if (a.splits > 1) {
-        part = at / (all / a.splits);
-        at -= part * (all / a.splits);
+        w.part = at / (all / a.splits);
+        at -= w.part * (all / a.splits);
     }
+    if (a.packed) {                                         // a lane to a sequence
+        const int lane = threadIdx.x & 63;
+        int r0 = 0, count = 0, n = 0;
+        if (lane < a.c.batch) kvc_rows(a, lane, r0, count, n);
+        const int sees = a.window && n - a.window - count > a.sinks ? a.window + count + a.sinks : n;
+        const int rank = kvc_rank(lane < a.c.batch, sees, a.max_kv);
+        const int from = __builtin_amdgcn_ds_permute(rank * 4, lane);       // lane r: the sequence that is r-th
+        const int tiles = __shfl((count * (int)a.group.d + a.tile_cols - 1) >> (31 - __clz(a.tile_cols)), from);
+        auto before = [&](int r) { return (r * a.c.hkv - xcd + 7) >> 3; };  // lists of this XCD before the r-th sequence's
+        const int blocks = lane < a.c.batch ? (before(lane + 1) - before(lane)) * tiles : 0;
+        int sum = blocks;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int other = __shfl_up(sum, d);
+            sum += lane >= d ? other : 0;
+        }
+        const int r = __popcll(__ballot(sum <= at));
+        if (r >= a.c.batch) return false;
+        const int t = __builtin_amdgcn_readlane(tiles, r), start = at - (__builtin_amdgcn_readlane(sum, r) - __builtin_amdgcn_readlane(blocks, r)), which = start / t;
+        w.b = __builtin_amdgcn_readlane(from, r);
+        w.tile = t - 1 - (start - which * t);
+        w.head = (before(r) + which) * 8 + xcd - r * a.c.hkv;
+        w.r0 = __builtin_amdgcn_readlane(r0, w.b);
+        w.count = __builtin_amdgcn_readlane(count, w.b);
+        w.n = __builtin_amdgcn_readlane(n, w.b);
+        return true;
+    }
+    int list;
     if (a.lists < 8 && 8 % a.lists == 0) {
         list = xcd % a.lists;
-        tile = at * (8 / a.lists) + xcd / a.lists;
+        w.tile = at * (8 / a.lists) + xcd / a.lists;
     } else {
         const int eight = a.by_tiles(at);
         list = eight * 8 + xcd;
-        tile = at - eight * a.tiles;
+        w.tile = at - eight * a.tiles;
     }
-    tile = a.tiles - 1 - tile;
-    return list < a.lists && tile >= 0;
+    w.tile = a.tiles - 1 - w.tile;
+    if (list >= a.lists || w.tile < 0) return false;
+    const int i = a.by_heads(list);
+    w.head = list - i * a.c.hkv;
+    w.b = kvc_by_length(a, i);
+    kvc_rows(a, w.b, w.r0, w.count, w.n);
+    return true;
 }
 
 // Activations of type T over a cache of type C.
@@ -437,7 +491,7 @@ __device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan
 // one chunk earlier still: one set of registers for each instead of two, and eight waves on a CU.
 // Bound by bytes: 256 sequences of 4096 .. 8192 entries, 7B heads, bf16 (3.24 GB): 537 us, 6.0 TB/s, what a read alone reaches (572 with two whole chunks of registers, 558 with four waves to a
 // block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 7 .. 9 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
-// rows: 45 us, matrix instructions in fp32 busy 42 % of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
+// rows: 43 us, matrix instructions in fp32 busy half of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
 template <typename T, typename C, int HD>
 __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;
@@ -445,12 +499,9 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     __shared__ __align__(16) float lds_o[WAVES][NB][64][4];
     __shared__ float lds_ml[WAVES][2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, quad = lane >> 4;
-    int list, tile, part;
-    if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
-    const int at = a.by_heads(list), head = list - at * a.c.hkv, b = kvc_by_length(a, at), col0 = tile * 16, col = col0 + (lane & 15);
-    int r0, count, n;
-    kvc_rows(a, b, r0, count, n);
-    const int cols = count * (int)a.group.d;
+    KvcWork work;
+    if (!kvc_work(a, blockIdx.x, work)) return;
+    const int b = work.b, head = work.head, part = work.part, r0 = work.r0, count = work.count, n = work.n, cols = count * (int)a.group.d, col0 = work.tile * 16, col = col0 + (lane & 15);
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, M::CH, count, n, col0, min(cols, col0 + 16));
     const int parts = kvc_parts(a, span);
@@ -540,7 +591,7 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
 // are busy 39 % of the time, vector instructions about as long (per 32 entries and 16 columns 16 of the one and 50 of the other, 8 of them exponentials); two waves on a SIMD, of different blocks,
 // overlap them in part.  Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  Neither priorities of waves nor eight-byte reads of the values
 // (no moves, twice the reads) changed the time.
-// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 112 us, 0.82 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
+// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 103 us, 0.90 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
 // 256 of 2048 entries, 8 rows: 198 us, 5.6 TB/s.
 template <typename T, typename C, int HD, int NT> struct KvcMany {
     static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);
@@ -556,12 +607,9 @@ __global__ __launch_bounds__(256, 2) void kvc_attn_many_kernel(KvcAttn a) {
     static_assert(2 * N % OWN == 0, "a wave's share lies in one page");
     __shared__ u32x4_t ring[R][PAGES][2 * N][64];           // keys, then values of each page
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
-    int list, tile, part;
-    if (!kvc_work(a, blockIdx.x, list, tile, part)) return;
-    const int at = a.by_heads(list), head = list - at * a.c.hkv, b = kvc_by_length(a, at), col0 = tile * COLS;
-    int r0, count, n;
-    kvc_rows(a, b, r0, count, n);
-    const int cols = count * (int)a.group.d;
+    KvcWork work;
+    if (!kvc_work(a, blockIdx.x, work)) return;
+    const int b = work.b, head = work.head, part = work.part, r0 = work.r0, count = work.count, n = work.n, cols = count * (int)a.group.d, col0 = work.tile * COLS;
     if (col0 >= cols) return;
     const KvcSpan span = kvc_span(a, CH, count, n, col0, min(cols, col0 + COLS));
     const int parts = kvc_parts(a, span);

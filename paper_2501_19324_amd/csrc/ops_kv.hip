@@ -147,7 +147,7 @@ template <typename T, typename C> void append_run(const RowArgs& a, const KvcRow
 
 struct AttnPlan {
     int lists, tiles, tile_cols, ch, waves, split, splits;
-    bool many, by_length;
+    bool many, by_length, packed;
     uint64_t o_bytes, ml_bytes;
     uint64_t bytes() const { return o_bytes + ml_bytes; }
 };
@@ -163,6 +163,8 @@ int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >=
 //    256 of 8192: 166 whole, 57 in eight), up to 48 columns for 768 (64 x 5 of 128 .. 5120: 89 whole, 74 in three, 85 in four; where all have 5120 the three cost: 116 whole, 140), no part under 512 or 1024 entries.
 //    Few columns for 256 blocks, no part under 768 (one sequence of 1279: 9.9 whole, 10.8 in two; of 2500: 14.4 whole, 11.9 in three; of 8000: 39 whole, 15.7 in ten; 16 of 8000: 67 whole, 46 .. 49 in two to four).
 //  - few columns: eight waves up to 256 blocks (one sequence of 896 .. 1279: 9.8, 11.1 with four) and for long lists (256 of 4096 .. 8192: 535 and 558), else four (window 1024: 101, 105 with eight; heads of 64: 49 and 54).
+//  - where sequences have unlike numbers of rows, blocks without columns go behind the others (16 of 17 .. 128 rows, 72B heads, fp32, window 1000: 103 and 111; 32 of 5 .. 128 rows of 300 .. 4096: 102 and 110;
+//    16 x 16 heads of 64, fp32: 43 and 46; where all have the same it costs a block's start 0.5 us: 64 x 128 of 300: 80 and 76).
 //  - the longest lists first, from the point where the blocks are more than the card holds at once (64 x 5 of 128 .. 5120: 75 and 84; 256 of 4096 .. 8192: 534 and 555).
 AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     AttnPlan p{};
@@ -197,6 +199,7 @@ AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     p.split = (int)ceil_div(chunks, std::max<int64_t>(1, parts));
     p.splits = (int)ceil_div(chunks, p.split);
     p.by_length = c->batch > 1 && base * p.splits * p.waves > 2048;
+    p.packed = p.tiles > 1 && a->rows < (int64_t)c->batch * a->max_rows && c->batch <= 64 && p.lists >= 8;
     const uint64_t lines = (uint64_t)a->rows * a->n_heads;
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
@@ -347,7 +350,7 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
     k.max_kv = std::min(a->max_kv, c->max_pages * KVC_PAGE), k.window = window_of(c, a), k.sinks = std::min(a->sinks, c->max_pages * KVC_PAGE);
-    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length;
+    k.lists = p.lists, k.ch = p.ch, k.tiles = p.tiles, k.tile_cols = p.tile_cols, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.packed = p.packed;
     k.part_o = static_cast<float*>(workspace);
     k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.o_bytes);
     Launches l(hip_stream);

@@ -88,6 +88,20 @@ def test_many_sequences_longest_first(torch, R, act, held, batch, heads, hkv, mo
     check_attention(torch, R, rng, lens.tolist(), m.tolist(), heads, hkv, 32, act, held, single=rows == 1)
 
 
+@pytest.mark.parametrize("batch,heads,hkv,most", [(9, 5, 1, 40), (64, 2, 1, 90), (33, 6, 3, 30), (5, 16, 8, 60), (13, 5, 5, 70), (65, 2, 1, 90), (8, 17, 17, 20)], ids=str)
+@pytest.mark.parametrize("act,held", PAIRS)
+def test_sequences_with_unlike_numbers_of_rows(torch, R, act, held, batch, heads, hkv, most):
+    """Most tiles of columns have no row; none at all, one row, all rows, more rows than entries; long ones in parts."""
+    rng = np.random.default_rng(batch * hkv)
+    m = rng.integers(0, 9, batch)
+    m[1], m[-1] = most, 0
+    lens = rng.integers(0, 100, batch)
+    lens[0] = 1300 if batch < 10 else 200
+    lens[2:5] = lens[1]
+    check_attention(torch, R, rng, lens.tolist(), m.tolist(), heads, hkv, 32, act, held, tight=batch % 2 == 0)
+    check_attention(torch, R, rng, lens.tolist(), m.tolist(), heads, hkv, 64, act, held, 24, 5, missing=[(0, 3)])
+
+
 @pytest.mark.parametrize("heads,rows", [(64, 1), (64, 3), (96, 5), (17, 2), (129, 1)])
 @pytest.mark.parametrize("act,held", PAIRS)
 def test_large_groups(torch, R, act, held, heads, rows):
