@@ -491,7 +491,7 @@ __device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan
 // one chunk earlier still: one set of registers for each instead of two, and eight waves on a CU.
 // Bound by bytes: 256 sequences of 4096 .. 8192 entries, 7B heads, bf16 (3.24 GB): 537 us, 6.0 TB/s, what a read alone reaches (572 with two whole chunks of registers, 558 with four waves to a
 // block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 7 .. 9 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
-// rows: 43 us, matrix instructions in fp32 busy half of it; 63 with the kernel of many columns, whose waves have no columns in a last tile.
+// rows: 43 us, matrix instructions in fp32 at 68 TFLOP/s; 63 with the kernel of many columns, whose waves have no columns in a last tile.
 template <typename T, typename C, int HD>
 __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
     typedef KvcMath<T, C, HD> M;
@@ -591,7 +591,7 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
 // are busy 39 % of the time, vector instructions about as long (per 32 entries and 16 columns 16 of the one and 50 of the other, 8 of them exponentials); two waves on a SIMD, of different blocks,
 // overlap them in part.  Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  Neither priorities of waves nor eight-byte reads of the values
 // (no moves, twice the reads) changed the time.
-// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 103 us, 0.90 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
+// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 106 us, 0.87 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
 // 256 of 2048 entries, 8 rows: 198 us, 5.6 TB/s.
 template <typename T, typename C, int HD, int NT> struct KvcMany {
     static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);

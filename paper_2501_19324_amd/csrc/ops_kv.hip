@@ -156,7 +156,7 @@ int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >=
 
 // Which kernel, which tiles, how the entries are split: by the sizes that the host knows.  Measured with 28 heads over 4 of 128, bf16, where nothing else is said, in us:
 //  - the kernel of few columns takes up to two tiles of 16 (21 columns, 4 sequences of 2048 entries: 13.2, the other 15.8; 64 of 128 .. 2048, fp32 activations: 32 and 39; 64 of 128 .. 5120: 71 and 70),
-//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 46 and 63).
+//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 43 and 63).
 //  - 128 columns to a block instead of 64 where rows see 768 entries and more before their own (2048 rows of 8192: 223 and 280, 16 x 128 of 1024: 48 and 54; against that 2048 of 2048: 58 and 50,
 //    64 x 128 of 300: 87 and 74) and there are 384 such blocks with their parts (512 rows of 8192: 84 and 92; against that 4 x 128 of 2048: 42 and 36, 256 of 8192: 56 and 54).
 //  - a part's sums are 4 bytes an element written and read, beside the join's launch.  Many columns are split up to 512 blocks (16 x 128 of 1024: 50 whole, 71 in two; 256 x 8 of 2048: 197 whole, 244 in two;

@@ -131,6 +131,31 @@ def test_addresses_aligned_to_their_type_only(torch, R, act, held, hd):
 
 
 @pytest.mark.parametrize("act,held", PAIRS)
+@pytest.mark.parametrize("lens,rows", [([300, 40], [1, 1]), ([300, 60], [7, 3]), ([300, 150], [90, 20])], ids=str)
+def test_infinite_queries_stay_in_their_rows(torch, R, act, held, lens, rows):
+    """A result is off by at most 2^-8 sum p|v| for bf16 weights, 2^-8 of itself for its rounding, and what its scores err by: with 300 entries, |scale q k| sums of at most 60 and
+    heads of 64, 4 * 2 * 112 * 2^-24 * 60 < 2^-8 of sum p|v|.  Two results without an infinity beside them differ by at most twice that, and sum p|v| <= max |v|."""
+    rng = np.random.default_rng(8)
+    hd, hkv, heads, total = 64, 2, 6, sum(rows)
+    c, _ = make_cache(torch, R, rng, lens, hkv, hd, held)
+    most = float(c.pool[:, :, 1].abs().max())
+    q, _ = dev(torch, rng.normal(size=(total, heads, hd)), kind(torch, act))
+    assert float(q.abs().max()) * float(c.pool[:, :, 0].abs().max()) * 0.04 * hd < 60
+    kw = dict(row_start=ints(torch, np.concatenate([[0], np.cumsum(rows)])), max_rows=max(rows), want_lse=True)
+    want, lse = (host(x) for x in R.rsd_kv_attention(c, q, 0.04, **kw))
+    at = rng.permutation(total * heads)[:max(total * heads // 5, 3)]
+    mark = np.zeros(total * heads, bool)
+    mark[at] = True
+    mark = mark.reshape(total, heads)
+    bad = q.clone()
+    for i, x in enumerate(at):
+        bad[x // heads, x % heads, int(rng.integers(hd))] = (np.nan, np.inf, -np.inf)[i % 3]
+    got, lse2 = (host(x) for x in R.rsd_kv_attention(c, bad, 0.04, **kw))
+    assert not np.isfinite(got[mark]).all(-1).any() and np.isfinite(got[~mark]).all()
+    assert (np.abs(got[~mark] - want[~mark]) <= (2 ** -5 if act == "bf16" else 2 ** -7) * most).all() and (np.abs(lse2[~mark] - lse[~mark]) <= 2 ** -7).all()
+
+
+@pytest.mark.parametrize("act,held", PAIRS)
 def test_lengths_that_the_device_cuts(torch, R, act, held):
     rng = np.random.default_rng(4)
     hd, hkv, heads, lens = 64, 2, 6, [200, 64, 96]
