@@ -578,7 +578,7 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
         kvc_copy<COUNT - 4>(lds + 4096, lane16, base + 4096);
     } else if constexpr (COUNT == 4)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+                     "global_load_lds_dwordx4 %1, %2 offset:0xc00" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
     else if constexpr (COUNT == 2)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
