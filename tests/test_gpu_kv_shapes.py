@@ -263,3 +263,20 @@ def test_values_of_neighbours_that_are_no_neighbours(torch, R, act, held):
     ref.fill(want, table, size, hd, seq, slot, to(k64), to(v64))
     R.rsd_kv_append(c, k, v, ints(torch, seq), ints(torch, slot))
     assert np.array_equal(host(c.pool), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_keys_without_queries(torch, R, dtype):
+    """The entry point takes keys alone, which the binding calls queries."""
+    from paper_2501_19324_amd import ops
+    rng = np.random.default_rng(3)
+    rows, heads, hd = 37, 3, 64
+    x, _ = dev(torch, rng.normal(size=(rows, heads, hd)), kind(torch, dtype))
+    w, _ = dev(torch, 1 + 0.3 * rng.normal(size=hd), kind(torch, dtype))
+    position, rope = ints(torch, rng.integers(0, 5000, rows)), R.rsd_rope(hd)
+    want, _ = R.rsd_qk_rope(x, None, position, rope, q_weight=w)
+    out = torch.empty_like(x)
+    k = ops._Heads(x.data_ptr(), out.data_ptr(), w.data_ptr(), heads * hd, hd, heads * hd, hd, heads)
+    turn = ops._Rope(rope.freq.data_ptr(), hd, 0, 1.0)
+    assert ops._load().rsd_qk_rope(None, bytes(k), position.data_ptr(), bytes(turn), 1e-6, rows, hd, int(dtype == "bf16"), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(bits(torch, out), bits(torch, want))
