@@ -2,7 +2,7 @@
 //
 // A column is a (row, head of the group) of one (sequence, kv head): column c is row c / group, head c % group.  Scores are S^T[token][column] = K Q^T, what
 // is gathered is O^T[dim][column] += V^T P^T, both in tiles of 16 x 16 whose accumulators hold row 4 (lane / 16) + i, column lane % 16: a column's probabilities leave the first product in
-// the lanes in which the second one wants them, and only the maximum and the sum cross lanes.  One pass over the entries with a running maximum (base 2) and sum in fp32.
+// the lanes in which the second one wants them, and only the maximum and the sum cross lanes.  One pass over the entries with a running maximum and sum in fp32.
 #pragma once
 #include "kvc.h"
 
@@ -22,10 +22,11 @@ struct KvcAttn {
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
     int total_rows, max_rows, heads;
     KvcDivisor group, by_heads, by_tiles;    // heads of a kv head; by the kv heads and by the tiles
-    float factor2;          // |scale| * log2(e); never 0 or NaN
-    float inverse2;         // 1 / factor2
+    float factor;           // |scale|; 1 where q is multiplied by it
+    float factor2;          // the same * log2(e): finite, never 0
+    float slack;            // 8 / factor2, finite: a score may pass the running maximum by so much
     bool negative;          // scale < 0: q changes its sign instead
-    bool plain;             // scale is 0 or NaN: q is multiplied by it and factor2 is log2(e), so that -inf means "not seen" and nothing else
+    bool plain;             // scale is 0, infinite or NaN: q is multiplied by it, so that -inf means "not seen" and nothing else
     float scale;
     void* out;
     int64_t o_row, o_head;
@@ -37,7 +38,7 @@ struct KvcAttn {
     bool by_length;         // the blocks of the longest sequences go first
     bool packed;            // blocks without columns lie behind the others
     float* part_o;          // [rows][heads][splits][hd], unnormalised
-    float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
+    float2* part_ml;        // [rows][heads][splits]: maximum, sum
 };
 // rows of sequence b: the first one and how many; entries it has
 __device__ __forceinline__ void kvc_rows(const KvcAttn& a, int b, int& r0, int& count, int& n) {
@@ -409,32 +410,38 @@ template <typename C, int HD, int PAGES> __device__ __forceinline__ void kvc_pag
     }
 }
 
-// The running state of a lane's column.  `top`, in units of the exponent (base 2), is the same in its four lanes, `sum` each lane's own.
+// The weight 2^(factor2 (s - top)) of a score, or of what was gathered under another maximum.  The difference is formed first and is 0 at the maximum.  (factor2 s - fl(factor2 top) in one
+// multiply-add keeps the rounding of the second product, half a step of it: beyond 2^31 that is 128 and more, and the weights of the largest scores themselves were 0 or infinite.)
+__device__ __forceinline__ float kvc_weight(const KvcAttn& a, float s, float base) { return __builtin_amdgcn_exp2f((s - base) * a.factor2); }
+__device__ __forceinline__ float kvc_base(float top) { return top == -INFINITY ? 0.f : top; }
+__device__ __forceinline__ float kvc_lse(const KvcAttn& a, float top, float total) { return total == 0.f ? -INFINITY : kvc_base(top) * a.factor + logf(total); }
+
+// The running state of a lane's column.  `top`, the largest score q.K, is the same in its four lanes, `sum` each lane's own.
 struct KvcRun {
     float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;      // base: top, or 0 where that is -inf; limit: of scores that need no new maximum
 };
-// Scores of a chunk -> probabilities in their place; the maximum moves, and what was gathered is scaled, only where a score passes it by 2^8 (probabilities up to 2^8 lose nothing
-// in 32 bits, nor in bf16): seldom after the first chunks, so the lanes of a column exchange their maxima there and nowhere else.  factor2 > 0.
+// Scores of a chunk -> probabilities in their place; the maximum moves, and what was gathered is scaled, only where a score passes it by so much that a probability would pass 2^8 (up to
+// there they lose nothing in 32 bits, nor in bf16): seldom after the first chunks, so the lanes of a column exchange their maxima there and nowhere else.  factor2 > 0.
 template <int PAGES, int NB>
 __device__ __forceinline__ void kvc_softmax(f32x4_t s[PAGES], const KvcAttn& a, KvcRun& r, f32x4_t o[NB]) {
     float best = s[0][0];
 #pragma unroll
     for (int i = 1; i < 4 * PAGES; ++i) best = fmaxf(best, s[i / 4][i % 4]);
     if (__any(best > r.limit)) {
-        const float top = fmaxf(r.top, rows4_max(best) * a.factor2), base = top == -INFINITY ? 0.f : top;
-        const float scale = __builtin_amdgcn_exp2f(r.top - base);
+        const float top = fmaxf(r.top, rows4_max(best)), base = kvc_base(top);
+        const float scale = kvc_weight(a, r.top, base);
         r.sum *= scale;
 #pragma unroll
         for (int d = 0; d < NB; ++d) o[d] *= scale;
         r.top = top;
         r.base = base;
-        r.limit = (top + 8.f) * a.inverse2;
+        r.limit = top + a.slack;
     }
 #pragma unroll
     for (int p = 0; p < PAGES; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[p][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], a.factor2, -r.base));
+            s[p][i] = kvc_weight(a, s[p][i], r.base);
             r.sum += s[p][i];
         }
 }
@@ -459,7 +466,7 @@ __device__ __forceinline__ void kvc_finish(const KvcAttn& a, int r0, int head, i
         if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst + i * 16) = u32x2_t{f2bf2(x[0], x[1]), f2bf2(x[2], x[3])};
         else *reinterpret_cast<f32x4_any_t*>(dst + i * 16) = x;
     }
-    if (d == 0 && quad == 0 && a.lse) a.lse[line] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
+    if (d == 0 && quad == 0 && a.lse) a.lse[line] = kvc_lse(a, top, total);
 }
 // Scores that a column must not see, where a chunk is not seen whole by all of them
 template <typename M, int NT> __device__ __forceinline__ void kvc_mask_scores(const KvcColumn see[NT], int slot0, int there, f32x4_t s[NT][M::PAGES]) {
@@ -560,10 +567,10 @@ __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
         const int c = lane & 15;
         float best = -INFINITY, total = 0.f;
         for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][c]);
-        const float base = best == -INFINITY ? 0.f : best;
+        const float base = kvc_base(best);
         f32x4_t acc = {};
         for (int w = 0; w < waves; ++w) {
-            const float scale = __builtin_amdgcn_exp2f(lds_ml[w][0][c] - base);
+            const float scale = kvc_weight(a, lds_ml[w][0][c], base);
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
@@ -741,13 +748,13 @@ __global__ __launch_bounds__(256) void kvc_join_kernel(KvcAttn a) {
     float best = -INFINITY;
     for (int s = l; s < parts; s += 16) best = fmaxf(best, a.part_ml[at + s].x);
     best = row16_max(best);
-    const float base = best == -INFINITY ? 0.f : best;
+    const float base = kvc_base(best);
     float total = 0.f, acc[N] = {};
     for (int s0 = 0; s0 < parts; s0 += 16) {
         float scale = 0.f;
         if (s0 + l < parts) {
             const float2 ml = a.part_ml[at + s0 + l];
-            scale = __builtin_amdgcn_exp2f(ml.x - base);
+            scale = kvc_weight(a, ml.x, base);
             total += scale * ml.y;
         }
         const int m = min(16, parts - s0);
@@ -763,5 +770,5 @@ __global__ __launch_bounds__(256) void kvc_join_kernel(KvcAttn a) {
     T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + l * N;
 #pragma unroll
     for (int i = 0; i < N; ++i) st1(dst + i, acc[i] * inv);
-    if (l == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
+    if (l == 0 && a.lse) a.lse[row * a.heads + qh] = kvc_lse(a, best, total);
 }

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "rsd_ops.h"
@@ -343,9 +344,10 @@ extern "C" int rsd_kv_attention(const rsd_kv_cache* c, const rsd_kv_attn* a, voi
     auto divisor = [](int d) { return KvcDivisor{(uint32_t)d, d == 1 ? 0xFFFFFFFFu : (uint32_t)((1ull << 32) / (uint64_t)d + 1)}; };
     k.group = divisor(a->n_heads / c->n_kv_heads), k.by_heads = divisor(c->n_kv_heads), k.by_tiles = divisor(p.tiles);
     k.scale = a->scale;
-    k.plain = !(std::fabs(a->scale) > 0.f);
-    k.factor2 = k.plain ? 1.4426950408889634f : (float)(std::fabs((double)a->scale) * 1.4426950408889634);
-    k.inverse2 = 1.f / k.factor2;
+    k.plain = !(std::fabs(a->scale) > 0.f) || std::isinf(a->scale);
+    k.factor = k.plain ? 1.f : std::fabs(a->scale);
+    k.factor2 = (float)std::min(k.factor * 1.4426950408889634, (double)FLT_MAX);
+    k.slack = (float)std::min(8. / k.factor2, (double)FLT_MAX);
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
