@@ -186,18 +186,20 @@ struct Kv4Attn {
     int64_t q_row, q_head;
     const int* row_start;   // [batch + 1]; null: row b is sequence b's
     int total_rows, max_rows, heads, group;
-    float factor2;          // |scale| * log2(e): exponents are taken to the base 2; never 0 or NaN
+    float factor;           // |scale|; 1 where q is multiplied by it
+    float factor2;          // the same * log2(e): exponents are taken to the base 2; finite, never 0
+    float slack;            // 8 / factor2, finite: a score may pass the running maximum by so much
     bool negative;          // scale < 0: q changes its sign instead
-    bool plain;             // scale is 0 or NaN: q is multiplied by it and factor2 is 1, so that -inf means "not seen" and nothing else (0 times an infinite score is NaN)
+    bool plain;             // scale is 0, infinite or NaN: q is multiplied by it, so that -inf means "not seen" and nothing else (0 times an infinite score is NaN)
     float scale;
     void* out;
     int64_t o_row, o_head;
     float* lse;             // [rows][heads] or null
-    float* lse2;            // kv4_weight_log of every row and head, for the kernels that add the weights afterwards (KV4_LOGS), or null
+    float2* dealt;          // kv4_dealt of every row and head, for the kernels that add the weights afterwards (KV4_LOGS), or null
     int max_kv, tiles, split, splits, hd;
     bool by_length;         // the blocks of the longest sequences go first
     float* part_o;          // [rows][heads][splits][hd], unnormalised
-    float2* part_ml;        // [rows][heads][splits]: maximum (base 2), sum
+    float2* part_ml;        // [rows][heads][splits]: maximum, sum
     Kv4Book book;
     int w_cols, w_groups;   // attention weights: the columns are dealt in groups of w_cols, at most w_groups of them
     int64_t w_slots;        // of a part below
@@ -367,9 +369,15 @@ __device__ __forceinline__ void kv4_nan_values(Kv4Vals<HD>& v, int slot0, int sa
         for (int g = 0; g < HD / 32; ++g) v.scale[p][g] &= ~((marks[p][g] >> 7) * 255u);
 }
 
-// The logarithm, to the base 2, of the sum that a column's weights are divided by.  A column that deals out nothing, because it sees nothing or all its scores are
-// -inf, has +inf: its weights are 0 (with -inf, the logarithm of its sum, those of the scores -inf were NaN).
-__device__ __forceinline__ float kv4_weight_log(float top, float total) { return total == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top) + log2f(total); }
+// The weight 2^(factor2 (s - top)) of a score, or of what was gathered under another maximum.  The difference is formed first and is 0 at the maximum.  (factor2 s - fl(factor2 top) in one
+// multiply-add keeps the rounding of the second product: beyond 2^31 that is 128 and more, and the weights of the largest scores themselves were 0 or infinite.)
+__device__ __forceinline__ float kv4_weight(const Kv4Attn& a, float s, float base) { return __builtin_amdgcn_exp2f((s - base) * a.factor2); }
+__device__ __forceinline__ float kv4_base(float top) { return top == -INFINITY ? 0.f : top; }
+__device__ __forceinline__ float kv4_lse(const Kv4Attn& a, float top, float total) { return total == 0.f ? -INFINITY : kv4_base(top) * a.factor + logf(total); }
+// What a column's weights are taken with: its maximum, and the logarithm to the base 2 of the sum that they are divided by (in one number, a large maximum would swallow the logarithm).  A column
+// that deals out nothing, because it sees nothing or all its scores are -inf, has +inf: its weights are 0 (with -inf, the logarithm of its sum, those of the scores -inf were NaN).
+__device__ __forceinline__ float2 kv4_dealt(float top, float total) { return make_float2(kv4_base(top), total == 0.f ? INFINITY : log2f(total)); }
+__device__ __forceinline__ float kv4_dealt_weight(const Kv4Attn& a, float s, float2 dealt) { return __builtin_amdgcn_exp2f(__builtin_fmaf(s - dealt.x, a.factor2, -dealt.y)); }
 // what a column has gathered, for the join: rows (dims) 4 quad + i of every block d of 16 dims, column lane % 16
 template <typename T, int WEIGHTS>
 __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh, int dim, bool first, f32x4_t acc, float top, float total, int parts) {
@@ -383,14 +391,14 @@ __device__ __forceinline__ void kv4_finish(const Kv4Attn& a, int64_t row, int qh
     T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + dim;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any_t*>(dst) = u32x2_t{f2bf2(acc[0] * inv, acc[1] * inv), f2bf2(acc[2] * inv, acc[3] * inv)};
     else *reinterpret_cast<f32x4_any_t*>(dst) = acc * inv;
-    if (first && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * 0.6931471805599453f + logf(total);
-    if (WEIGHTS == KV4_LOGS && first) a.lse2[row * a.heads + qh] = kv4_weight_log(top, total);
+    if (first && a.lse) a.lse[row * a.heads + qh] = kv4_lse(a, top, total);
+    if (WEIGHTS == KV4_LOGS && first) a.dealt[row * a.heads + qh] = kv4_dealt(top, total);
 }
 
 // One chunk against one tile of columns: scores q.k (masked where `whole` is false), new maximum, probabilities in place of the scores; what was gathered is scaled.
-// factor2 > 0; top is in units of the exponent.
+// factor2 > 0; top is a score.
 template <int NB>
-__device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there, int slot0, int limit, int quad, float factor2, float& top, float& sum, f32x4_t o[NB]) {
+__device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there, int slot0, int limit, int quad, const Kv4Attn& a, float& top, float& sum, f32x4_t o[NB]) {
     if (!whole) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -405,21 +413,21 @@ __device__ __forceinline__ void kv4_softmax(f32x4_t s[4], bool whole, int there,
 #pragma unroll
         for (int i = 0; i < 4; ++i) best = fmaxf(best, s[p][i]);
     best = rows4_max(best);
-    best = fmaxf(top, best * factor2);
-    // The maximum moves only where some column of the tile passes it by 2^8 (probabilities up to 2^8 lose nothing in 32 bits): seldom after the first chunks.
-    if (__any(best > top + 8.f)) {
-        const float scale = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.f : best));
+    best = fmaxf(top, best);
+    // The maximum moves only where a probability of some column of the tile would pass 2^8 (up to there they lose nothing in 32 bits): seldom after the first chunks.
+    if (__any(best > top + a.slack)) {
+        const float scale = kv4_weight(a, top, kv4_base(best));
         sum *= scale;
 #pragma unroll
         for (int d = 0; d < NB; ++d) o[d] *= scale;
         top = best;
     }
-    const float base = top == -INFINITY ? 0.f : top;
+    const float base = kv4_base(top);
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[p][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], factor2, -base));
+            s[p][i] = kv4_weight(a, s[p][i], base);
             sum += s[p][i];
         }
 }
@@ -449,18 +457,18 @@ __device__ __forceinline__ void kv4_seen_weights(f32x4_t& w, int slot, int end) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = slot + i < end ? w[i] : 0.f;
 }
-// Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: lse2 is their kv4_weight_log, +inf for a
+// Attention weights of a chunk's entries (rows of the scores) from one tile of columns, whose sums are known: `dealt` is their kv4_dealt, (0, +inf) for a
 // column that does not exist.  WHOLE: every column sees every entry.
 template <int HD, int PLANES>
-__device__ __forceinline__ void kv4_add_weights(const Kv4Keys<HD>& k, const u32x4_t q[HD / 32][PLANES], bool whole, int there, int slot0, int limit, float factor2,
-                                                float lse2, f32x4_t weight[4]) {
+__device__ __forceinline__ void kv4_add_weights(const Kv4Keys<HD>& k, const u32x4_t q[HD / 32][PLANES], bool whole, int there, int slot0, int limit, const Kv4Attn& a,
+                                                float2 dealt, f32x4_t weight[4]) {
     const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const f32x4_t s = kv4_scores<HD, PLANES>(k, p, q);
         f32x4_t w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor2, -lse2));
+        for (int i = 0; i < 4; ++i) w[i] = kv4_dealt_weight(a, s[i], dealt);
         if (!whole) kv4_seen_weights(w, slot0 + p * KV4_PAGE + quad * 4, (there >> p) & 1 ? limit : 0);
         weight[p] += w;
     }
@@ -497,7 +505,7 @@ __device__ __forceinline__ float kv4_sum_weights(const f32x4_t weight[4]) {
 // both tiles in one wave's registers 28 columns of 64 sequences took a quarter longer).
 // 256 sequences of 4096 .. 8192 entries, 7B heads: 859 MB in 163 .. 167 us, 5.2 TB/s, what a copy reaches (8 us more in the order of the sequences); 480 vector
 // and 48 matrix instructions per chunk keep a SIMD busy for two thirds of that.  Without the requests ahead, or with them dropped for a third wave per SIMD, it
-// took 5 and 10 % longer.  At 128 dims the fp32 instances spill 4 to 6 of 256 registers.
+// took 5 and 10 % longer.  At 128 dims the fp32 instances spill 5 of 256 registers.
 // KV4_WEIGHTS: the tile is the only one and its entries are not split, so the block knows the sums of its columns and adds the weights itself, with the keys
 // once more.  Against two launches: 64 x 4 of 64 .. 512 entries 12.5 us and 16.9, of 128 .. 5120 47 and 47 (fp32 57 and 61; 256 blocks, so the longest sequence
 // decides); where the blocks go in rounds the weights' own, finer blocks are ahead (256 x 4 of 512 .. 4096: 118 and 104).
@@ -541,7 +549,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
         f32x4_t s[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) s[p] = kv4_scores<HD, PLANES>(k_, p, q);
-        kv4_softmax<2 * G>(s, whole, there_, slot0, limit, quad, a.factor2, top, sum, o);
+        kv4_softmax<2 * G>(s, whole, there_, slot0, limit, quad, a, top, sum, o);
 #pragma unroll
         for (int p = 0; p < 4; p += 2) {
             u32x4_t w[PP];
@@ -587,10 +595,10 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
         const int c = lane & 15;
         float best = -INFINITY, total = 0.f;
         for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][c]);
-        const float base = best == -INFINITY ? 0.f : best;
+        const float base = kv4_base(best);
         f32x4_t acc = {};
         for (int w = 0; w < waves; ++w) {
-            const float scale = __builtin_amdgcn_exp2f(lds_ml[w][0][c] - base);
+            const float scale = kv4_weight(a, lds_ml[w][0][c], base);
             total += scale * lds_ml[w][1][c];
             acc += scale * *reinterpret_cast<const f32x4_t*>(lds_o[w][d][lane]);
         }
@@ -599,9 +607,9 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
     if constexpr (WEIGHTS == KV4_WEIGHTS) {
         float best = -INFINITY, total = 0.f;
         for (int w = 0; w < waves; ++w) best = fmaxf(best, lds_ml[w][0][lane & 15]);
-        const float base = best == -INFINITY ? 0.f : best;
-        for (int w = 0; w < waves; ++w) total += __builtin_amdgcn_exp2f(lds_ml[w][0][lane & 15] - base) * lds_ml[w][1][lane & 15];
-        const float lse2 = col < cols ? kv4_weight_log(best, total) : INFINITY;
+        const float base = kv4_base(best);
+        for (int w = 0; w < waves; ++w) total += kv4_weight(a, lds_ml[w][0][lane & 15], base) * lds_ml[w][1][lane & 15];
+        const float2 dealt = kv4_dealt(best, col < cols ? total : 0.f);
         float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
         slot0 = begin + wave * KV4_CHUNK;
         kv4_pages<HD>(a.c, b, head, slot0, page[0], there[0]);
@@ -613,7 +621,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
             const float before = slot >= 0 ? scores[slot] : 0.f;
             kv4_pages<HD>(a.c, b, head, slot0 + 2 * step, page[1], there[1]);
             f32x4_t weight[4] = {};
-            kv4_add_weights<HD, PLANES>(k[0], q, slot0 + KV4_CHUNK <= safe && there[0] == 15, there[0], slot0, limit, a.factor2, lse2, weight);
+            kv4_add_weights<HD, PLANES>(k[0], q, slot0 + KV4_CHUNK <= safe && there[0] == 15, there[0], slot0, limit, a, dealt, weight);
             const float sum_ = kv4_sum_weights(weight);
             if (slot >= 0) scores[slot] = before + sum_;
             k[0] = k[1];
@@ -627,7 +635,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_kernel(Kv4Attn a) {
 // Several blocks per CU cover each other's waits: 16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 131 .. 138 us, by which rows meet which
 // lengths, 0.95 executed PFLOP/s (three bf16 parts of q and of the weights) of the 1.22 that a plain product reaches; bf16 102 .. 106 us.  (4 % more in fp32 with the sums of a
 // tile one after the other, 18 % in the order of the sequences.)  Two tiles to a wave, for half the reads of LDS, take two waves a SIMD: fp32 26 %, bf16 7 % more.
-// The fp32 instance at 128 dims spills 9 of 168 registers, reloaded in every chunk.
+// The fp32 instance at 128 dims spills 10 of 168 registers, reloaded in every chunk.
 template <typename T, int HD, int PLANES, int WEIGHTS>
 __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, PP = PLANES == 1 ? 2 : 3, NW = 4, COLS = 16 * NW;
@@ -735,7 +743,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_many_kernel(Kv4Attn a) {
             u32x4_t v[2][AT];
 #pragma unroll
             for (int d = 0; d < AT; ++d) v[0][d] = lds_v[d][lane];
-            kv4_softmax<2 * G>(s, slot0 + KV4_CHUNK <= safe && there0 == 15, there0, slot0, limit, quad, a.factor2, top, sum, o);
+            kv4_softmax<2 * G>(s, slot0 + KV4_CHUNK <= safe && there0 == 15, there0, slot0, limit, quad, a, top, sum, o);
             u32x4_t w[PP];
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
@@ -777,13 +785,13 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     float best = -INFINITY;
     for (int s = l; s < parts; s += 16) best = fmaxf(best, a.part_ml[at + s].x);
     best = row16_max(best);
-    const float base = best == -INFINITY ? 0.f : best;
+    const float base = kv4_base(best);
     float total = 0.f, acc[N] = {};
     for (int s0 = 0; s0 < parts; s0 += 16) {
         float scale = 0.f;
         if (s0 + l < parts) {
             const float2 ml = a.part_ml[at + s0 + l];
-            scale = __builtin_amdgcn_exp2f(ml.x - base);
+            scale = kv4_weight(a, ml.x, base);
             total += scale * ml.y;
         }
         const int m = min(16, parts - s0);
@@ -799,8 +807,8 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     T* dst = static_cast<T*>(a.out) + row * a.o_row + qh * a.o_head + l * N;
 #pragma unroll
     for (int i = 0; i < N; ++i) st1(dst + i, acc[i] * inv);
-    if (l == 0 && a.lse) a.lse[row * a.heads + qh] = total == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(total);
-    if (l == 0 && a.lse2) a.lse2[row * a.heads + qh] = kv4_weight_log(best, total);
+    if (l == 0 && a.lse) a.lse[row * a.heads + qh] = kv4_lse(a, best, total);
+    if (l == 0 && a.dealt) a.dealt[row * a.heads + qh] = kv4_dealt(best, total);
 }
 
 // Attention weight per entry, added to the accumulated one: the scores are computed a second time (keys are half of the cache; storing a
@@ -822,7 +830,7 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
     kv4_pages<HD>(a.c, b, head, slot0, page, there);
     kv4_load_keys<HD>(page, lane, k);
     const int limit = col < cols ? n - (count - 1 - col / a.group) : 0;
-    const float lse2 = col < cols ? a.lse2[(int64_t)(r0 + col / a.group) * a.heads + head * a.group + col % a.group] : INFINITY;
+    const float2 dealt = col < cols ? a.dealt[(int64_t)(r0 + col / a.group) * a.heads + head * a.group + col % a.group] : kv4_dealt(0.f, 0.f);
     kv4_load_q<T, HD, PLANES>(a, r0, count, head, col, lane, q);
     float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
     for (; slot0 < n; slot0 += step) {
@@ -831,7 +839,7 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
         const int slot = kv4_score_slot(slot0, n, there);
         const float before = slot >= 0 ? scores[slot] : 0.f;
         f32x4_t weight[4] = {};
-        kv4_add_weights<HD, PLANES>(k, q, slot0 + KV4_CHUNK <= safe && there == 15, there, slot0, limit, a.factor2, lse2, weight);
+        kv4_add_weights<HD, PLANES>(k, q, slot0 + KV4_CHUNK <= safe && there == 15, there, slot0, limit, a, dealt, weight);
         const float mine = kv4_sum_weights(weight);
         if (slot >= 0) scores[slot] = before + mine;
         k = k1;
@@ -848,7 +856,7 @@ template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
     constexpr int G = HD / 32, TILES = 4 / G;
     __shared__ u32x4_t lds_q[2][4][PLANES][64];             // [buffer][tile * G + 32 dims]
-    __shared__ float lds_lse2[2][TILES][16];
+    __shared__ float2 lds_dealt[2][TILES][16];
     __shared__ int lds_limit[2][TILES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
     const int b = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv;
@@ -857,16 +865,17 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
     const int begin = blockIdx.z * a.w_cols, cols = min(count * a.group, begin + a.w_cols), safe = n - (count - 1);
     if (begin >= cols) return;
     float* scores = a.book.scores + b * a.book.score_b + head * a.book.score_h;
-    // this lane's column of the tile that its wave cuts: its row, its head of the group, and where q and the logarithm of the sum lie
+    // this lane's column of the tile that its wave cuts: its row, its head of the group, and where q and its kv4_dealt lie
     const int first = begin + wave / G * 16 + (lane & 15), rows_on = 16 * TILES / a.group, heads_on = 16 * TILES % a.group;
     int col, head_at, limit, buf = 0;
     const T* at;
-    const float* lse;
-    float raw[8] = {}, lse2;
+    const float2* from;
+    float raw[8] = {};
+    float2 dealt;
     auto request = [&]() {                                  // a column beyond the last one keeps the values of the one before it; it sees nothing
         const bool is = col < cols;
         if (is) kv4_load8(at, raw);
-        lse2 = is ? *lse : INFINITY;
+        dealt = is ? *from : kv4_dealt(0.f, 0.f);
     };
     auto advance = [&]() {
         const bool over = (head_at += heads_on) >= a.group;
@@ -875,7 +884,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
         col += 16 * TILES;
         limit = col < cols ? limit + rows : 0;
         at += rows * a.q_row + heads * a.q_head;
-        lse += (int64_t)rows * a.heads + heads;
+        from += (int64_t)rows * a.heads + heads;
     };
     for (int base = blockIdx.y * 4 * KV4_CHUNK; base < n; base += gridDim.y * 4 * KV4_CHUNK) {      // the same for all waves: they meet below
         const int slot0 = base + wave * KV4_CHUNK;
@@ -886,7 +895,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
         col = first, head_at = first % a.group;
         limit = col < cols ? n - (count - 1 - col / a.group) : 0;
         at = static_cast<const T*>(a.q) + (int64_t)(r0 + col / a.group) * a.q_row + (int64_t)(head * a.group + head_at) * a.q_head + quad * (HD / 4) + wave % G * 8;
-        lse = a.lse2 + (int64_t)(r0 + col / a.group) * a.heads + head * a.group + head_at;
+        from = a.dealt + (int64_t)(r0 + col / a.group) * a.heads + head * a.group + head_at;
         request();
         kv4_pages<HD>(a.c, b, head, slot0, page, there);
         kv4_load_keys<HD>(page, lane, raw_k);
@@ -903,7 +912,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
             q4_operand<PLANES>(raw, o);
 #pragma unroll
             for (int x = 0; x < PLANES; ++x) lds_q[buf][wave][x][lane] = o[x];
-            if (wave % G == 0 && quad == 0) lds_lse2[buf][wave / G][lane] = lse2, lds_limit[buf][wave / G][lane] = limit;
+            if (wave % G == 0 && quad == 0) lds_dealt[buf][wave / G][lane] = dealt, lds_limit[buf][wave / G][lane] = limit;
             __syncthreads();
             advance();
             request();
@@ -911,7 +920,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 if (c0 + t * 16 >= cols) break;
-                const float sum2 = lds_lse2[buf][t][lane & 15];
+                const float2 of = lds_dealt[buf][t][lane & 15];
                 f32x4_t s[4] = {};
 #pragma unroll
                 for (int j = 0; j < G; ++j)
@@ -926,7 +935,7 @@ __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {
                 for (int p = 0; p < 4; ++p) {
                     f32x4_t w;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], a.factor2, -sum2));
+                    for (int i = 0; i < 4; ++i) w[i] = kv4_dealt_weight(a, s[p][i], of);
                     if (!whole) kv4_seen_weights(w, slot0 + p * KV4_PAGE + quad * 4, (there >> p) & 1 ? sees : 0);
                     weight[p] += w;
                 }

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -97,8 +98,8 @@ bool lists_overlap(const rsd_kv4_cache* c, int64_t batch_stride, int64_t head_st
 struct AttnPlan {
     int tiles, waves, split, splits, w_cols, w_groups;
     bool many, by_length, fused;
-    uint64_t o_bytes, ml_bytes, lse_bytes, w_bytes;
-    uint64_t bytes() const { return o_bytes + ml_bytes + lse_bytes + w_bytes; }
+    uint64_t o_bytes, ml_bytes, dealt_bytes, w_bytes;
+    uint64_t bytes() const { return o_bytes + ml_bytes + dealt_bytes + w_bytes; }
 };
 
 // Which kernel, and how the entries are split (by the sizes that the host knows; times with launch):
@@ -138,7 +139,7 @@ AttnPlan attn_plan(const rsd_kv4_cache* c, const rsd_kv4_attn* a, bool scored) {
     p.o_bytes = p.splits > 1 ? up256(lines * p.splits * c->head_dim * 4) : 0;
     p.ml_bytes = p.splits > 1 ? up256(lines * p.splits * 8) : 0;
     p.fused = scored && !p.many && p.tiles == 1 && p.splits == 1;
-    p.lse_bytes = scored && !p.fused ? up256(lines * 4) : 0;
+    p.dealt_bytes = scored && !p.fused ? up256(lines * 8) : 0;
     const int64_t tiles = ceil_div(cols, 16), pairs = (int64_t)c->batch * c->n_kv_heads;
     const int64_t groups = tiles == 1 ? 1 : std::max<int64_t>(1, std::min(4096 / (pairs * ceil_div(chunks, 4)), tiles / 8));
     p.w_cols = (int)(ceil_div(tiles, groups) * 16);
@@ -163,10 +164,10 @@ int check_attn(const rsd_kv4_cache* c, const rsd_kv4_attn* a) {
 template <typename T, int HD, int PLANES> void attn_run(const Kv4Attn& k, const AttnPlan& p, Launches& l) {
     const unsigned lists = (unsigned)(k.c.batch * k.c.hkv);
     const dim3 grid(lists, (unsigned)p.tiles, (unsigned)p.splits), many(lists * (unsigned)p.tiles, 1, (unsigned)p.splits);
-    if (p.many && k.lse2) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS>, many, 256, 0, k);
+    if (p.many && k.dealt) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_LOGS>, many, 256, 0, k);
     else if (p.many) l.run(kv4_attn_many_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, many, 256, 0, k);
     else if (p.fused) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_WEIGHTS>, grid, 64 * p.waves, 0, k);
-    else if (k.lse2) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_LOGS>, grid, 64 * p.waves, 0, k);
+    else if (k.dealt) l.run(kv4_attn_kernel<T, HD, PLANES, KV4_LOGS>, grid, 64 * p.waves, 0, k);
     else l.run(kv4_attn_kernel<T, HD, PLANES, KV4_NO_WEIGHTS>, grid, 64 * p.waves, 0, k);
     if (p.splits > 1)
         l.run(kv4_join_kernel<T, HD>, (unsigned)ceil_div((int64_t)k.c.batch * k.max_rows * k.heads, 16), 256, 0, k);
@@ -306,19 +307,21 @@ extern "C" int rsd_kv4_attention(const rsd_kv4_cache* c, const rsd_kv4_attn* a, 
     k.q = a->q, k.q_row = a->q_row, k.q_head = a->q_head;
     k.row_start = a->row_start, k.total_rows = a->rows, k.max_rows = a->max_rows, k.heads = a->n_heads, k.group = a->n_heads / c->n_kv_heads;
     k.scale = a->scale;
-    k.plain = !(std::fabs(a->scale) > 0.f);
-    k.factor2 = k.plain ? 1.f : (float)(std::fabs((double)a->scale) * 1.4426950408889634);
+    k.plain = !(std::fabs(a->scale) > 0.f) || std::isinf(a->scale);
+    k.factor = k.plain ? 1.f : std::fabs(a->scale);
+    k.factor2 = (float)std::min(k.factor * 1.4426950408889634, (double)FLT_MAX);
+    k.slack = (float)std::min(8. / k.factor2, (double)FLT_MAX);
     k.negative = a->scale < 0.f;
     k.out = a->out, k.o_row = a->out_row, k.o_head = a->out_head;
     k.lse = a->lse;
-    k.lse2 = p.lse_bytes ? reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
+    k.dealt = p.dealt_bytes ? reinterpret_cast<float2*>(ws + p.o_bytes + p.ml_bytes) : nullptr;
     k.max_kv = a->max_kv, k.tiles = p.tiles, k.split = p.split, k.splits = p.splits, k.by_length = p.by_length, k.hd = c->head_dim;
     k.part_o = reinterpret_cast<float*>(ws);
     k.part_ml = reinterpret_cast<float2*>(ws + p.o_bytes);
     if (scored) k.book = dev_book(book);
     k.w_cols = p.w_cols, k.w_groups = p.w_groups;
     k.w_slots = ceil_div(std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KV4_PAGE), KV4_CHUNK) * KV4_CHUNK;
-    k.part_w = reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes + p.lse_bytes);
+    k.part_w = reinterpret_cast<float*>(ws + p.o_bytes + p.ml_bytes + p.dealt_bytes);
     Launches l(hip_stream);
     if (a->dtype == RSD_F32) attn_run<float, 3>(k, p, c->head_dim, l);
     else attn_run<bf16_t, 1>(k, p, c->head_dim, l);
