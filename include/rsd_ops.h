@@ -190,8 +190,8 @@ int rsd_kv_read(const rsd_kv_cache *c, const int32_t *seq, const int32_t *slot, 
  * most max_rows of them (further ones are not computed), and n = min(kv_len[b], max_kv) entries.  Row j of its m rows stands at slot p = n - m + j and sees the
  * slots s <= p that have a page and, with window > 0, lie near or at the front: s > p - window or s < sinks.  (Pages that no row sees any more are not read: the table may drop them.)
  * q, out dev [rows][n_heads][head_dim] of `dtype` with row and head strides; head h reads kv head h / (n_heads / n_kv_heads).  out = softmax(scale q.K) V; a row
- * that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of the sum of exp(scale q.k), -inf for such rows.  An infinity or NaN
- * in an entry reaches the rows that see it and no others.  Sizes: batch * n_kv_heads * (max_rows * n_heads / n_kv_heads in whole 64s) up to
+ * that sees nothing, or scores -inf with all that it sees, gives 0.  lse (dev [rows][n_heads] or NULL) = log of the sum of exp(scale q.k), -inf for such rows.  Scores and sums are fp32; the
+ * weights that meet the values hold 16 bits where `dtype` is bf16, and 24 where it is fp32.  An infinity or NaN in an entry reaches the rows that see it and no others.  Sizes: batch * n_kv_heads * (max_rows * n_heads / n_kv_heads in whole 64s) up to
  * 2^26, max_rows * n_heads below 2^27.  out may be q itself; but for that, out, lse and the workspace share no memory with each other or with
  * what the call reads (an array that lies between the ends of another counts as sharing). */
 typedef struct rsd_kv_attn {

@@ -190,15 +190,16 @@ __device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, KvcWork& w) {
 }
 
 // Activations of type T over a cache of type C.
-//   bf16 over bf16: operands as they are.  A probability enters the second product rounded to bf16, off by at most 2^-8 of itself like a
-//     result that is rounded to bf16 itself; the sum it is divided by has all of its bits.
-//   fp32 over bf16: q and probabilities in three bf16 parts, which hold all 24 bits; three matrix instructions each.  They are cut, not rounded, so that all have the sign of the whole, and
-//     none is 0 where the whole is not (2^-30 of it stands in, or is added): an infinite key or value meets no 0 that would make a NaN of it.
+//   bf16 over bf16: q as it is, a probability in two bf16 parts, which hold 16 bits (2^-16 of it, as over the 4-bit cache, where its result is rounded to 8 bits); one bf16 number was off by up to 2^-8
+//     and cost a third more error than the rounding of the result alone (2.2e-3 against 1.66e-3 of it in the mean).
+//   fp32 over bf16: q and probabilities in three bf16 parts, which hold all 24 bits; three matrix instructions each.
+//   First parts are cut, not rounded, so that all have the sign of the whole, and none is 0 where the whole is not (2^-22 of the first or 2^-30 of the whole is added, or stands in): an infinite key or
+//     value meets no 0 that would make a NaN of it.
 //   fp32 over fp32: matrix instructions in fp32.
 template <typename T, typename C, int HD> struct KvcMath {
     typedef KvcLayout<C, HD> L;
     static constexpr bool F32 = sizeof(C) == 4;
-    static constexpr int N = L::N, PAGES = F32 ? 1 : 2, CH = PAGES * KVC_PAGE, PLANES = !F32 && sizeof(T) == 4 ? 3 : 1;
+    static constexpr int N = L::N, PAGES = F32 ? 1 : 2, CH = PAGES * KVC_PAGE, PLANES = !F32 && sizeof(T) == 4 ? 3 : 1, PARTS = F32 ? 1 : sizeof(T) == 4 ? 3 : 2;     // of q; of a probability
     struct Q { u32x4_t w[N][PLANES]; };
     struct Entries { u32x4_t w[PAGES][N]; };        // keys, or values, of a chunk as pages hold them
     struct Values { u32x4_t w[HD / 16]; };          // values as operands: block d of 16 dims, rows (dims) lane % 16, tokens 4 (lane / 16) + i of the first page, then of the second
@@ -282,7 +283,7 @@ template <typename T, typename C, int HD> struct KvcMath {
                     }
     }
     // probabilities of a chunk as operands
-    struct P { u32x4_t w[PLANES]; };
+    struct P { u32x4_t w[PARTS]; };
     static __device__ __forceinline__ P weights(const f32x4_t s[PAGES]) {
         P p;
         if constexpr (F32) p.w[0] = u32x4_t{__float_as_uint(s[0][0]), __float_as_uint(s[0][1]), __float_as_uint(s[0][2]), __float_as_uint(s[0][3])};
@@ -290,8 +291,11 @@ template <typename T, typename C, int HD> struct KvcMath {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = s[i / 2][2 * (i & 1)], y = s[i / 2][2 * (i & 1) + 1];
-                if constexpr (PLANES == 1) p.w[0][i] = f2bf2(x, y);
-                else {                                      // (a probability is not negative)
+                if constexpr (PARTS == 2) {
+                    constexpr float LESS = -1.f + 0x1p-22f;
+                    p.w[0][i] = first_parts(x, y);
+                    p.w[1][i] = f2bf2(__builtin_fmaf(first_part(x), LESS, x), __builtin_fmaf(first_part(y), LESS, y));
+                } else {                                    // (a probability is not negative)
                     const float x1 = __builtin_fmaf(x, 0x1p-30f, x - first_part(x)), y1 = __builtin_fmaf(y, 0x1p-30f, y - first_part(y));
                     const float x2 = __builtin_fmaf(x, 0x1p-30f, x1 - first_part(x1)), y2 = __builtin_fmaf(y, 0x1p-30f, y1 - first_part(y1));
                     p.w[0][i] = first_parts(x, y);
@@ -307,7 +311,7 @@ template <typename T, typename C, int HD> struct KvcMath {
 #pragma unroll
         for (int d0 = 0; d0 < HD / 16; d0 += SIDE)
 #pragma unroll
-            for (int e = 0; e < (F32 ? 4 : PLANES); ++e)
+            for (int e = 0; e < (F32 ? 4 : PARTS); ++e)
 #pragma unroll
                 for (int d = d0; d < d0 + SIDE; ++d)
 #pragma unroll
@@ -497,7 +501,7 @@ __device__ __forceinline__ void kvc_bound_values(const KvcAttn& a, const KvcSpan
 // turn, each with its own running maximum and sum; they are joined in LDS.  The next chunk's keys are requested as soon as this one's are used up, the values likewise, the table entries
 // one chunk earlier still: one set of registers for each instead of two, and eight waves on a CU.
 // Bound by bytes: 256 sequences of 4096 .. 8192 entries, 7B heads, bf16 (3.24 GB): 537 us, 6.0 TB/s, what a read alone reaches (572 with two whole chunks of registers, 558 with four waves to a
-// block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 7 .. 9 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
+// block); with a window of 1024 and 4 sinks (543 MB) 102 us, 5.3 TB/s.  One sequence of 1279 entries: 10 us, five chunks to a wave, one latency each.  fp32, 16 x 16 heads of 64, 17 .. 128
 // rows: 43 us, matrix instructions in fp32 at 68 TFLOP/s; 63 with the kernel of many columns, whose waves have no columns in a last tile.
 template <typename T, typename C, int HD>
 __global__ __launch_bounds__(512, 2) void kvc_attn_few_kernel(KvcAttn a) {
@@ -594,12 +598,12 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
 // Many columns over a bf16 cache (chunks of prompts, steps, scoring): a block of four waves owns 64 * NT columns, NT tiles to a wave, and one part of their steps of U chunks.  The steps go through a ring of
 // R stages in LDS, straight from memory (pages are operands as they are), a quarter of each by every wave.  The one barrier of a step stands in the middle of its last chunk,
 // when all of the step's operands are in registers: behind it the next step's keys are read and this one's stage is requested anew.
-// 2048 rows of a 7B prompt's 8192 entries: 218 us, 963 TFLOP/s of the 1396 that a plain product of 8192^3 reaches (281 with NT = 1; 423 with a tile of 16 to a block and no ring).  Matrix instructions
-// are busy 39 % of the time, vector instructions about as long (per 32 entries and 16 columns 16 of the one and 50 of the other, 8 of them exponentials); two waves on a SIMD, of different blocks,
-// overlap them in part.  Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  Neither priorities of waves nor eight-byte reads of the values
-// (no moves, twice the reads) changed the time.
-// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 106 us, 0.87 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 75 .. 79 us with the join, 4.5 TB/s;
-// 256 of 2048 entries, 8 rows: 198 us, 5.6 TB/s.
+// 2048 rows of a 7B prompt's 8192 entries: 305 us, 690 TFLOP/s, or 1035 with the second parts of the probabilities, of the 1396 that a plain product of 8192^3 reaches (348 with NT = 1; 229 with
+// probabilities of 8 bits).  Per 32 entries and 16 columns there are 24 matrix instructions and 75 others, 8 of them exponentials; two waves on a SIMD, of different blocks, overlap them in part.
+// Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  The instance of NT = 2 at 128 dims spills 33 of 256 registers, all of them in the steps with
+// a mask, whose reloads wait for the ring's copies too; also where a window makes more of those it is ahead of NT = 1 (2048 rows of 8192, window 2000: 107 and 113 us).
+// 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 106 us, 0.87 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 76 .. 78 us with the join, 4.5 TB/s;
+// 256 of 2048 entries, 8 rows: 201 us, 5.5 TB/s.
 template <typename T, typename C, int HD, int NT> struct KvcMany {
     static constexpr bool SMALL = NT == 1 && sizeof(T) == sizeof(C);
     static constexpr int U = SMALL ? 1 : 2, R = SMALL ? 3 : 2, CH = U * KvcMath<T, C, HD>::CH;      // CH: slots of a step

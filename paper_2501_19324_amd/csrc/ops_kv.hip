@@ -156,17 +156,17 @@ struct AttnPlan {
 int window_of(const rsd_kv_cache* c, const rsd_kv_attn* a) { return a->window >= std::min<int64_t>(a->max_kv, (int64_t)c->max_pages * KVC_PAGE) ? 0 : a->window; }
 
 // Which kernel, which tiles, how the entries are split: by the sizes that the host knows.  Measured with 28 heads over 4 of 128, bf16, where nothing else is said, in us:
-//  - the kernel of few columns takes up to two tiles of 16 (21 columns, 4 sequences of 2048 entries: 13.2, the other 15.8; 64 of 128 .. 2048, fp32 activations: 32 and 39; 64 of 128 .. 5120: 71 and 70),
-//    but one tile where the lists of entries alone fill the card (21 columns, 256 of 2048: 219 and 189), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 43 and 63).
-//  - 128 columns to a block instead of 64 where rows see 768 entries and more before their own (2048 rows of 8192: 223 and 280, 16 x 128 of 1024: 48 and 54; against that 2048 of 2048: 58 and 50,
-//    64 x 128 of 300: 87 and 74) and there are 384 such blocks with their parts (512 rows of 8192: 84 and 92; against that 4 x 128 of 2048: 42 and 36, 256 of 8192: 56 and 54).
-//  - a part's sums are 4 bytes an element written and read, beside the join's launch.  Many columns are split up to 512 blocks (16 x 128 of 1024: 50 whole, 71 in two; 256 x 8 of 2048: 197 whole, 244 in two;
-//    256 of 8192: 166 whole, 57 in eight), up to 48 columns for 768 (64 x 5 of 128 .. 5120: 89 whole, 74 in three, 85 in four; where all have 5120 the three cost: 116 whole, 140), no part under 512 or 1024 entries.
-//    Few columns for 256 blocks, no part under 768 (one sequence of 1279: 9.9 whole, 10.8 in two; of 2500: 14.4 whole, 11.9 in three; of 8000: 39 whole, 15.7 in ten; 16 of 8000: 67 whole, 46 .. 49 in two to four).
-//  - few columns: eight waves up to 256 blocks (one sequence of 896 .. 1279: 9.8, 11.1 with four) and for long lists (256 of 4096 .. 8192: 535 and 558), else four (window 1024: 101, 105 with eight; heads of 64: 49 and 54).
-//  - where sequences have unlike numbers of rows, blocks without columns go behind the others (16 of 17 .. 128 rows, 72B heads, fp32, window 1000: 103 and 111; 32 of 5 .. 128 rows of 300 .. 4096: 102 and 110;
-//    16 x 16 heads of 64, fp32: 43 and 46; where all have the same it costs a block's start 0.5 us: 64 x 128 of 300: 80 and 76).
-//  - the longest lists first, from the point where the blocks are more than the card holds at once (64 x 5 of 128 .. 5120: 75 and 84; 256 of 4096 .. 8192: 534 and 555).
+//  - the kernel of few columns takes up to two tiles of 16 (21 columns, 4 sequences of 2048 entries: 13.3, the other 17.0; 8, 32 of 128 .. 5120: 18 and 24, 38 and 51; fp32 activations 19 and 31, 40 and 54; of 64 such
+//    sequences the longest decide: 81 and 72), but one tile where the lists of entries alone fill the card (21 columns, 128, 256 of 2048: 113 and 97, 221 and 191), and all over an fp32 cache (16 x 16 heads of 64, 17 .. 128 rows: 43 and 63).
+//  - 128 columns to a block instead of 64 where rows see 768 entries and more before their own (2048 rows of 8192: 305 and 348, with a window of 2000 107 and 113; 16 x 128 of 1024: 56 and 60; against that 2048 of 2048: 71 and 58,
+//    64 x 128 of 300: 88 and 84) and there are 384 such blocks with their parts (512 rows of 8192: 104 and 111; against that 4 x 128 of 2048: 47 and 41, 256 of 8192: 64 and 63).
+//  - a part's sums are 4 bytes an element written and read, beside the join's launch.  Many columns are split up to 512 blocks (16 x 128 of 1024: 58 whole, 79 in two; 256 x 8 of 2048: 200 whole, 246 in two;
+//    256 of 8192: 219 whole, 65 in eight), up to 48 columns for 768 (64 x 5 of 128 .. 5120: 97 whole, 76 in three, 88 in four; where all have 5120 the three cost: 117 whole, 142), no part under 512 or 1024 entries.
+//    Few columns for 256 blocks, no part under 768 (one sequence of 1279: 10.2 whole, 11.1 in two; of 2500: 15.0 whole, 12.2 in three; of 8000: 39 whole, 15.8 in ten; 16 of 8000: 67 whole, 45 .. 48 in two to four).
+//  - few columns: eight waves up to 256 blocks (one sequence of 896 .. 1279: 10.2, 11.9 with four) and for long lists (256 of 4096 .. 8192: 535 and 558), else four (window 1024: 101, 105 with eight; heads of 64: 49 and 54).
+//  - where sequences have unlike numbers of rows, blocks without columns go behind the others (16 of 17 .. 128 rows, 72B heads, fp32, window 1000: 103 and 111; 32 of 5 .. 128 rows of 300 .. 4096: 133 and 146;
+//    16 x 16 heads of 64, fp32: 43 and 46; where all have the same it costs a block's start 0.5 us: 64 x 128 of 300: 87 and 83).
+//  - the longest lists first, from the point where the blocks are more than the card holds at once (64 x 5 of 128 .. 5120: 76 and 87; 256 of 4096 .. 8192: 534 and 555).
 AttnPlan attn_plan(const rsd_kv_cache* c, const rsd_kv_attn* a) {
     AttnPlan p{};
     const int group = a->n_heads / c->n_kv_heads, window = window_of(c, a);

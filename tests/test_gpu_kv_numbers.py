@@ -66,3 +66,22 @@ def test_scores_beyond_the_range_of_the_exponential(torch, R, act, held, form, s
         close(out, o, 2 * (n + 96) * U * mass * 1.01 + HALF[act] * np.abs(o), (form, n))
         with np.errstate(over="ignore"):
             close(lse, l.astype(np.float32), 8 * U * np.abs(np.where(np.isfinite(l), l, 0)) + 2 * (n + 96) * U, ("lse", form, n))
+
+
+@pytest.mark.parametrize("hd", [32, 128])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("act,held", PAIRS)
+def test_weights_that_nearly_cancel(torch, R, act, held, form, hd):
+    """Neighbours with values of opposite sign and nearly the same weight: the result is small beside sum p|v|, and so is its rounding, so the bits that weights are held in show.  bf16 activations: two bf16
+    numbers, the first cut to 8 bits and the second rounded, 2^-16 of a weight; fp32: as the tolerances of ``test_gpu_kv``."""
+    rng = np.random.default_rng(hd)
+
+    def entries(n, hkv):
+        v = rng.choice([-2.0, -1.5, -1.0, 1.0, 1.25, 2.0], (n, hkv, hd))
+        v[1::2] = -v[:n // 2 * 2:2]
+        return rng.normal(size=(n, hkv, hd)), v
+
+    for out, lse, (o, l, mass, big), n in call(torch, R, rng, form, hd, act, held, entries, lambda rows, heads: 0.03 * rng.normal(size=(rows, heads, hd)), 1 / np.sqrt(hd)):
+        ds = 2 * (hd + 48) * U * big + 8 * U * np.abs(np.where(np.isfinite(l), l, 0)) + 8 * U * big
+        rel = 2 * ds + 2 * (n + 96) * U
+        close(out, o, (rel[..., None] + (2.0 ** -16 if act == "bf16" else 0)) * mass * 1.01 + HALF[act] * np.abs(o), (form, n))
