@@ -178,7 +178,8 @@ typedef struct rsd_kv_cache {
 
 /* Writes entries: row i (keys and values [n_kv_heads][head_dim], dev, of `dtype`) becomes slot[i] of sequence seq[i] (dev int32 [rows]; the pairs must differ), the keys as in
  * rsd_qk_rope on their way (k->out is not used), both rounded once to the cache's type.  kv_len is neither read nor changed.  q (may be NULL) goes to q->out in
- * the same launch, also for rows that name no entry of the cache.  q->out may be q->x and shares no memory with anything else of the call; k, v and q->x lie outside the pool. */
+ * the same launch, also for rows that name no entry of the cache.  q->out may be q->x and shares no memory with anything else of the call; nothing that the call reads lies in the pool (between the
+ * ends of an array counts as in it). */
 int rsd_kv_append(const rsd_kv_cache *c, const rsd_heads *k, const void *v, int64_t v_row, int64_t v_head, const rsd_heads *q, const int32_t *seq,
                   const int32_t *slot, const int32_t *position, const rsd_rope *rope, float eps, int32_t rows, int32_t dtype, void *hip_stream);
 

@@ -40,11 +40,13 @@ Bytes bytes_of(const void* p, int64_t n0, int64_t s0, int64_t n1, int64_t s1, in
 }
 Bytes bytes_of(const void* p, int64_t bytes) { return bytes_of(p, 1, 0, 1, 0, bytes, 1); }
 bool meet(Bytes a, Bytes b) { return a.from < b.to && b.from < a.to; }
+Bytes pool_of(const rsd_kv_cache* c) {
+    const int64_t page = 2ll * KVC_PAGE * c->head_dim * c->n_kv_heads;
+    return bytes_of(c->pool, c->n_pages, page, 1, 0, page, size_of(c->dtype));
+}
 // whether an array meets the pool, the table or (where it is used) kv_len
 bool meets_cache(Bytes a, const rsd_kv_cache* c, bool lengths) {
-    const int64_t page = 2ll * KVC_PAGE * c->head_dim * c->n_kv_heads;
-    return meet(a, bytes_of(c->pool, c->n_pages, page, 1, 0, page, size_of(c->dtype))) || meet(a, bytes_of(c->table, 4ll * c->batch * c->max_pages)) ||
-           (lengths && meet(a, bytes_of(c->kv_len, 4ll * c->batch)));
+    return meet(a, pool_of(c)) || meet(a, bytes_of(c->table, 4ll * c->batch * c->max_pages)) || (lengths && meet(a, bytes_of(c->kv_len, 4ll * c->batch)));
 }
 
 struct RowArgs {
@@ -118,6 +120,22 @@ int check_rows(const RowArgs& a, bool cached, const char* what) {
             return fail(RSD_EINVAL, "%s: the out of %s shares memory with weights, positions, frequencies, sequences or slots", what, i ? "k" : "q");
     }
     return RSD_OK;
+}
+// Whether something that an append reads lies in the pool that it writes
+int check_pool(const rsd_kv_cache* c, const RowArgs& a) {
+    const Bytes pool = pool_of(c);
+    const size_t size = size_of(a.dtype);
+    auto heads = [&](const void* p, int64_t row, int64_t head, int n) { return meet(pool, bytes_of(p, a.rows, row, n, head, a.head_dim, size)); };
+    auto array = [&](const void* p, int64_t n) { return p && meet(pool, bytes_of(p, n)); };
+    const char* name = nullptr;
+    if (heads(a.k->x, a.k->row, a.k->head, a.k->n_heads)) name = "k";
+    else if (heads(a.v, a.v_row, a.v_head, a.k->n_heads)) name = "v";
+    else if (a.q && heads(a.q->x, a.q->row, a.q->head, a.q->n_heads)) name = "q";
+    else if (array(a.k->weight, a.head_dim * size) || array(a.q ? a.q->weight : nullptr, a.head_dim * size)) name = "a weight";
+    else if (array(a.seq, 4ll * a.rows) || array(a.slot, 4ll * a.rows)) name = "seq or slot";
+    else if (a.rope && (array(a.position, 4ll * a.rows) || array(a.rope->freq, 4ll * a.rope->rot_dim))) name = "position or freq";
+    else if (array(c->table, 4ll * c->batch * c->max_pages)) name = "the table";
+    return name ? fail(RSD_EINVAL, "append: %s lies in the pool", name) : RSD_OK;
 }
 KvcHeads dev_heads(const rsd_heads* h) { return h ? KvcHeads{h->x, h->out, h->weight, h->row, h->head, h->out_row, h->out_head, h->n_heads} : KvcHeads{}; }
 KvcRows dev_rows(const RowArgs& a, const KvcCache& c) {
@@ -278,6 +296,7 @@ extern "C" int rsd_kv_append(const rsd_kv_cache* c, const rsd_heads* k, const vo
     if (!aligned(v, size_of(dtype))) return fail(RSD_EINVAL, "append: v is not aligned to its type");
     const RowArgs a{q, k, v, v_row, v_head, position, seq, slot, rope, eps, rows, c->head_dim, dtype};
     if (int rc = check_rows(a, true, "append")) return rc;
+    if (int rc = check_pool(c, a)) return rc;
     if (q && meets_cache(bytes_of(q->out, rows, q->out_row, q->n_heads, q->out_head, c->head_dim, size_of(dtype)), c, false))
         return fail(RSD_EINVAL, "append: the out of q shares memory with the cache");
     Launches l(hip_stream);
