@@ -849,8 +849,8 @@ __global__ __launch_bounds__(256) void kv4_weight_kernel(Kv4Attn a) {
 
 // The same for more than one tile of columns: a wave keeps its chunk's keys decoded and goes over the tiles, whose q the block cuts into operands in LDS, one
 // (tile, 32 dims) by each wave, the next ones while these are worked on.  Where blocks are few or unlike the columns are dealt in groups, whose weights the next
-// kernel adds up.  16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 89 .. 115 us and 5 for the sum, bf16 56 .. 69 and 5; 19 and 12 us
-// more in one group; three times as long with every wave cutting q for itself, chunk by chunk.  Some 216 vector instructions a tile and chunk beside 48 matrix
+// kernel adds up.  16 sequences of 17 .. 128 rows and 512 .. 2560 entries, 72B heads, fp32: 99 .. 115 us and 5 for the sum, bf16 61 .. 69 and 5; 19 and 12 us
+// more in one group; three times as long with every wave cutting q for itself, chunk by chunk.  Some 232 vector instructions a tile and chunk beside 48 matrix
 // instructions; three waves a SIMD (two: 15 % more), for which the fp32 instance at 128 dims spills 3 registers.
 template <typename T, int HD, int PLANES>
 __global__ __launch_bounds__(256, 3) void kv4_weight_many_kernel(Kv4Attn a) {

@@ -193,8 +193,8 @@ __device__ __forceinline__ bool kvc_work(const KvcAttn& a, int id, KvcWork& w) {
 //   bf16 over bf16: q as it is, a probability in two bf16 parts, which hold 16 bits (2^-16 of it, as over the 4-bit cache, where its result is rounded to 8 bits); one bf16 number was off by up to 2^-8
 //     and cost a third more error than the rounding of the result alone (2.2e-3 against 1.66e-3 of it in the mean).
 //   fp32 over bf16: q and probabilities in three bf16 parts, which hold all 24 bits; three matrix instructions each.
-//   First parts are cut, not rounded, so that all have the sign of the whole, and none is 0 where the whole is not (2^-22 of the first or 2^-30 of the whole is added, or stands in): an infinite key or
-//     value meets no 0 that would make a NaN of it.
+//   First parts are cut, not rounded, so that all have the sign of the whole, and from 2^-100 on none is 0 where the whole is not (2^-22 of the first or 2^-30 of the whole is added, or stands in): an
+//     infinite key or value meets no 0 that would make a NaN of it.
 //   fp32 over fp32: matrix instructions in fp32.
 template <typename T, typename C, int HD> struct KvcMath {
     typedef KvcLayout<C, HD> L;
@@ -588,10 +588,10 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
         kvc_copy<4>(lds, lane16, base);
         kvc_copy<COUNT - 4>(lds + 4096, lane16, base + 4096);
     } else if constexpr (COUNT == 4)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x400\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x800\n\t"
                      "global_load_lds_dwordx4 %1, %2 offset:0xc00" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
     else if constexpr (COUNT == 2)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:0x400" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
 }
 
@@ -599,7 +599,7 @@ template <int COUNT> __device__ __forceinline__ void kvc_copy(uint32_t lds, uint
 // R stages in LDS, straight from memory (pages are operands as they are), a quarter of each by every wave.  The one barrier of a step stands in the middle of its last chunk,
 // when all of the step's operands are in registers: behind it the next step's keys are read and this one's stage is requested anew.
 // 2048 rows of a 7B prompt's 8192 entries: 305 us, 690 TFLOP/s, or 1035 with the second parts of the probabilities, of the 1396 that a plain product of 8192^3 reaches (348 with NT = 1; 229 with
-// probabilities of 8 bits).  Per 32 entries and 16 columns there are 24 matrix instructions and 75 others, 8 of them exponentials; two waves on a SIMD, of different blocks, overlap them in part.
+// probabilities of 8 bits).  Per 32 entries and 16 columns there are 24 matrix instructions and 78 others, 8 of them exponentials, which a wave does in turn; two waves on a SIMD, of different blocks, overlap them in part.
 // Steps without a mask have a loop of their own: where both kinds met in one, every operand was copied.  The instance of NT = 2 at 128 dims spills 33 of 256 registers, all of them in the steps with
 // a mask, whose reloads wait for the ring's copies too; also where a window makes more of those it is ahead of NT = 1 (2048 rows of 8192, window 2000: 107 and 113 us).
 // 16 sequences of 17 .. 128 rows, 72B heads, fp32 (three parts), window 1000: 106 us, 0.87 executed PFLOP/s.  64 sequences of 128 .. 5120 entries, 5 rows each, 7B heads: 76 .. 78 us with the join, 4.5 TB/s;
